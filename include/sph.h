@@ -299,6 +299,110 @@ sph_status sph_fake_quant_backward(const sph_format* fmt, int64_t n, int64_t k, 
                                    const int64_t* d_offsets, float* d_grad_rho, float* d_grad_codebook, void* d_ws,
                                    size_t ws_bytes, void* stream);
 
+/* ---- Between the linear layers of a decoder block: rotary positions, the paged key-value cache and the
+ * attention that reads it. Activations are fp16 as the GEMMs take and give them (fp32 where stated). A
+ * "row" is one token's vector of one head: head_dim consecutive elements, 16-byte aligned. Token and
+ * head strides are in elements and keep that alignment (multiples of 8 for fp16, of 4 for fp32), so q, k
+ * and v may be column ranges of the fused product's output. Token counts are 0..2^26 (SPH_ERR_SHAPE for more, and where a
+ * call would need 2^32 threads of eight channels each); calls on no tokens do nothing. Values that only the device holds (positions, slots, lengths, pages) cannot be refused by the
+ * host; each call says what it does with wrong ones, and none reads or writes outside its arrays. ---- */
+
+/* Rotary positions: the first rot_dim channels of a row turn by position-dependent angles, the others
+ * stay. d_table: device fp32[max_pos][rot_dim/2][2] of (cos, sin) for every position and pair (e.g. from
+ * sph_rope_table), 16-byte aligned. flags: SPH_ROPE_INTERLEAVED pairs channels (2i, 2i+1), otherwise pair i
+ * is (i, i + rot_dim/2); SPH_ROPE_INVERSE turns back (sin -> -sin), which is also the gradient, since a
+ * rotation's transpose is its inverse and the table's common factor stays. */
+#define SPH_ROPE_INTERLEAVED 1
+#define SPH_ROPE_INVERSE 2
+typedef struct {
+  const float* d_table;
+  int64_t max_pos;      /* 1..2^31-1 */
+  int32_t rot_dim;      /* a positive multiple of 16, at most head_dim */
+  int32_t flags;
+} sph_rope_desc;
+
+/* Fill a table: (cos, sin)(p * inv_freq[i]) * magnitude for 0 <= p < max_pos, computed in fp64 and rounded
+ * once. inv_freq: HOST double[rot_dim/2] (read before the call returns), rot_dim a multiple of 16 up to 512.
+ * SPH_ERR_BAD_VALUE for a frequency or magnitude that is not finite. Asynchronous. */
+sph_status sph_rope_table(int32_t rot_dim, int64_t max_pos, const double* inv_freq, double magnitude, float* d_table,
+                          void* stream);
+
+/* y = rotated x: rows of `heads` heads (1..65535) of head_dim channels (a multiple of 16, at most 512) for each token, fp16 or
+ * fp32 (dtype), computed in fp32 and rounded once. d_pos: device int32[tokens]; a token whose position is
+ * outside 0..max_pos-1 gets NaN in the rotated channels. d_y may be d_x with the same strides.
+ * Asynchronous. */
+sph_status sph_rope(const sph_rope_desc* rope, sph_dtype dtype, int64_t tokens, int32_t heads, int32_t head_dim,
+                    const void* d_x, int64_t x_token_stride, int64_t x_head_stride, const int32_t* d_pos, void* d_y,
+                    int64_t y_token_stride, int64_t y_head_stride, void* stream);
+
+/* A key-value cache in pages of page_size tokens: a plain host-side value that describes caller-owned
+ * device arrays. Slot s is token s % page_size of page s / page_size. With 16 bits a row of d_k / d_v is
+ * head_dim fp16 numbers. With 8 or 4 bits it is head_dim codes (bytes; at 4 bits the 32-bit word w of a row
+ * holds channel 8w + 2i at bit 4i and channel 8w + 2i + 1 at bit 16 + 4i), and d_k_par / d_v_par hold an fp16
+ * pair (offset, step) for every 32 channels. A code q stands for the fp16 number nearest to
+ * offset + q * step; sph_kv_read and sph_attention see exactly these numbers. Strides are in bytes and
+ * common to keys and values: code strides multiples of 16, parameter strides multiples of 4; d_k and d_v 16-byte, parameter
+ * arrays 4-byte aligned. */
+typedef struct {
+  int32_t bits;         /* 16, 8 or 4 */
+  int32_t kv_heads;     /* 1..1024 */
+  int32_t head_dim;     /* 64, 96, 128, 192 or 256 */
+  int32_t page_size;    /* tokens a page: a power of two, at most 65536 */
+  int64_t n_pages;      /* n_pages * page_size < 2^31 */
+  void *d_k, *d_v;
+  int64_t page_stride, head_stride, token_stride;
+  void *d_k_par, *d_v_par;            /* NULL with 16 bits */
+  int64_t par_page_stride, par_head_stride, par_token_stride;
+} sph_kv_cache;
+
+/* Write one key row and one value row per token and kv head into the slots d_slots (device int32[tokens]).
+ * rope, if not NULL, rotates the keys on the way, and the queries d_q -> d_q_out (q_heads rows a token; both
+ * NULL and q_heads 0 for none; without rope no queries are taken) in the same launch. d_k, d_v, d_q: device rows of dtype (fp16 or
+ * fp32); d_q_out: fp16 rows, may be an fp16 d_q with the same strides. Quantising, per row and 32 channels of the
+ * fp32 (rotated) values x: offset = fp16(min x), step = fp16((max x - offset)/(2^bits - 1)),
+ * q = clip(round((x - offset)/step), 0, 2^bits - 1), half to even, 0 for a step of 0; 32 channels with an entry that is not finite (or
+ * too large for fp16) all read back as NaN. A slot outside the pool (such as -1 for padding) writes nothing; a position outside the
+ * table rotates to NaN. Two tokens of one call must not share a slot. Asynchronous. */
+sph_status sph_kv_append(const sph_kv_cache* cache, const sph_rope_desc* rope, sph_dtype dtype, int64_t tokens,
+                         const void* d_k, int64_t k_token_stride, int64_t k_head_stride, const void* d_v,
+                         int64_t v_token_stride, int64_t v_head_stride, const int32_t* d_slots, int32_t q_heads,
+                         const void* d_q, int64_t q_token_stride, int64_t q_head_stride, void* d_q_out,
+                         int64_t qo_token_stride, int64_t qo_head_stride, const int32_t* d_pos, void* stream);
+
+/* Read tokens back: d_k_out and d_v_out (device fp16[tokens][kv_heads][head_dim], contiguous) receive the
+ * rows of the slots d_slots (device int32[tokens], any order, repeats allowed). A slot outside the pool reads as zeros. Asynchronous. */
+sph_status sph_kv_read(const sph_kv_cache* cache, int64_t tokens, const int32_t* d_slots, void* d_k_out, void* d_v_out,
+                       void* stream);
+
+/* Attention of new tokens over a paged cache that already holds their keys and values (sph_kv_append
+ * first): sequence b has d_seq_lens[b] tokens (0..max_len), of which the last n_b are new and ask. Token j of the
+ * sequence is slot d_pages[b * pages_stride + j / page_size] * page_size + j % page_size. The query at
+ * position p sees the tokens j <= p, and with window > 0 only j > p - window; o = sum_j softmax_j(scale
+ * q.k_j) v_j, with query head h reading kv head h / (q_heads / kv_heads). A query that sees nothing
+ * gets zeros. Scores, the softmax's maximum and sum and the output are held in fp32; the weights
+ * exp(s - max) are rounded to fp16 for the matrix cores.
+ *
+ * d_q, d_o: device fp16 rows [tokens][q_heads]. d_q_start: device int32[batch + 1], ascending from 0 to
+ * `tokens`: sequence b's queries are tokens d_q_start[b]..d_q_start[b+1]-1, at most max_q of them; or NULL with
+ * max_q = 1 and tokens = batch: one each. d_seq_lens: device int32[batch]; d_pages: device int32[batch][pages_stride], at least
+ * ceil(max_len / page_size) entries each, of which only those below the sequence's length are read. max_len (0..2^30): the
+ * host's bound of the lengths; the launch is planned for it. d_lse: device fp32[tokens][q_heads], natural
+ * logarithm of sum_j exp(scale q.k_j) (-inf where nothing is seen), or NULL. scale must be finite. d_ws: at
+ * least sph_attention_workspace_bytes, 256-byte aligned, no initial contents; concurrent calls must not share one.
+ * Keys and values that no query sees are never used, whatever they hold. Queries of a sequence whose length is outside 0..max_len, whose start and count are
+ * outside their range, or that see a page outside the pool get NaN. Every sum runs in an order fixed by the
+ * arguments, so repeated calls give bitwise identical results. Asynchronous. */
+sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t tokens, int32_t q_heads, const void* d_q,
+                         int64_t q_token_stride, int64_t q_head_stride, const int32_t* d_q_start, int64_t max_q,
+                         const int32_t* d_pages, int64_t pages_stride, const int32_t* d_seq_lens, int64_t max_len,
+                         int64_t window, float scale, void* d_o, int64_t o_token_stride, int64_t o_head_stride,
+                         float* d_lse, void* d_ws, size_t ws_bytes, void* stream);
+
+/* Device workspace of sph_attention with these arguments on the current device (0 when it needs none): partial
+ * outputs where a sequence's length is split between workgroups. */
+sph_status sph_attention_workspace_bytes(const sph_kv_cache* cache, int64_t batch, int64_t tokens, int32_t q_heads,
+                                         int64_t max_q, int64_t max_len, int64_t window, size_t* bytes);
+
 /* Whether (dir_bits, radius_bits) is one of the built-in formats: 1 yes, 0 no. */
 int sph_format_supported(const sph_format* fmt);
 

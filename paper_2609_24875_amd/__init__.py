@@ -3,3 +3,5 @@ from .sph import (EXPORTS, FORMATS, LIB_PATH, SphError, SphLibraryMissing, SphWe
                   codes_to_host, encode, format_supported, gemm, gemm_small, gemm_small_noalloc, gemv,
                   kmeans_codebook, kmeans_workspace_bytes, load_library, pack, packed_bytes, status_str,
                   unpack, workspace_bytes)
+from .attn import (KVCache, attention, attention_workspace_bytes, kv_append, kv_read, rope,  # noqa: F401
+                   rope_frequencies, rope_table)

@@ -1,0 +1,356 @@
+"""Rotary positions, the paged key-value cache and its attention (include/sph.h): argument
+marshalling only, as in ``sph``.
+
+A decoder block runs ``gemm`` (fused q/k/v), ``kv_append`` (rotates keys and queries and writes the
+cache), ``attention`` and ``gemm`` (o); ``block.AttentionBlock`` does so. The cache's pages are plain
+torch tensors that the caller may hold, copy and share between layers' handles.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+
+import numpy as np
+
+from .sph import SPH_F16, SPH_F32, SphError, _check, _stream_handle, load_library
+
+ROPE_INTERLEAVED, ROPE_INVERSE = 1, 2
+KV_BITS = (16, 8, 4)
+KV_HEAD_DIMS = (64, 96, 128, 192, 256)
+KV_GROUP = 32                       # channels that share an offset and a step
+
+
+class CRope(ctypes.Structure):
+    _fields_ = [("d_table", ctypes.c_void_p), ("max_pos", ctypes.c_int64), ("rot_dim", ctypes.c_int32),
+                ("flags", ctypes.c_int32)]
+
+
+class CKVCache(ctypes.Structure):
+    _fields_ = [("bits", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int64), ("d_k", ctypes.c_void_p),
+                ("d_v", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64), ("d_k_par", ctypes.c_void_p), ("d_v_par", ctypes.c_void_p),
+                ("par_page_stride", ctypes.c_int64), ("par_head_stride", ctypes.c_int64),
+                ("par_token_stride", ctypes.c_int64)]
+
+
+_declared = None
+
+
+def _library():
+    global _declared
+    if _declared is None:
+        lib = load_library()
+        P, I64, SZ, I32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_size_t, ctypes.c_int32
+        pr, pc = ctypes.POINTER(CRope), ctypes.POINTER(CKVCache)
+        lib.sph_rope_table.argtypes = [I32, I64, ctypes.POINTER(ctypes.c_double), ctypes.c_double, P, P]
+        lib.sph_rope.argtypes = [pr, I32, I64, I32, I32, P, I64, I64, P, P, I64, I64, P]
+        lib.sph_kv_append.argtypes = [pc, pr, I32, I64, P, I64, I64, P, I64, I64, P, I32, P, I64, I64, P, I64, I64, P, P]
+        lib.sph_kv_read.argtypes = [pc, I64, P, P, P, P]
+        lib.sph_attention.argtypes = [pc, I64, I64, I32, P, I64, I64, P, I64, P, I64, P, I64, I64, ctypes.c_float,
+                                      P, I64, I64, P, P, SZ, P]
+        lib.sph_attention_workspace_bytes.argtypes = [pc, I64, I64, I32, I64, I64, I64, ctypes.POINTER(SZ)]
+        for name in ("sph_rope_table", "sph_rope", "sph_kv_append", "sph_kv_read", "sph_attention",
+                     "sph_attention_workspace_bytes"):
+            getattr(lib, name).restype = ctypes.c_int
+        _declared = lib
+    return _declared
+
+
+# ------------------------------------------------------------------ rotary positions
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                     original_max_pos: int = 4096, beta_fast: float = 32.0, beta_slow: float = 1.0):
+    """(angle per position of each pair, fp64 [rot_dim/2]; common factor of cos and sin).
+
+    base^(-2i/rot_dim), for longer contexts than a model was trained on scaled by one of
+    "linear"  every frequency divided by ``factor``;
+    "ntk"     the base grown by factor^(rot_dim/(rot_dim-2)), which leaves the fastest pair and divides the
+              slowest by ``factor``;
+    "yarn"    pairs that turn more than ``beta_fast`` times over ``original_max_pos`` tokens kept, those
+              with fewer than ``beta_slow`` turns divided by ``factor``, a linear ramp over the pair index between, and cos and sin times
+              0.1 ln(factor) + 1.
+    """
+    if rot_dim < 16 or rot_dim % 16 or not base > 1.0 or not factor >= 1.0:
+        raise ValueError("rot_dim must be a positive multiple of 16, base above 1, factor at least 1")
+    i = np.arange(rot_dim // 2, dtype=np.float64)
+    if scaling == "ntk":
+        base = base * factor ** (rot_dim / (rot_dim - 2))
+    f = base ** (-2.0 * i / rot_dim)
+    if scaling in ("none", "ntk"):
+        return f, 1.0
+    if scaling == "linear":
+        return f / factor, 1.0
+    if scaling == "yarn":
+        # the pair that makes `turns` turns over the original context
+        def pair(turns):
+            return rot_dim * math.log(original_max_pos / (turns * 2.0 * math.pi)) / (2.0 * math.log(base))
+        lo, hi = max(math.floor(pair(beta_fast)), 0), min(math.ceil(pair(beta_slow)), rot_dim // 2 - 1)
+        keep = 1.0 - np.clip((i - lo) / max(hi - lo, 1e-3), 0.0, 1.0)
+        return f * keep + f / factor * (1.0 - keep), 0.1 * math.log(factor) + 1.0
+    raise ValueError(f"scaling must be none, linear, ntk or yarn, not {scaling!r}")
+
+
+def rope_table(rot_dim: int, max_pos: int, device="cuda", stream=None, **scaling):
+    """fp32 [max_pos][rot_dim/2][2] of (cos, sin) (sph_rope_table); keywords as ``rope_frequencies``."""
+    import torch
+    f, magnitude = rope_frequencies(rot_dim, **scaling)
+    out = torch.empty((max_pos, rot_dim // 2, 2), dtype=torch.float32, device=device)
+    arr = (ctypes.c_double * len(f))(*f)
+    _check(_library().sph_rope_table(rot_dim, max_pos, arr, magnitude, out.data_ptr(), _stream_handle(stream)), "sph_rope_table")
+    return out
+
+
+def _ints(t, name: str, device, count: int | None = None):
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32:
+        raise TypeError(f"{name} must be a torch.int32 tensor")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the rows on {device}")
+    if t.dim() != 1 or (count is not None and t.shape[0] != count) or (t.shape[0] > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be contiguous [{count}], got shape {tuple(t.shape)} and strides {tuple(t.stride())}")
+    return t.data_ptr()
+
+
+def _rows(t, name: str, device, dtypes, shape=None):
+    """Checks [tokens][heads][channels] rows with unit channel stride; (pointer, token stride, head stride)."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
+        raise TypeError(f"{name} must be a tensor of {' or '.join(str(d) for d in dtypes)}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.dim() != 3 or (shape is not None and tuple(t.shape) != shape) or (t.numel() > 0 and t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name} must be {list(shape) if shape else '[tokens][heads][channels]'} with unit channel stride, got "
+                         f"shape {tuple(t.shape)} and strides {tuple(t.stride())}")
+    n, h, _ = t.shape
+    # the stride of a dimension of one element is never used and may hold anything
+    return t.data_ptr(), t.stride(0) if n > 1 else 0, t.stride(1) if h > 1 else 0
+
+
+def _rope_desc(table, device, interleaved: bool, inverse: bool) -> CRope:
+    import torch
+    if not isinstance(table, torch.Tensor) or table.dtype != torch.float32:
+        raise TypeError("table must be a torch.float32 tensor")
+    if table.device != device:
+        raise ValueError(f"table is on {table.device}, the rows on {device}")
+    if table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous():
+        raise ValueError(f"table must be contiguous [positions][pairs][2], got shape {tuple(table.shape)}")
+    return CRope(table.data_ptr(), table.shape[0], 2 * table.shape[1],
+                 (ROPE_INTERLEAVED if interleaved else 0) | (ROPE_INVERSE if inverse else 0))
+
+
+def aligned_rows(t):
+    """``t`` itself where its rows suit the library (unit channel stride, 16-byte aligned, no broadcast), else a copy: what
+    autograd hands a backward pass may be any view."""
+    per = 16 // t.element_size()
+    ok = t.stride(-1) == 1 and t.data_ptr() % 16 == 0 and all(t.stride(d) % per == 0 for d in range(t.dim() - 1) if t.shape[d] > 1)
+    return t if ok else t.contiguous()
+
+
+def rope(x, positions, table, interleaved: bool = False, inverse: bool = False, out=None, stream=None):
+    """Rotary positions of device rows x[tokens][heads][channels], fp16 or fp32 (sph_rope): the first
+    2 * table.shape[1] channels of each row turn by the angles of its token's position, the others are
+    copied. ``inverse`` turns back and is the gradient (``train.rope`` is the differentiable form).
+    ``out`` may be x."""
+    import torch
+    px, xt, xh = _rows(x, "x", None, (torch.float16, torch.float32))
+    desc = _rope_desc(table, x.device, interleaved, inverse)
+    pos = _ints(positions, "positions", x.device, x.shape[0])
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    py, yt, yh = _rows(out, "out", x.device, (x.dtype,), tuple(x.shape))
+    _check(_library().sph_rope(ctypes.byref(desc), SPH_F16 if x.dtype == torch.float16 else SPH_F32, x.shape[0], x.shape[1],
+                               x.shape[2], px, xt, xh, pos, py, yt, yh, _stream_handle(stream)), "sph_rope")
+    return out
+
+
+# ------------------------------------------------------------------ the cache
+
+class KVCache:
+    """A paged key-value cache over caller-owned tensors (sph_kv_cache): ``k`` and ``v``
+    [pages][kv heads][tokens a page][channels], fp16 with ``bits`` 16; with 8 or 4 bits uint8 codes
+    ([..][channels * bits / 8]) and ``k_par``, ``v_par`` fp16 [pages][kv heads][tokens a page][channels / 32][2]
+    of (offset, step). Any strides of the first three dimensions that keep rows 16-byte aligned and are the
+    same for keys and values, so both may be views of one allocation or of another order. The handle keeps the
+    attention's workspaces, one a stream."""
+
+    def __init__(self, k, v, k_par=None, v_par=None, bits: int = 16):
+        import torch
+        if bits not in KV_BITS:
+            raise ValueError(f"bits must be one of {KV_BITS}")
+        want = torch.float16 if bits == 16 else torch.uint8
+        for t, name in ((k, "k"), (v, "v")):
+            if not isinstance(t, torch.Tensor) or t.dtype != want:
+                raise TypeError(f"{name} must be a {want} tensor for {bits} bits")
+            if t.dim() != 4 or t.stride(3) != 1:
+                raise ValueError(f"{name} must be [pages][kv heads][tokens a page][channels] with unit channel stride")
+        strides = self._strides(k, k.element_size())
+        if v.shape != k.shape or v.device != k.device or self._strides(v, v.element_size()) != strides:
+            raise ValueError("k and v must have the same shape, device and strides")
+        pages, heads, page, width = k.shape
+        dim = width * 8 // bits if bits < 16 else width
+        par = (0, 0, 0)
+        if bits < 16:
+            for t, name in ((k_par, "k_par"), (v_par, "v_par")):
+                if not isinstance(t, torch.Tensor) or t.dtype != torch.float16:
+                    raise TypeError(f"{name} must be a torch.float16 tensor for {bits} bits")
+                if tuple(t.shape) != (pages, heads, page, dim // KV_GROUP, 2) or t.device != k.device or t.stride(4) != 1 or \
+                        (t.shape[3] > 1 and t.stride(3) != 2):
+                    raise ValueError(f"{name} must be [{pages}][{heads}][{page}][{dim // KV_GROUP}][2] on {k.device} with contiguous pairs")
+            par = self._strides(k_par, 2)
+            if self._strides(v_par, 2) != par:
+                raise ValueError("k_par and v_par must have the same strides")
+        elif k_par is not None or v_par is not None:
+            raise ValueError("a 16-bit cache has no offsets and steps")
+        self.k, self.v, self.k_par, self.v_par = k, v, k_par, v_par
+        self.bits, self.n_pages, self.kv_heads, self.page_size, self.head_dim = bits, pages, heads, page, dim
+        self.device = k.device
+        self.workspaces = {}
+        self.desc = CKVCache(bits, heads, dim, page, pages, k.data_ptr(), v.data_ptr(), *strides,
+                             k_par.data_ptr() if bits < 16 else None, v_par.data_ptr() if bits < 16 else None, *par)
+        self._ref = ctypes.byref(self.desc)
+
+    @staticmethod
+    def _strides(t, size: int):
+        # a dimension of one element may carry any stride: the library is told what a contiguous one would have
+        got, inner = [], t.shape[3] * size * (t.shape[4] if t.dim() == 5 else 1)
+        for d in (2, 1, 0):
+            st = t.stride(d) * size if t.shape[d] > 1 else inner
+            got.append(st)
+            inner = max(inner, st * t.shape[d])
+        return tuple(reversed(got))
+
+    @classmethod
+    def empty(cls, n_pages: int, kv_heads: int, head_dim: int, page_size: int = 64, bits: int = 16, device="cuda"):
+        """A cache over new tensors (uninitialised: slots are written before they are read)."""
+        import torch
+        if bits not in KV_BITS or head_dim not in KV_HEAD_DIMS:
+            raise ValueError(f"bits must be one of {KV_BITS}, head_dim one of {KV_HEAD_DIMS}")
+        shape = (n_pages, kv_heads, page_size)
+        if bits == 16:
+            return cls(*(torch.empty((*shape, head_dim), dtype=torch.float16, device=device) for _ in range(2)))
+        codes = [torch.empty((*shape, head_dim * bits // 8), dtype=torch.uint8, device=device) for _ in range(2)]
+        par = [torch.empty((*shape, head_dim // KV_GROUP, 2), dtype=torch.float16, device=device) for _ in range(2)]
+        return cls(*codes, *par, bits=bits)
+
+    @property
+    def nbytes(self) -> int:
+        return sum(t.numel() * t.element_size() for t in (self.k, self.v, self.k_par, self.v_par) if t is not None)
+
+
+def kv_append(cache: KVCache, k, v, slots, positions=None, table=None, interleaved: bool = False, q=None, q_out=None, stream=None):
+    """Write a key and a value row per token and head, k and v [tokens][kv heads][channels] (fp16 or fp32,
+    any row strides), to the int32 ``slots`` (sph_kv_append; page * page_size + place in the page, -1 for a padding token). With
+    ``table`` and ``positions`` the keys are rotated on the way, and so are the queries q [tokens][q heads][channels] in
+    the same launch. Returns the rotated queries in fp16 (``q_out`` or a new tensor; None without q)."""
+    import torch
+    n = k.shape[0] if isinstance(k, torch.Tensor) and k.dim() else 0
+    shape = (n, cache.kv_heads, cache.head_dim)
+    dt = (k.dtype,) if isinstance(k, torch.Tensor) and k.dtype in (torch.float16, torch.float32) else (torch.float16, torch.float32)
+    pk, kt, kh = _rows(k, "k", cache.device, dt, shape)
+    pv, vt, vh = _rows(v, "v", cache.device, dt, shape)
+    ps = _ints(slots, "slots", cache.device, n)
+    desc = pos = None
+    if table is not None:
+        desc = ctypes.byref(_rope_desc(table, cache.device, interleaved, False))
+        pos = _ints(positions, "positions", cache.device, n)
+    elif positions is not None or q is not None:
+        raise ValueError("positions and q need a table")
+    pq = po = None
+    heads = qt = qh = ot = oh = 0
+    if q is not None:
+        heads = q.shape[1] if q.dim() == 3 else 0
+        pq, qt, qh = _rows(q, "q", cache.device, dt, (n, heads, cache.head_dim))
+        if q_out is None:
+            q_out = torch.empty((n, heads, cache.head_dim), dtype=torch.float16, device=cache.device)
+        po, ot, oh = _rows(q_out, "q_out", cache.device, (torch.float16,), (n, heads, cache.head_dim))
+    _check(_library().sph_kv_append(cache._ref, desc, SPH_F16 if dt[0] == torch.float16 else SPH_F32, n, pk, kt, kh, pv, vt, vh, ps,
+                                    heads, pq, qt, qh, po, ot, oh, pos, _stream_handle(stream)), "sph_kv_append")
+    return q_out if q is not None else None
+
+
+def kv_read(cache: KVCache, slots, out=None, stream=None):
+    """The keys and values of int32 ``slots`` as two fp16 tensors [tokens][kv heads][channels]
+    (sph_kv_read); rows of slots outside the pool are zero. ``out``: a pair of contiguous tensors."""
+    import torch
+    ps = _ints(slots, "slots", cache.device)
+    shape = (slots.shape[0], cache.kv_heads, cache.head_dim)
+    if out is None:
+        out = tuple(torch.empty(shape, dtype=torch.float16, device=cache.device) for _ in range(2))
+    for t in out:
+        if t.dtype != torch.float16 or t.device != cache.device or tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError(f"out must be two contiguous fp16 tensors of shape {shape} on {cache.device}")
+    _check(_library().sph_kv_read(cache._ref, shape[0], ps, out[0].data_ptr(), out[1].data_ptr(), _stream_handle(stream)), "sph_kv_read")
+    return out
+
+
+# ------------------------------------------------------------------ attention
+
+def attention_workspace_bytes(cache: KVCache, batch: int, tokens: int, q_heads: int, max_q: int, max_len: int, window: int = 0) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_library().sph_attention_workspace_bytes(cache._ref, batch, tokens, q_heads, max_q, max_len, window, ctypes.byref(out)),
+           "sph_attention_workspace_bytes")
+    return out.value
+
+
+def _attention_workspace(cache: KVCache, need: int, handle: int, stream):
+    """A workspace of at least ``need`` bytes for calls on the stream ``handle``, kept with the cache and grown when a
+    call needs more; streams do not share one, since their calls may run together."""
+    import torch
+    if need == 0:
+        return None, 0
+    ws = cache.workspaces.get(handle)
+    if ws is None or ws.numel() < need:
+        if torch.cuda.is_current_stream_capturing():
+            # memory of the graph's own pool must not serve later calls outside it
+            raise RuntimeError("no workspace of this size on this stream yet: make one call on the capture stream before "
+                               "capturing a graph")
+        # allocated on the stream that uses it, so that the one it replaces is freed behind that stream's calls
+        with torch.cuda.stream(stream):
+            ws = torch.empty(need, dtype=torch.uint8, device=cache.device)
+        cache.workspaces[handle] = ws
+    return ws.data_ptr(), ws.numel()
+
+
+def attention(q, cache: KVCache, pages, seq_lens, q_start=None, max_q: int = 1, max_len: int | None = None, window: int = 0,
+              scale: float | None = None, out=None, return_lse: bool = False, stream=None):
+    """Attention of new tokens over a cache that already holds their keys and values (sph_attention).
+
+    q: fp16 [tokens][q heads][channels] (rotated). pages: int32 [batch][columns], the pages of every sequence in
+    order. seq_lens: int32 [batch], tokens in the cache with the new ones. Sequence b asks with its last
+    q_start[b+1] - q_start[b] tokens (at most ``max_q``), or without q_start with its last one. A query sees the tokens up to its
+    own, with ``window`` only the last ``window`` of them. max_len: bound of the lengths that the launch is planned for
+    (default: what the pages' columns hold). scale: default channels^-0.5. Returns fp16 o like q, with ``return_lse`` also fp32
+    [tokens][q heads], the logarithm of each softmax's sum."""
+    import torch
+    pq, qt, qh = _rows(q, "q", cache.device, (torch.float16,))
+    n, heads, dim = q.shape
+    if dim != cache.head_dim:
+        raise ValueError(f"q has {dim} channels a head, the cache {cache.head_dim}")
+    if not isinstance(pages, torch.Tensor) or pages.dtype != torch.int32:
+        raise TypeError("pages must be a torch.int32 tensor")
+    if pages.dim() != 2 or pages.device != cache.device or (pages.numel() > 0 and pages.shape[1] > 1 and pages.stride(1) != 1):
+        raise ValueError(f"pages must be [batch][columns] on {cache.device} with unit stride along the columns")
+    batch, cols = pages.shape
+    lens = _ints(seq_lens, "seq_lens", cache.device, batch)
+    start = None
+    if q_start is not None:
+        start = _ints(q_start, "q_start", cache.device, batch + 1)
+    held = cols * cache.page_size
+    if max_len is None:
+        max_len = held
+    elif max_len > held:
+        raise ValueError(f"max_len {max_len} is more than the {cols} columns of pages hold")
+    stride = pages.stride(0) if batch > 1 else cols
+    if stride < cols:
+        raise ValueError("rows of pages must not overlap")
+    if out is None:
+        out = torch.empty((n, heads, dim), dtype=torch.float16, device=cache.device)
+    po, ot, oh = _rows(out, "out", cache.device, (torch.float16,), (n, heads, dim))
+    lse = torch.empty((n, heads), dtype=torch.float32, device=cache.device) if return_lse else None
+    handle = _stream_handle(stream)
+    ws, nb = _attention_workspace(cache, attention_workspace_bytes(cache, batch, n, heads, max_q, max_len, window), handle, stream)
+    _check(_library().sph_attention(cache._ref, batch, n, heads, pq, qt, qh, start, max_q, pages.data_ptr(), stride, lens, max_len,
+                                    window, dim ** -0.5 if scale is None else scale, po, ot, oh,
+                                    lse.data_ptr() if return_lse else None, ws, nb, handle), "sph_attention")
+    return (out, lse) if return_lse else out

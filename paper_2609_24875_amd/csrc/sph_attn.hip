@@ -1,0 +1,411 @@
+// Attention of new tokens over the paged key-value cache (sph_attention).
+//
+// For one kv head, row r = t * group + h is new token t under query head h of the head's group. A workgroup
+// takes 16 rows and a stretch of keys; its waves take tiles of 32 keys in turn, each with a running
+// maximum m and sum l per row (o and l scale by exp(m_old - m_new) when m grows), and meet in LDS at the
+// end. A long sequence is cut into stretches for several workgroups, whose partial (o, m, l) a second kernel joins in order.
+//
+// Products are v_mfma_f32_16x16x32_f16. S^T = K Q^T has a row per key and a column per query row, so a
+// lane keeps eight keys of one row: with the key in matrix row m of tile t chosen as 8 (m / 4) + 4 t + m % 4,
+// they are the eight consecutive keys 8 (lane / 16) .. + 7 that the B operand of O^T = V^T P^T wants from the
+// same lane, and the weights go from one product to the next without leaving their lane. V^T's operand comes
+// from rows staged in LDS by transposing reads.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "sph_cache.h"
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kTile = 32;                 // keys of a wave's step
+constexpr int kRows = 16;                 // rows of a workgroup
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+struct AttnArgs {
+  CacheView c;
+  const char* q;
+  char* o;
+  int64_t qt, qh, ot, oh;  // strides in bytes
+  const int32_t* q_start;
+  const int32_t* pages;
+  int64_t pages_stride;
+  const int32_t* lens;
+  float* lse;
+  float* part;             // [splits][tokens][q_heads][dim], then (m, l) pairs [splits][tokens][q_heads]
+  float2* ml;
+  int64_t tokens;
+  int batch, q_heads, group, max_q, max_len, window, tiles, splits, chunk;
+  float scale;             // times log2 e
+};
+
+// The queries of one sequence.
+struct Seq {
+  int start, n, len;
+  bool bad;
+  __device__ __forceinline__ void load(const AttnArgs& a, int b) {
+    start = a.q_start ? a.q_start[b] : b;
+    const int end = a.q_start ? a.q_start[b + 1] : b + 1;
+    n = end - start;
+    len = a.lens[b];
+    bad = len < 0 || len > a.max_len || start < 0 || end > a.tokens || n < 0 || n > a.max_q;
+  }
+};
+
+__device__ __forceinline__ void write_out(const AttnArgs& a, int split, int64_t token, int head, int ch, f32x4 acc, float m, float l) {
+  if (a.splits > 1) {
+    const int64_t row = (split * a.tokens + token) * a.q_heads + head;
+    *(f32x4*)(a.part + row * a.c.dim + ch) = acc;
+    if (ch == 0) a.ml[row] = make_float2(m, l);
+    return;
+  }
+  // l is NaN for poisoned rows; 0 where nothing is seen
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  f16x4 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = (_Float16)(l == 0.0f ? 0.0f : acc[i] * inv);
+  *(f16x4*)(a.o + token * a.ot + head * a.oh + 2 * ch) = y;
+  if (ch == 0 && a.lse) a.lse[token * a.q_heads + head] = l == 0.0f ? -INFINITY : (m + __builtin_log2f(l)) * kLn2;
+}
+
+// Every row of a sequence that the device found to be outside its bounds becomes NaN.
+__device__ void write_bad(const AttnArgs& a, const Seq& s, int kvh, int split) {
+  const int64_t t0 = max(s.start, 0), t1 = min((int64_t)s.start + s.n, a.tokens);
+  const float nan = __builtin_nanf("");
+  const int per = a.group * (a.c.dim / 4);
+  for (int64_t t = t0; t < t1; ++t)
+    for (int i = threadIdx.x; i < per; i += blockDim.x)
+      write_out(a, split, t, kvh * a.group + i / (a.c.dim / 4), i % (a.c.dim / 4) * 4, f32x4{nan, nan, nan, nan}, 0.0f, nan);
+}
+
+template <int DIM, int BITS>
+struct Lay {
+  static constexpr int kRowBytes = DIM * BITS / 8;
+  // bytes of a key row that one of its four lanes loads at once
+  static constexpr int kPiece = kRowBytes % 64 == 0 ? 16 : kRowBytes % 32 == 0 ? 8 : 4;
+  static constexpr int kLoads = kRowBytes / (4 * kPiece);
+  static constexpr int kPieceCh = kPiece * 8 / BITS;
+  static constexpr int kSteps = DIM / 32;
+  static constexpr int kBlocks = kPieceCh / 8;              // products of a piece
+  // a value row's pieces: 16 bytes, and with codes 16 channels
+  static constexpr int kVCh = BITS == 16 ? 8 : 16;
+  static constexpr int kVPer = DIM / kVCh;
+  static constexpr int kVLoads = kTile * kVPer / 64;
+  static constexpr int kVStride = DIM * 2 + 32;             // bytes between rows in LDS: four rows' transposed read hits all banks
+};
+
+template <int BYTES>
+__device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
+  if constexpr (BYTES == 16) {
+    const uint4 v = *(const uint4*)p;
+    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+  } else if constexpr (BYTES == 8) {
+    const uint2 v = *(const uint2*)p;
+    w[0] = v.x, w[1] = v.y;
+  } else {
+    w[0] = *(const uint32_t*)p;
+  }
+}
+
+template <int DIM, int BITS>
+__global__ __launch_bounds__(kThreads) void k_attn(AttnArgs a) {
+  typedef Lay<DIM, BITS> L;
+  constexpr int kVBytes = kTile * L::kVStride, kOStride = DIM + 4;
+  constexpr int kLds = kWaves * (kVBytes > kRows * kOStride * 4 ? kVBytes : kRows * kOStride * 4);
+  __shared__ __attribute__((aligned(16))) char lds[kLds];
+  __shared__ float2 ml_s[kWaves][kRows];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, g4 = lane >> 4;
+  uint32_t id = blockIdx.x;
+  const int kvh = id % a.c.kv_heads;
+  id /= a.c.kv_heads;
+  const int split = id % a.splits;
+  id /= a.splits;
+  const int tile = id % a.tiles, b = id / a.tiles;
+  Seq s;
+  s.load(a, b);
+  if (s.bad) {
+    if (tile == 0) write_bad(a, s, kvh, split);
+    return;
+  }
+  const int rows = s.n * a.group, r0 = tile * kRows;
+  if (r0 >= rows) return;
+  const int nrow = min(kRows, rows - r0);
+  const int first = s.len - s.n;                            // position of the first new token
+  const int t_lo = r0 / a.group, t_hi = (r0 + nrow - 1) / a.group;
+  const int lo = a.window ? max(0, first + t_lo - a.window + 1) : 0, hi = first + t_hi + 1;
+  const int k_lo = max(lo, (lo & ~(kTile - 1)) + split * a.chunk), k_hi = min(hi, (lo & ~(kTile - 1)) + (split + 1) * a.chunk);
+
+  const int r = r0 + min(col, nrow - 1);
+  const int t = r / a.group, h = kvh * a.group + r % a.group;
+  const int pos = first + t, see = a.window ? pos - a.window : -1;  // keys see + 1 .. pos
+
+  f32x4 o[DIM / 16] = {};
+  float m = -INFINITY, l = 0.0f;
+  if (k_lo < k_hi) {
+    f16x8 q[L::kSteps];
+    const char* qr = a.q + (s.start + t) * a.qt + h * a.qh;
+#pragma unroll
+    for (int i = 0; i < L::kLoads; ++i)
+#pragma unroll
+      for (int j = 0; j < L::kBlocks; ++j)
+        q[i * L::kBlocks + j] = *(const f16x8*)(qr + 2 * ((4 * i + g4) * L::kPieceCh + 8 * j));
+    const int32_t* pages = a.pages + b * a.pages_stride;
+    const int pmask = (1 << a.c.page_shift) - 1;
+    const char* kb = a.c.k + kvh * a.c.head_stride;
+    const char* vb = a.c.v + kvh * a.c.head_stride;
+    const char* kpb = a.c.k_par + kvh * a.c.par_head_stride;
+    const char* vpb = a.c.v_par + kvh * a.c.par_head_stride;
+    char* vs = lds + wave * kVBytes;
+
+    for (int kt = (k_lo & ~(kTile - 1)) + kTile * wave; kt < k_hi; kt += kTile * kWaves) {
+      // scores
+      f32x4 st[2] = {};
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int key = min(max(kt + 8 * (col >> 2) + 4 * u + (col & 3), k_lo), k_hi - 1);
+        const int page = pages[key >> a.c.page_shift];
+        const bool there = (unsigned)page < (uint64_t)a.c.n_pages;
+        const int64_t pg = there ? page : 0;
+        const char* kr = kb + pg * a.c.page_stride + (key & pmask) * a.c.token_stride;
+        const char* pr = kpb + pg * a.c.par_page_stride + (key & pmask) * a.c.par_token_stride;
+#pragma unroll
+        for (int i = 0; i < L::kLoads; ++i) {
+          uint32_t w[4];
+          load_words<L::kPiece>(kr + (4 * i + g4) * L::kPiece, w);
+#pragma unroll
+          for (int j = 0; j < L::kBlocks; ++j) {
+            f16x8 kv;
+            if constexpr (BITS == 16) {
+              kv = __builtin_bit_cast(f16x8, make_uint4(w[0], w[1], w[2], w[3]));
+            } else {
+              const uint32_t par = *(const uint32_t*)(pr + ((4 * i + g4) * L::kPieceCh + 8 * j) / 32 * 4);
+              kv = BITS == 8 ? decode8w<8>(w[2 * j], w[2 * j + 1], par) : decode8w<4>(w[j], 0, par);
+            }
+            const _Float16 nan = __builtin_bit_cast(_Float16, (uint16_t)0x7E00);
+            if (!there) kv = f16x8{nan, nan, nan, nan, nan, nan, nan, nan};
+            st[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv, q[i * L::kBlocks + j], st[u], 0, 0, 0);
+          }
+        }
+      }
+      // values into LDS
+#pragma unroll
+      for (int i = 0; i < L::kVLoads; ++i) {
+        const int p = lane + 64 * i, kk = p / L::kVPer, piece = p % L::kVPer;
+        const int key = min(max(kt + kk, k_lo), k_hi - 1);
+        const int page = pages[key >> a.c.page_shift];
+        const bool there = (unsigned)page < (uint64_t)a.c.n_pages && key == kt + kk;
+        const int64_t pg = there ? page : 0;
+        const char* vr = vb + pg * a.c.page_stride + (key & pmask) * a.c.token_stride;
+        f16x8 v[2];
+        if constexpr (BITS == 16) {
+          v[0] = *(const f16x8*)(vr + 16 * piece);
+        } else {
+          const uint32_t par = *(const uint32_t*)(vpb + pg * a.c.par_page_stride + (key & pmask) * a.c.par_token_stride + piece / 2 * 4);
+          v[0] = decode8<BITS>(vr + piece * 2 * BITS, par);
+          v[1] = decode8<BITS>(vr + piece * 2 * BITS + BITS, par);
+        }
+#pragma unroll
+        for (int j = 0; j < L::kVCh / 8; ++j) {
+          if (!there) v[j] = f16x8{};
+          *(f16x8*)(vs + kk * L::kVStride + (piece * L::kVCh + 8 * j) * 2) = v[j];
+        }
+      }
+      // weights
+      float x[8], top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int key = kt + 8 * g4 + i;
+        x[i] = key <= pos && key > see && key >= k_lo && key < k_hi ? st[i >> 2][i & 3] * a.scale : -INFINITY;
+        top = fmaxf(top, x[i]);
+      }
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float mn = fmaxf(m, top), base = mn == -INFINITY ? 0.0f : mn;
+      const float keep = __builtin_amdgcn_exp2f(m - base);
+      m = mn;
+      l *= keep;
+#pragma unroll
+      for (int i = 0; i < DIM / 16; ++i) o[i] *= keep;
+      f16x8 p;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float e = __builtin_amdgcn_exp2f(x[i] - base);
+        l += e;
+        p[i] = (_Float16)e;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int i = 0; i < DIM / 16; ++i) {
+        f16x8 vt;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const s16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) s16x4*)(vs + (8 * g4 + 4 * j + (col >> 2)) * L::kVStride + 32 * i + 8 * (col & 3)));
+          const f16x4 f = __builtin_bit_cast(f16x4, w);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) vt[4 * j + e] = f[e];
+        }
+        o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, p, o[i], 0, 0, 0);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+  }
+
+  // the waves' parts meet
+  __syncthreads();
+  float* os = (float*)lds + wave * kRows * kOStride;
+  if (g4 == 0) ml_s[wave][col] = make_float2(m, l);
+#pragma unroll
+  for (int i = 0; i < DIM / 16; ++i) *(f32x4*)(os + col * kOStride + 16 * i + 4 * g4) = o[i];
+  __syncthreads();
+  for (int i = threadIdx.x; i < nrow * (DIM / 4); i += kThreads) {
+    const int row = i / (DIM / 4), ch = i % (DIM / 4) * 4;
+    float mm = ml_s[0][row].x;
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) mm = fmaxf(mm, ml_s[w][row].x);
+    const float base = mm == -INFINITY ? 0.0f : mm;
+    f32x4 acc = {};
+    float ll = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(ml_s[w][row].x - base);
+      ll += f * ml_s[w][row].y;
+      acc += f * *(const f32x4*)((float*)lds + (w * kRows + row) * kOStride + ch);
+    }
+    const int rr = r0 + row;
+    write_out(a, split, s.start + rr / a.group, kvh * a.group + rr % a.group, ch, acc, mm, ll);
+  }
+}
+
+// One workgroup a row: the stretches' parts in order. Stretches without a seen key have l = 0 and are not read.
+__global__ __launch_bounds__(64) void k_attn_join(AttnArgs a) {
+  const int64_t row = blockIdx.x, rows = a.tokens * a.q_heads;
+  float mm = -INFINITY;
+  for (int s = 0; s < a.splits; ++s) mm = fmaxf(mm, a.ml[s * rows + row].x);
+  const float base = mm == -INFINITY ? 0.0f : mm;
+  const int ch = threadIdx.x * 4;
+  f32x4 acc = {};
+  float l = 0.0f;
+  for (int s = 0; s < a.splits; ++s) {
+    const float2 p = a.ml[s * rows + row];
+    if (p.y == 0.0f) continue;
+    const float f = __builtin_amdgcn_exp2f(p.x - base);
+    l += f * p.y;
+    if (ch < a.c.dim) acc += f * *(const f32x4*)(a.part + (s * rows + row) * a.c.dim + ch);
+  }
+  a.splits = 1;
+  if (ch < a.c.dim) write_out(a, 0, row / a.q_heads, (int)(row % a.q_heads), ch, acc, mm, l);
+}
+
+// ------------------------------------------------------------------ host side
+
+struct Plan {
+  int tiles, splits, chunk;
+  size_t bytes;
+};
+
+// Stretches of at least 128 keys (one tile a wave), and few enough workgroups that each has work for a while.
+Plan plan_of(const sph_kv_cache* c, int64_t batch, int64_t tokens, int q_heads, int64_t max_q, int64_t max_len, int64_t window) {
+  Plan p{};
+  const int group = q_heads / c->kv_heads;
+  p.tiles = (int)((max_q * group + kRows - 1) / kRows);
+  const int64_t span = window > 0 ? std::min<int64_t>(max_len, window + kRows / group + 1 + kTile) : max_len;
+  const int64_t units = (int64_t)c->kv_heads * batch * p.tiles, step = kTile * kWaves;
+  const int64_t want = std::max<int64_t>(1, 2048 / units);
+  int64_t chunk = (span + want - 1) / want;
+  chunk = std::max<int64_t>(step, (chunk + step - 1) / step * step);
+  p.chunk = (int)chunk;
+  p.splits = (int)std::max<int64_t>(1, (span + chunk - 1) / chunk);
+  if (p.splits > 1) p.bytes = (size_t)p.splits * tokens * q_heads * (c->head_dim + 2) * sizeof(float);
+  return p;
+}
+
+sph_status check_sizes(const sph_kv_cache* c, int64_t batch, int64_t tokens, int32_t q_heads, int64_t max_q, int64_t max_len,
+                       int64_t window) {
+  if (!c) return SPH_ERR_NULL;
+  if (const int st = sph_cache_check(c)) return (sph_status)st;
+  if (batch < 0 || batch > 65536 || tokens < 0 || tokens > (1 << 26) || q_heads < 1 || q_heads > 65535 || q_heads % c->kv_heads ||
+      max_q < 1 || max_q > (1 << 24) || max_len < 0 || max_len > (1 << 30) || window < 0)
+    return SPH_ERR_SHAPE;
+  return SPH_OK;
+}
+
+template <int BITS>
+const void* kernel_for(int dim) {
+  return dim == 64    ? (const void*)k_attn<64, BITS>
+         : dim == 96  ? (const void*)k_attn<96, BITS>
+         : dim == 128 ? (const void*)k_attn<128, BITS>
+         : dim == 192 ? (const void*)k_attn<192, BITS>
+                      : (const void*)k_attn<256, BITS>;
+}
+
+bool launch_ok(const void* fn, unsigned grid, unsigned block, hipStream_t s, AttnArgs& a) {
+  void* kargs[] = {(void*)&a};
+  return hipLaunchKernel(fn, dim3(grid), dim3(block), kargs, 0, s) == hipSuccess && hipGetLastError() == hipSuccess;
+}
+
+}  // namespace
+
+extern "C" {
+
+sph_status sph_attention_workspace_bytes(const sph_kv_cache* cache, int64_t batch, int64_t tokens, int32_t q_heads,
+                                         int64_t max_q, int64_t max_len, int64_t window, size_t* bytes) {
+  if (!bytes) return SPH_ERR_NULL;
+  if (const sph_status st = check_sizes(cache, batch, tokens, q_heads, max_q, max_len, window)) return st;
+  *bytes = batch && tokens ? plan_of(cache, batch, tokens, q_heads, max_q, max_len, window).bytes : 0;
+  return SPH_OK;
+}
+
+sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t tokens, int32_t q_heads, const void* d_q,
+                         int64_t q_token_stride, int64_t q_head_stride, const int32_t* d_q_start, int64_t max_q,
+                         const int32_t* d_pages, int64_t pages_stride, const int32_t* d_seq_lens, int64_t max_len,
+                         int64_t window, float scale, void* d_o, int64_t o_token_stride, int64_t o_head_stride,
+                         float* d_lse, void* d_ws, size_t ws_bytes, void* stream) {
+  if (const sph_status st = check_sizes(cache, batch, tokens, q_heads, max_q, max_len, window)) return st;
+  if (!std::isfinite(scale)) return SPH_ERR_BAD_VALUE;
+  if (!d_q_start && (max_q != 1 || tokens != batch)) return SPH_ERR_SHAPE;
+  const int64_t pages_needed = (max_len + cache->page_size - 1) / cache->page_size;
+  if (pages_stride < pages_needed || pages_stride > INT32_MAX) return SPH_ERR_SHAPE;
+  if (!batch || !tokens) return SPH_OK;
+  if (!d_q || !d_o || !d_seq_lens || (!d_pages && max_len > 0)) return SPH_ERR_NULL;
+  const int64_t lim = int64_t(1) << 40;
+  for (int64_t s : {q_token_stride, q_head_stride, o_token_stride, o_head_stride})
+    if (s < 0 || s >= lim || s % 8) return SPH_ERR_SHAPE;
+  if ((uintptr_t)d_q % 16 || (uintptr_t)d_o % 16 || (uintptr_t)d_q_start % 4 || (uintptr_t)d_pages % 4 || (uintptr_t)d_seq_lens % 4 ||
+      (uintptr_t)d_lse % 4 || (uintptr_t)d_ws % 256)
+    return SPH_ERR_SHAPE;
+  if ((tokens > 1 && o_token_stride == 0) || (q_heads > 1 && o_head_stride == 0)) return SPH_ERR_SHAPE;  // rows written twice
+  const Plan p = plan_of(cache, batch, tokens, q_heads, max_q, max_len, window);
+  if (p.bytes && !d_ws) return SPH_ERR_NULL;
+  if (ws_bytes < p.bytes) return SPH_ERR_BUFFER_TOO_SMALL;
+  AttnArgs a{};
+  a.c = sph_cache_view(cache);
+  a.q = (const char*)d_q, a.o = (char*)d_o;
+  a.qt = 2 * q_token_stride, a.qh = 2 * q_head_stride, a.ot = 2 * o_token_stride, a.oh = 2 * o_head_stride;
+  a.q_start = d_q_start, a.pages = d_pages, a.pages_stride = pages_stride, a.lens = d_seq_lens, a.lse = d_lse;
+  a.tokens = tokens, a.batch = (int)batch, a.q_heads = q_heads, a.group = q_heads / cache->kv_heads;
+  a.max_q = (int)max_q, a.max_len = (int)max_len, a.window = (int)std::min<int64_t>(window, INT32_MAX);
+  a.tiles = p.tiles, a.splits = p.splits, a.chunk = p.chunk;
+  a.scale = scale * kLog2e;
+  a.part = (float*)d_ws;
+  if (p.bytes) a.ml = (float2*)((float*)d_ws + (size_t)p.splits * tokens * q_heads * cache->head_dim);
+  const int64_t grid = (int64_t)cache->kv_heads * p.splits * p.tiles * batch, rows = tokens * q_heads;
+  if (grid >= (1 << 24) || (p.splits > 1 && rows >= (1 << 26))) return SPH_ERR_SHAPE;
+  const void* fn = cache->bits == 16 ? kernel_for<16>(cache->head_dim) : cache->bits == 8 ? kernel_for<8>(cache->head_dim) : kernel_for<4>(cache->head_dim);
+  if (!launch_ok(fn, (unsigned)grid, kThreads, (hipStream_t)stream, a)) return SPH_ERR_HIP;
+  if (p.splits > 1 && !launch_ok((const void*)k_attn_join, (unsigned)rows, 64, (hipStream_t)stream, a)) return SPH_ERR_HIP;
+  return SPH_OK;
+}
+
+}  // extern "C"

@@ -30,7 +30,8 @@ EXPORTS = ("sph_packed_bytes", "sph_pack_weights", "sph_gemv", "sph_gemm_small",
            "sph_kmeans_codebook", "sph_angular_codebook", "sph_angular_codebook_backward",
            "sph_angular_logits", "sph_direction_groups", "sph_fake_quant_init_rho",
            "sph_fake_quant_forward", "sph_fake_quant_backward_workspace_bytes",
-           "sph_fake_quant_backward", "sph_format_supported", "sph_status_str")
+           "sph_fake_quant_backward", "sph_rope_table", "sph_rope", "sph_kv_append", "sph_kv_read", "sph_attention",
+           "sph_attention_workspace_bytes", "sph_format_supported", "sph_status_str")
 
 FORMATS = {
     "W2": (6, 4), "W3": (13, 3), "W2_cfg": (4, 4), "W3_cfg": (8, 8), "W2_16": (6, 2),

@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import numpy as np
 
+from . import attn as A
 from . import sph as B
 
 
@@ -71,13 +72,40 @@ class _FakeQuant:
         return Fn
 
 
+class _Rope:
+    """autograd Function: rows -> rows at their rotary positions; the gradient turns back."""
+
+    @staticmethod
+    def build():
+        torch = _torch()
+
+        class Fn(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, x, positions, table, interleaved):
+                ctx.save_for_backward(positions, table)
+                ctx.interleaved = interleaved
+                return A.rope(x.detach(), positions, table, interleaved=interleaved)
+
+            @staticmethod
+            def backward(ctx, grad_y):
+                positions, table = ctx.saved_tensors
+                return A.rope(A.aligned_rows(grad_y), positions, table, interleaved=ctx.interleaved, inverse=True), None, None, None
+
+        return Fn
+
+
 _FNS = {}
 
 
 def _fn(name):
     if name not in _FNS:
-        _FNS[name] = {"angular": _AngularCodebook, "fq": _FakeQuant}[name].build()
+        _FNS[name] = {"angular": _AngularCodebook, "fq": _FakeQuant, "rope": _Rope}[name].build()
     return _FNS[name]
+
+
+def rope(x, positions, table, interleaved: bool = False):
+    """``attn.rope`` with its gradient with respect to x (positions and table are constants)."""
+    return _fn("rope").apply(x, positions, table, interleaved)
 
 
 def make_module(w, dir_bits: int, radius_bits: int, init_codebook=None, kmeans_uniforms=None,
