@@ -1,7 +1,7 @@
 // Attention of new tokens over the paged key-value cache (sph_attention).
 //
 // For one kv head, row r = t * group + h is new token t under query head h of the head's group. A workgroup
-// takes 16 rows and a stretch of keys; its waves take tiles of 32 keys in turn, each with a running
+// takes 16 or 32 rows and a stretch of keys; its waves take tiles of 32 keys in turn, each with a running
 // maximum m and sum l per row (o and l scale by exp(m_old - m_new) when m grows), and meet in LDS at the
 // end. A long sequence is cut into stretches for several workgroups, whose partial (o, m, l) a second kernel joins in order.
 //
@@ -24,7 +24,6 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kTile = 32;                 // keys of a wave's step
-constexpr int kRows = 16;                 // rows of a workgroup
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
@@ -93,11 +92,20 @@ struct Lay {
   static constexpr int kPieceCh = kPiece * 8 / BITS;
   static constexpr int kSteps = DIM / 32;
   static constexpr int kBlocks = kPieceCh / 8;              // products of a piece
-  // a value row's pieces: 16 bytes, and with codes 16 channels
+  // a value row's pieces: eight fp16 channels or 16 codes
   static constexpr int kVCh = BITS == 16 ? 8 : 16;
+  static constexpr int kVPiece = kVCh * BITS / 8;
   static constexpr int kVPer = DIM / kVCh;
   static constexpr int kVLoads = kTile * kVPer / 64;
   static constexpr int kVStride = DIM * 2 + 32;             // bytes between rows in LDS: four rows' transposed read hits all banks
+};
+
+// A wave's loads of one tile of keys, as they come from memory.
+template <int DIM, int BITS>
+struct Tile {
+  typedef Lay<DIM, BITS> L;
+  uint32_t k[2][L::kLoads][L::kPiece / 4], v[L::kVLoads][L::kVPiece / 4];
+  uint32_t k_par[2][L::kLoads], v_par[L::kVLoads];
 };
 
 template <int BYTES>
@@ -113,9 +121,87 @@ __device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
   }
 }
 
+// One kv head's pages. Lane l holds the page of key l % 32 of a tile (0 where the pool has no such page).
+struct Pages {
+  const char *k, *v, *k_par, *v_par;
+  int64_t stride, par_stride;
+  int token, par_token;      // bytes between tokens of a page
+  int mask;
+  __device__ __forceinline__ const char* row(const char* base, int64_t page_stride, int token_stride, int page, int key) const {
+    return base + page * page_stride + (uint32_t)((key & mask) * token_stride);
+  }
+};
+
 template <int DIM, int BITS>
-__global__ __launch_bounds__(kThreads) void k_attn(AttnArgs a) {
+__device__ __forceinline__ void load_keys(Tile<DIM, BITS>& t, const Pages& pg, int page, int kt, int lane) {
   typedef Lay<DIM, BITS> L;
+  const int col = lane & 15, g4 = lane >> 4;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int kk = 8 * (col >> 2) + 4 * u + (col & 3), mine = __shfl(page, kk);
+    const char* kr = pg.row(pg.k, pg.stride, pg.token, mine, kt + kk) + g4 * L::kPiece;
+#pragma unroll
+    for (int i = 0; i < L::kLoads; ++i) load_words<L::kPiece>(kr + 4 * i * L::kPiece, t.k[u][i]);
+    if constexpr (BITS < 16) {
+      const char* pr = pg.row(pg.k_par, pg.par_stride, pg.par_token, mine, kt + kk);
+#pragma unroll
+      for (int i = 0; i < L::kLoads; ++i) t.k_par[u][i] = *(const uint32_t*)(pr + (4 * i + g4) * L::kPieceCh / 32 * 4);
+    }
+  }
+}
+
+template <int DIM, int BITS>
+__device__ __forceinline__ void load_values(Tile<DIM, BITS>& t, const Pages& pg, int page, int kt, int lane) {
+  typedef Lay<DIM, BITS> L;
+#pragma unroll
+  for (int i = 0; i < L::kVLoads; ++i) {
+    const int p = lane + 64 * i, kk = p / L::kVPer, piece = p % L::kVPer, mine = __shfl(page, kk);
+    load_words<L::kVPiece>(pg.row(pg.v, pg.stride, pg.token, mine, kt + kk) + piece * L::kVPiece, t.v[i]);
+    if constexpr (BITS < 16)
+      t.v_par[i] = *(const uint32_t*)(pg.row(pg.v_par, pg.par_stride, pg.par_token, mine, kt + kk) + piece / 2 * 4);
+  }
+}
+// Keys that a workgroup's rows see: [k_lo, k_hi) at most, of them each row those in (pos - window, pos].
+struct Span {
+  int k_lo, k_hi, p_lo, p_hi, window;
+  // every row sees the whole tile at kt
+  __device__ __forceinline__ bool whole(int kt) const {
+    return kt >= k_lo && kt + kTile <= k_hi && kt + kTile - 1 <= p_lo && (!window || kt > p_hi - window);
+  }
+  __device__ __forceinline__ bool seen(int key, int pos) const { return key >= k_lo && key < k_hi && key <= pos && (!window || key > pos - window); }
+};
+
+// The sum of the infinities and NaN among channels ch .. ch + 3 of the values that a row at position pos sees in tiles that not
+// every row sees: a weight is positive, so it leaves them what they are. Only called where there are some.
+template <int DIM, int BITS>
+__device__ __forceinline__ f32x4 odd_values(Span s, Pages pg, const int32_t* pages, int shift, int n_pages, int pos, int ch) {
+  f32x4 sum = {};
+#pragma unroll 1
+  for (int key = s.k_lo; key < s.k_hi; ++key) {
+    const int page = pages[key >> shift];
+    if (s.whole(key & ~(kTile - 1)) || !s.seen(key, pos) || (unsigned)page >= (unsigned)n_pages) continue;
+    const char* row = pg.row(pg.v, pg.stride, pg.token, page, key);
+    f16x8 v;
+    if constexpr (BITS == 16)
+      v = *(const f16x8*)(row + 2 * (ch & ~7));
+    else
+      v = decode8<BITS>(row + (ch & ~7) * BITS / 8, *(const uint32_t*)(pg.row(pg.v_par, pg.par_stride, pg.par_token, page, key) + ch / 32 * 4));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float f = (float)(ch & 4 ? v[4 + e] : v[e]);
+      if (!__builtin_isfinite(f)) sum[e] += f;
+    }
+  }
+  return sum;
+}
+
+// What bounds it: HBM reads of the pages. Each wave keeps one tile of keys and values in flight in registers while
+// it works on the one before, and a SIMD holds two to four such waves; the 16 rows that a product has cost the same
+// whether one query head or 16 share the kv head. The page numbers of a tile are loaded two tiles ahead.
+template <int DIM, int BITS, int NB>
+__global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 4 : DIM * NB <= 128 ? 2 : 1)) void k_attn(AttnArgs a) {
+  typedef Lay<DIM, BITS> L;
+  constexpr int kRows = 16 * NB;
   constexpr int kVBytes = kTile * L::kVStride, kOStride = DIM + 4;
   constexpr int kLds = kWaves * (kVBytes > kRows * kOStride * 4 ? kVBytes : kRows * kOStride * 4);
   __shared__ __attribute__((aligned(16))) char lds[kLds];
@@ -138,110 +224,163 @@ __global__ __launch_bounds__(kThreads) void k_attn(AttnArgs a) {
   if (r0 >= rows) return;
   const int nrow = min(kRows, rows - r0);
   const int first = s.len - s.n;                            // position of the first new token
-  const int t_lo = r0 / a.group, t_hi = (r0 + nrow - 1) / a.group;
-  const int lo = a.window ? max(0, first + t_lo - a.window + 1) : 0, hi = first + t_hi + 1;
+  const int p_lo = first + r0 / a.group, p_hi = first + (r0 + nrow - 1) / a.group;  // positions of the rows
+  const int lo = a.window ? max(0, p_lo - a.window + 1) : 0, hi = p_hi + 1;
   const int k_lo = max(lo, (lo & ~(kTile - 1)) + split * a.chunk), k_hi = min(hi, (lo & ~(kTile - 1)) + (split + 1) * a.chunk);
+  const Span span = {k_lo, k_hi, p_lo, p_hi, a.window};
+  const int32_t* pages = a.pages + b * a.pages_stride;
+  Pages pg;
+  pg.k = a.c.k + kvh * a.c.head_stride, pg.v = a.c.v + kvh * a.c.head_stride;
+  pg.k_par = a.c.k_par + kvh * a.c.par_head_stride, pg.v_par = a.c.v_par + kvh * a.c.par_head_stride;
+  pg.stride = a.c.page_stride, pg.par_stride = a.c.par_page_stride;
+  pg.token = (int)a.c.token_stride, pg.par_token = (int)a.c.par_token_stride;
+  const int shift = a.c.page_shift, n_pages = (int)a.c.n_pages;
+  pg.mask = (1 << shift) - 1;
 
-  const int r = r0 + min(col, nrow - 1);
-  const int t = r / a.group, h = kvh * a.group + r % a.group;
-  const int pos = first + t, see = a.window ? pos - a.window : -1;  // keys see + 1 .. pos
-
-  f32x4 o[DIM / 16] = {};
-  float m = -INFINITY, l = 0.0f;
-  if (k_lo < k_hi) {
-    f16x8 q[L::kSteps];
-    const char* qr = a.q + (s.start + t) * a.qt + h * a.qh;
+  int pos[NB];
+  bool odd = false;
+  f32x4 o[NB][DIM / 16] = {};
+  float m[NB], base[NB], l[NB];
 #pragma unroll
-    for (int i = 0; i < L::kLoads; ++i)
+  for (int n = 0; n < NB; ++n) m[n] = -INFINITY, base[n] = 0.0f, l[n] = 0.0f;
+  const int t0 = (k_lo & ~(kTile - 1)) + kTile * wave;
+  if (t0 < k_hi) {
+    f16x8 q[NB][L::kSteps];
 #pragma unroll
-      for (int j = 0; j < L::kBlocks; ++j)
-        q[i * L::kBlocks + j] = *(const f16x8*)(qr + 2 * ((4 * i + g4) * L::kPieceCh + 8 * j));
-    const int32_t* pages = a.pages + b * a.pages_stride;
-    const int pmask = (1 << a.c.page_shift) - 1;
-    const char* kb = a.c.k + kvh * a.c.head_stride;
-    const char* vb = a.c.v + kvh * a.c.head_stride;
-    const char* kpb = a.c.k_par + kvh * a.c.par_head_stride;
-    const char* vpb = a.c.v_par + kvh * a.c.par_head_stride;
+    for (int n = 0; n < NB; ++n) {
+      const int r = r0 + min(16 * n + col, nrow - 1), t = r / a.group, h = kvh * a.group + r % a.group;
+      pos[n] = first + t;
+      const char* qr = a.q + (s.start + t) * a.qt + h * a.qh;
+#pragma unroll
+      for (int i = 0; i < L::kLoads; ++i)
+#pragma unroll
+        for (int j = 0; j < L::kBlocks; ++j)
+          q[n][i * L::kBlocks + j] = *(const f16x8*)(qr + 2 * ((4 * i + g4) * L::kPieceCh + 8 * j));
+    }
+    const int e_lo = k_lo >> shift, e_hi = (k_hi - 1) >> shift;
+    // keys outside the stretch take a page inside it: their rows are read and not used
+    auto page_of = [&](int kt) { return pages[min(max((kt + (lane & 31)) >> shift, e_lo), e_hi)]; };
     char* vs = lds + wave * kVBytes;
 
-    for (int kt = (k_lo & ~(kTile - 1)) + kTile * wave; kt < k_hi; kt += kTile * kWaves) {
+    Tile<DIM, BITS> T;
+    int kt = t0, nt = t0 + kTile * kWaves < k_hi ? t0 + kTile * kWaves : t0;
+    int page = page_of(kt), next = page_of(nt);
+    uint64_t gone = __ballot((unsigned)page >= (unsigned)n_pages);
+    page = (unsigned)page < (unsigned)n_pages ? page : 0;
+    load_keys(T, pg, page, kt, lane);
+    load_values(T, pg, page, kt, lane);
+    while (true) {
+      const bool last = kt + kTile * kWaves >= k_hi;
+      // every row sees the whole tile
+      const bool whole = span.whole(kt) && !gone;
+      const uint64_t next_gone = __ballot((unsigned)next >= (unsigned)n_pages);
+      page = (unsigned)next < (unsigned)n_pages ? next : 0;
       // scores
-      f32x4 st[2] = {};
+      f32x4 st[NB][2] = {};
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int key = min(max(kt + 8 * (col >> 2) + 4 * u + (col & 3), k_lo), k_hi - 1);
-        const int page = pages[key >> a.c.page_shift];
-        const bool there = (unsigned)page < (uint64_t)a.c.n_pages;
-        const int64_t pg = there ? page : 0;
-        const char* kr = kb + pg * a.c.page_stride + (key & pmask) * a.c.token_stride;
-        const char* pr = kpb + pg * a.c.par_page_stride + (key & pmask) * a.c.par_token_stride;
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int i = 0; i < L::kLoads; ++i) {
-          uint32_t w[4];
-          load_words<L::kPiece>(kr + (4 * i + g4) * L::kPiece, w);
+        for (int i = 0; i < L::kLoads; ++i)
 #pragma unroll
           for (int j = 0; j < L::kBlocks; ++j) {
             f16x8 kv;
-            if constexpr (BITS == 16) {
-              kv = __builtin_bit_cast(f16x8, make_uint4(w[0], w[1], w[2], w[3]));
-            } else {
-              const uint32_t par = *(const uint32_t*)(pr + ((4 * i + g4) * L::kPieceCh + 8 * j) / 32 * 4);
-              kv = BITS == 8 ? decode8w<8>(w[2 * j], w[2 * j + 1], par) : decode8w<4>(w[j], 0, par);
-            }
-            const _Float16 nan = __builtin_bit_cast(_Float16, (uint16_t)0x7E00);
-            if (!there) kv = f16x8{nan, nan, nan, nan, nan, nan, nan, nan};
-            st[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv, q[i * L::kBlocks + j], st[u], 0, 0, 0);
+            if constexpr (BITS == 16)
+              kv = __builtin_bit_cast(f16x8, make_uint4(T.k[u][i][0], T.k[u][i][1], T.k[u][i][2], T.k[u][i][3]));
+            else if constexpr (BITS == 8)
+              kv = decode8w<8>(T.k[u][i][2 * j], T.k[u][i][2 * j + 1], T.k_par[u][i]);
+            else
+              kv = decode8w<4>(T.k[u][i][j], 0, T.k_par[u][i]);
+#pragma unroll
+            for (int n = 0; n < NB; ++n) st[n][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv, q[n][i * L::kBlocks + j], st[n][u], 0, 0, 0);
           }
-        }
-      }
+      // not above the products: the loads would take registers of their own beside those that they refill
+      __builtin_amdgcn_sched_barrier(0);
+      load_keys(T, pg, page, nt, lane);
+      __builtin_amdgcn_sched_barrier(0);
       // values into LDS
 #pragma unroll
       for (int i = 0; i < L::kVLoads; ++i) {
         const int p = lane + 64 * i, kk = p / L::kVPer, piece = p % L::kVPer;
-        const int key = min(max(kt + kk, k_lo), k_hi - 1);
-        const int page = pages[key >> a.c.page_shift];
-        const bool there = (unsigned)page < (uint64_t)a.c.n_pages && key == kt + kk;
-        const int64_t pg = there ? page : 0;
-        const char* vr = vb + pg * a.c.page_stride + (key & pmask) * a.c.token_stride;
-        f16x8 v[2];
+        f16x8 v[L::kVCh / 8];
         if constexpr (BITS == 16) {
-          v[0] = *(const f16x8*)(vr + 16 * piece);
+          v[0] = __builtin_bit_cast(f16x8, make_uint4(T.v[i][0], T.v[i][1], T.v[i][2], T.v[i][3]));
+        } else if constexpr (BITS == 8) {
+          v[0] = decode8w<8>(T.v[i][0], T.v[i][1], T.v_par[i]);
+          v[1] = decode8w<8>(T.v[i][2], T.v[i][3], T.v_par[i]);
         } else {
-          const uint32_t par = *(const uint32_t*)(vpb + pg * a.c.par_page_stride + (key & pmask) * a.c.par_token_stride + piece / 2 * 4);
-          v[0] = decode8<BITS>(vr + piece * 2 * BITS, par);
-          v[1] = decode8<BITS>(vr + piece * 2 * BITS + BITS, par);
+          v[0] = decode8w<4>(T.v[i][0], 0, T.v_par[i]);
+          v[1] = decode8w<4>(T.v[i][1], 0, T.v_par[i]);
         }
 #pragma unroll
-        for (int j = 0; j < L::kVCh / 8; ++j) {
-          if (!there) v[j] = f16x8{};
-          *(f16x8*)(vs + kk * L::kVStride + (piece * L::kVCh + 8 * j) * 2) = v[j];
+        for (int j = 0; j < L::kVCh / 8; ++j) *(f16x8*)(vs + kk * L::kVStride + (piece * L::kVCh + 8 * j) * 2) = v[j];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      load_values(T, pg, page, nt, lane);
+      __builtin_amdgcn_sched_barrier(0);
+      const int nnt = nt + kTile * kWaves < k_hi ? nt + kTile * kWaves : nt;
+      next = page_of(nnt);
+      // weights; the reference m is raised, and o and l scaled down, only when a score passes it by 2^8: weights up to
+      // 256 lose nothing in fp16 or fp32
+      f16x8 p[NB];
+      bool rise = false;
+      float x[NB][8], top[NB];
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        top[n] = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[n][i] = st[n][i >> 2][i & 3] * a.scale;
+        if (!whole) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int key = kt + 8 * g4 + i;
+            x[n][i] = !span.seen(key, pos[n]) ? -INFINITY : (gone >> (8 * g4 + i) & 1) ? __builtin_nanf("") : x[n][i];
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top[n] = fmaxf(top[n], x[n][i]);
+        rise |= top[n] > m[n] + 8.0f;
+      }
+      if (__any(rise)) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          float mn = fmaxf(m[n], top[n]);
+          mn = fmaxf(mn, __shfl_xor(mn, 16));
+          mn = fmaxf(mn, __shfl_xor(mn, 32));
+          base[n] = mn == -INFINITY ? 0.0f : mn;
+          const float keep = __builtin_amdgcn_exp2f(m[n] - base[n]);
+          m[n] = mn;
+          l[n] *= keep;
+#pragma unroll
+          for (int i = 0; i < DIM / 16; ++i) o[n][i] *= keep;
         }
       }
-      // weights
-      float x[8], top = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int key = kt + 8 * g4 + i;
-        x[i] = key <= pos && key > see && key >= k_lo && key < k_hi ? st[i >> 2][i & 3] * a.scale : -INFINITY;
-        top = fmaxf(top, x[i]);
-      }
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float mn = fmaxf(m, top), base = mn == -INFINITY ? 0.0f : mn;
-      const float keep = __builtin_amdgcn_exp2f(m - base);
-      m = mn;
-      l *= keep;
+      for (int n = 0; n < NB; ++n)
 #pragma unroll
-      for (int i = 0; i < DIM / 16; ++i) o[i] *= keep;
-      f16x8 p;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float e = __builtin_amdgcn_exp2f(x[i] - base);
-        l += e;
-        p[i] = (_Float16)e;
-      }
+        for (int i = 0; i < 8; ++i) {
+          x[n][i] = __builtin_amdgcn_exp2f(x[n][i] - base[n]);
+          l[n] += x[n][i];
+          p[n][i] = (_Float16)x[n][i];
+        }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
+      if (!whole) {
+        // A weight of 0 does not hide an infinity or a NaN in a value that its row does not see: values that no row sees
+        // become zeros here, and so do infinities and NaN, which the rows that see them get at the end.
+#pragma unroll 1
+        for (int i = lane; i < kTile * (DIM / 2); i += 64) {
+          const int kk = i / (DIM / 2);
+          uint32_t* w = (uint32_t*)(vs + kk * L::kVStride + i % (DIM / 2) * 4);
+          uint32_t v = *w;
+          if (kt + kk < k_lo || kt + kk >= k_hi || (gone >> kk & 1)) v = 0;
+          if ((v & 0x7C00u) == 0x7C00u || (v & 0x7C000000u) == 0x7C000000u) odd = true;
+          if ((v & 0x7C00u) == 0x7C00u) v &= 0xFFFF0000u;
+          if ((v & 0x7C000000u) == 0x7C000000u) v &= 0xFFFFu;
+          *w = v;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+      }
 #pragma unroll
       for (int i = 0; i < DIM / 16; ++i) {
         f16x8 vt;
@@ -253,37 +392,49 @@ __global__ __launch_bounds__(kThreads) void k_attn(AttnArgs a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) vt[4 * j + e] = f[e];
         }
-        o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, p, o[i], 0, 0, 0);
+#pragma unroll
+        for (int n = 0; n < NB; ++n) o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, p[n], o[n][i], 0, 0, 0);
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
+      if (last) break;
+      kt = nt;
+      nt = nnt;
+      gone = next_gone;
     }
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      l[n] += __shfl_xor(l[n], 16);
+      l[n] += __shfl_xor(l[n], 32);
+    }
   }
 
   // the waves' parts meet
-  __syncthreads();
+  const bool any_odd = __syncthreads_or(odd);
   float* os = (float*)lds + wave * kRows * kOStride;
-  if (g4 == 0) ml_s[wave][col] = make_float2(m, l);
 #pragma unroll
-  for (int i = 0; i < DIM / 16; ++i) *(f32x4*)(os + col * kOStride + 16 * i + 4 * g4) = o[i];
+  for (int n = 0; n < NB; ++n) {
+    if (g4 == 0) ml_s[wave][16 * n + col] = make_float2(m[n], l[n]);
+#pragma unroll
+    for (int i = 0; i < DIM / 16; ++i) *(f32x4*)(os + (16 * n + col) * kOStride + 16 * i + 4 * g4) = o[n][i];
+  }
   __syncthreads();
   for (int i = threadIdx.x; i < nrow * (DIM / 4); i += kThreads) {
     const int row = i / (DIM / 4), ch = i % (DIM / 4) * 4;
     float mm = ml_s[0][row].x;
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) mm = fmaxf(mm, ml_s[w][row].x);
-    const float base = mm == -INFINITY ? 0.0f : mm;
+    const float ref = mm == -INFINITY ? 0.0f : mm;
     f32x4 acc = {};
     float ll = 0.0f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float f = __builtin_amdgcn_exp2f(ml_s[w][row].x - base);
+      const float f = __builtin_amdgcn_exp2f(ml_s[w][row].x - ref);
       ll += f * ml_s[w][row].y;
       acc += f * *(const f32x4*)((float*)lds + (w * kRows + row) * kOStride + ch);
     }
     const int rr = r0 + row;
+    if (any_odd) acc += odd_values<DIM, BITS>(span, pg, pages, shift, n_pages, first + rr / a.group, ch);
     write_out(a, split, s.start + rr / a.group, kvh * a.group + rr % a.group, ch, acc, mm, ll);
   }
 }
@@ -311,7 +462,7 @@ __global__ __launch_bounds__(64) void k_attn_join(AttnArgs a) {
 // ------------------------------------------------------------------ host side
 
 struct Plan {
-  int tiles, splits, chunk;
+  int nb, tiles, splits, chunk;
   size_t bytes;
 };
 
@@ -319,8 +470,10 @@ struct Plan {
 Plan plan_of(const sph_kv_cache* c, int64_t batch, int64_t tokens, int q_heads, int64_t max_q, int64_t max_len, int64_t window) {
   Plan p{};
   const int group = q_heads / c->kv_heads;
-  p.tiles = (int)((max_q * group + kRows - 1) / kRows);
-  const int64_t span = window > 0 ? std::min<int64_t>(max_len, window + kRows / group + 1 + kTile) : max_len;
+  p.nb = max_q * group <= 16 || c->head_dim > 128 ? 1 : 2;  // two blocks of rows of wider heads do not fit the registers
+  const int rows = 16 * p.nb;
+  p.tiles = (int)((max_q * group + rows - 1) / rows);
+  const int64_t span = window > 0 ? std::min<int64_t>(max_len, window + rows / group + 1 + kTile) : max_len;
   const int64_t units = (int64_t)c->kv_heads * batch * p.tiles, step = kTile * kWaves;
   const int64_t want = std::max<int64_t>(1, 2048 / units);
   int64_t chunk = (span + want - 1) / want;
@@ -341,13 +494,18 @@ sph_status check_sizes(const sph_kv_cache* c, int64_t batch, int64_t tokens, int
   return SPH_OK;
 }
 
-template <int BITS>
+template <int BITS, int NB>
 const void* kernel_for(int dim) {
-  return dim == 64    ? (const void*)k_attn<64, BITS>
-         : dim == 96  ? (const void*)k_attn<96, BITS>
-         : dim == 128 ? (const void*)k_attn<128, BITS>
-         : dim == 192 ? (const void*)k_attn<192, BITS>
-                      : (const void*)k_attn<256, BITS>;
+  if (dim == 64) return (const void*)k_attn<64, BITS, NB>;
+  if (dim == 96) return (const void*)k_attn<96, BITS, NB>;
+  if (dim == 128) return (const void*)k_attn<128, BITS, NB>;
+  if constexpr (NB == 1) return dim == 192 ? (const void*)k_attn<192, BITS, 1> : (const void*)k_attn<256, BITS, 1>;
+  return nullptr;
+}
+
+template <int NB>
+const void* kernel_for(int bits, int dim) {
+  return bits == 16 ? kernel_for<16, NB>(dim) : bits == 8 ? kernel_for<8, NB>(dim) : kernel_for<4, NB>(dim);
 }
 
 bool launch_ok(const void* fn, unsigned grid, unsigned block, hipStream_t s, AttnArgs& a) {
@@ -402,7 +560,7 @@ sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t token
   if (p.bytes) a.ml = (float2*)((float*)d_ws + (size_t)p.splits * tokens * q_heads * cache->head_dim);
   const int64_t grid = (int64_t)cache->kv_heads * p.splits * p.tiles * batch, rows = tokens * q_heads;
   if (grid >= (1 << 24) || (p.splits > 1 && rows >= (1 << 26))) return SPH_ERR_SHAPE;
-  const void* fn = cache->bits == 16 ? kernel_for<16>(cache->head_dim) : cache->bits == 8 ? kernel_for<8>(cache->head_dim) : kernel_for<4>(cache->head_dim);
+  const void* fn = p.nb == 1 ? kernel_for<1>(cache->bits, cache->head_dim) : kernel_for<2>(cache->bits, cache->head_dim);
   if (!launch_ok(fn, (unsigned)grid, kThreads, (hipStream_t)stream, a)) return SPH_ERR_HIP;
   if (p.splits > 1 && !launch_ok((const void*)k_attn_join, (unsigned)rows, 64, (hipStream_t)stream, a)) return SPH_ERR_HIP;
   return SPH_OK;
