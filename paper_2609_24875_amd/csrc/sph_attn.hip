@@ -211,9 +211,9 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 4 : DIM * NB <= 128 ? 2
   uint32_t id = blockIdx.x;
   const int kvh = id % a.c.kv_heads;
   id /= a.c.kv_heads;
-  const int split = id % a.splits;
-  id /= a.splits;
-  const int tile = id % a.tiles, b = id / a.tiles;
+  const int b = id % a.batch;
+  id /= a.batch;
+  const int tile = id % a.tiles, split = id / a.tiles;
   Seq s;
   s.load(a, b);
   if (s.bad) {
@@ -439,24 +439,61 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 4 : DIM * NB <= 128 ? 2
   }
 }
 
-// One workgroup a row: the stretches' parts in order. Stretches without a seen key have l = 0 and are not read.
-__global__ __launch_bounds__(64) void k_attn_join(AttnArgs a) {
+// Joins the stretches of a row, 32 channels a workgroup: the stretches' factors first, then each group of eight threads adds every
+// 32nd stretch in order, and the groups' sums are added in order. Stretches without a seen key have l = 0 and hold nothing.
+constexpr int kMaxSplits = 512, kJoinCh = 32;
+
+__global__ __launch_bounds__(kThreads) void k_attn_join(AttnArgs a) {
+  constexpr int kPer = kJoinCh / 4, kGroups = kThreads / kPer;
+  __shared__ float factor[kMaxSplits];
+  __shared__ float2 red[kWaves];
+  __shared__ __attribute__((aligned(16))) float sums[kThreads * 4];
   const int64_t row = blockIdx.x, rows = a.tokens * a.q_heads;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float mm = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) mm = fmaxf(mm, a.ml[s * rows + row].x);
-  const float base = mm == -INFINITY ? 0.0f : mm;
-  const int ch = threadIdx.x * 4;
-  f32x4 acc = {};
-  float l = 0.0f;
-  for (int s = 0; s < a.splits; ++s) {
-    const float2 p = a.ml[s * rows + row];
-    if (p.y == 0.0f) continue;
-    const float f = __builtin_amdgcn_exp2f(p.x - base);
-    l += f * p.y;
-    if (ch < a.c.dim) acc += f * *(const f32x4*)(a.part + (s * rows + row) * a.c.dim + ch);
+  float2 mine[kMaxSplits / kThreads];
+#pragma unroll
+  for (int i = 0; i < kMaxSplits / kThreads; ++i) {
+    const int s = threadIdx.x + i * kThreads;
+    mine[i] = s < a.splits ? a.ml[s * rows + row] : make_float2(-INFINITY, 0.0f);
+    mm = fmaxf(mm, mine[i].x);
   }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) mm = fmaxf(mm, __shfl_xor(mm, d));
+  if (lane == 0) red[wave].x = mm;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, red[w].x);
+  const float ref = mm == -INFINITY ? 0.0f : mm;
+  float l = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kMaxSplits / kThreads; ++i) {
+    const int s = threadIdx.x + i * kThreads;
+    const float f = mine[i].y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(mine[i].x - ref);
+    if (s < a.splits) factor[s] = f;
+    l += f * mine[i].y;
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
+  if (lane == 0) red[wave].y = l;
+  __syncthreads();
+  l = red[0].y;
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) l += red[w].y;
+  const int group = threadIdx.x / kPer, ch = blockIdx.y * kJoinCh + threadIdx.x % kPer * 4;
+  f32x4 acc = {};
+#pragma unroll 4
+  for (int s = group; s < a.splits; s += kGroups) {
+    const float f = factor[s];
+    // a part without a seen key is not read: what it holds is not defined
+    if (f != 0.0f) acc += f * *(const f32x4*)(a.part + (s * rows + row) * a.c.dim + ch);
+  }
+  *(f32x4*)(sums + threadIdx.x * 4) = acc;
+  __syncthreads();
+  if (group) return;
+  for (int g = 1; g < min(kGroups, a.splits); ++g) acc += *(const f32x4*)(sums + (g * kPer + threadIdx.x) * 4);
   a.splits = 1;
-  if (ch < a.c.dim) write_out(a, 0, row / a.q_heads, (int)(row % a.q_heads), ch, acc, mm, l);
+  write_out(a, 0, row / a.q_heads, (int)(row % a.q_heads), ch, acc, mm, l);
 }
 
 // ------------------------------------------------------------------ host side
@@ -465,6 +502,8 @@ struct Plan {
   int nb, tiles, splits, chunk;
   size_t bytes;
 };
+
+constexpr int kWant = 1024;
 
 // Stretches of at least 128 keys (one tile a wave), and few enough workgroups that each has work for a while.
 Plan plan_of(const sph_kv_cache* c, int64_t batch, int64_t tokens, int q_heads, int64_t max_q, int64_t max_len, int64_t window) {
@@ -475,7 +514,7 @@ Plan plan_of(const sph_kv_cache* c, int64_t batch, int64_t tokens, int q_heads, 
   p.tiles = (int)((max_q * group + rows - 1) / rows);
   const int64_t span = window > 0 ? std::min<int64_t>(max_len, window + rows / group + 1 + kTile) : max_len;
   const int64_t units = (int64_t)c->kv_heads * batch * p.tiles, step = kTile * kWaves;
-  const int64_t want = std::max<int64_t>(1, 2048 / units);
+  const int64_t want = std::min<int64_t>(kMaxSplits, std::max<int64_t>(1, kWant / units));
   int64_t chunk = (span + want - 1) / want;
   chunk = std::max<int64_t>(step, (chunk + step - 1) / step * step);
   p.chunk = (int)chunk;
@@ -508,9 +547,9 @@ const void* kernel_for(int bits, int dim) {
   return bits == 16 ? kernel_for<16, NB>(dim) : bits == 8 ? kernel_for<8, NB>(dim) : kernel_for<4, NB>(dim);
 }
 
-bool launch_ok(const void* fn, unsigned grid, unsigned block, hipStream_t s, AttnArgs& a) {
+bool launch_ok(const void* fn, dim3 grid, hipStream_t s, AttnArgs& a) {
   void* kargs[] = {(void*)&a};
-  return hipLaunchKernel(fn, dim3(grid), dim3(block), kargs, 0, s) == hipSuccess && hipGetLastError() == hipSuccess;
+  return hipLaunchKernel(fn, grid, dim3(kThreads), kargs, 0, s) == hipSuccess && hipGetLastError() == hipSuccess;
 }
 
 }  // namespace
@@ -561,8 +600,8 @@ sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t token
   const int64_t grid = (int64_t)cache->kv_heads * p.splits * p.tiles * batch, rows = tokens * q_heads;
   if (grid >= (1 << 24) || (p.splits > 1 && rows >= (1 << 26))) return SPH_ERR_SHAPE;
   const void* fn = p.nb == 1 ? kernel_for<1>(cache->bits, cache->head_dim) : kernel_for<2>(cache->bits, cache->head_dim);
-  if (!launch_ok(fn, (unsigned)grid, kThreads, (hipStream_t)stream, a)) return SPH_ERR_HIP;
-  if (p.splits > 1 && !launch_ok((const void*)k_attn_join, (unsigned)rows, 64, (hipStream_t)stream, a)) return SPH_ERR_HIP;
+  if (!launch_ok(fn, dim3((unsigned)grid), (hipStream_t)stream, a)) return SPH_ERR_HIP;
+  if (p.splits > 1 && !launch_ok((const void*)k_attn_join, dim3((unsigned)rows, cache->head_dim / kJoinCh), (hipStream_t)stream, a)) return SPH_ERR_HIP;
   return SPH_OK;
 }
 
