@@ -5,11 +5,10 @@
 // maximum m and sum l per row (o and l scale by exp(m_old - m_new) when m grows), and meet in LDS at the
 // end. A long sequence is cut into stretches for several workgroups, whose partial (o, m, l) a second kernel joins in order.
 //
-// Products are v_mfma_f32_16x16x32_f16. S^T = K Q^T has a row per key and a column per query row, so a
-// lane keeps eight keys of one row: with the key in matrix row m of tile t chosen as 8 (m / 4) + 4 t + m % 4,
-// they are the eight consecutive keys 8 (lane / 16) .. + 7 that the B operand of O^T = V^T P^T wants from the
-// same lane, and the weights go from one product to the next without leaving their lane. V^T's operand comes
-// from rows staged in LDS by transposing reads.
+// Products are v_mfma_f32_16x16x32_f16. S^T = K Q^T has a row per key and a column per query row: of the tile's two
+// products of 16 keys, a lane keeps keys 4 (lane / 16) .. + 3 of each for one row. In O^T = V^T P^T the order of the 32 keys
+// is free as long as both operands share it, so the lane's eight weights go into that product where they are, and
+// V^T's operand takes the same keys from rows staged in LDS by two transposing reads of four keys each.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -26,6 +25,8 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kTile = 32;                 // keys of a wave's step
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 struct AttnArgs {
   CacheView c;
@@ -92,11 +93,17 @@ struct Lay {
   static constexpr int kPieceCh = kPiece * 8 / BITS;
   static constexpr int kSteps = DIM / 32;
   static constexpr int kBlocks = kPieceCh / 8;              // products of a piece
-  // a value row's pieces: eight fp16 channels or 16 codes
-  static constexpr int kVCh = BITS == 16 ? 8 : 16;
+  // a value row's pieces: eight fp16 channels or 16 codes (eight where 16 rows of pieces would not be whole loads), loaded
+  // by half tiles of 16 rows
+  static constexpr int kVCh = BITS == 16 || DIM % 64 == 32 ? 8 : 16;
   static constexpr int kVPiece = kVCh * BITS / 8;
   static constexpr int kVPer = DIM / kVCh;
-  static constexpr int kVLoads = kTile * kVPer / 64;
+  static constexpr int kVLoads = 16 * kVPer / 64;
+  static_assert(16 * kVPer % 64 == 0, "whole loads");
+  __device__ static __forceinline__ int v_row(int lane, int i) {
+    return 64 % kVPer ? (lane + 64 * i) / kVPer : lane / kVPer + i * (64 / kVPer);
+  }
+  __device__ static __forceinline__ int v_piece(int lane, int i) { return 64 % kVPer ? (lane + 64 * i) % kVPer : lane % kVPer; }
   static constexpr int kVStride = DIM * 2 + 32;             // bytes between rows in LDS: four rows' transposed read hits all banks
 };
 
@@ -104,8 +111,8 @@ struct Lay {
 template <int DIM, int BITS>
 struct Tile {
   typedef Lay<DIM, BITS> L;
-  uint32_t k[2][L::kLoads][L::kPiece / 4], v[L::kVLoads][L::kVPiece / 4];
-  uint32_t k_par[2][L::kLoads], v_par[L::kVLoads];
+  uint32_t k[2][L::kLoads][L::kPiece / 4], v[2 * L::kVLoads][L::kVPiece / 4];
+  uint32_t k_par[2][L::kLoads], v_par[2 * L::kVLoads];
 };
 
 template <int BYTES>
@@ -121,7 +128,7 @@ __device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
   }
 }
 
-// One kv head's pages. Lane l holds the page of key l % 32 of a tile (0 where the pool has no such page).
+// One kv head's pages.
 struct Pages {
   const char *k, *v, *k_par, *v_par;
   int64_t stride, par_stride;
@@ -132,35 +139,79 @@ struct Pages {
   }
 };
 
-template <int DIM, int BITS>
-__device__ __forceinline__ void load_keys(Tile<DIM, BITS>& t, const Pages& pg, int page, int kt, int lane) {
-  typedef Lay<DIM, BITS> L;
-  const int col = lane & 15, g4 = lane >> 4;
+// Where a tile's rows are. Pages of 16 tokens and more (UNI): each half of the tile lies in one page, so a scalar buffer
+// descriptor holds its address, and a lane's 32-bit offset into it stays the same from tile to tile. Smaller pages: lane l % 32 holds
+// the offsets of key l % 32, and the lanes that load a part of its row fetch them by a shuffle.
+template <bool UNI>
+struct Rows {
+  int64_t off[2], par_off[2];
+  // page: lane l holds the page of key kt + l % 32
+  __device__ __forceinline__ void set(const Pages& pg, int page, int kt, int lane, bool par) {
+    if constexpr (UNI) {
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int kk = 8 * (col >> 2) + 4 * u + (col & 3), mine = __shfl(page, kk);
-    const char* kr = pg.row(pg.k, pg.stride, pg.token, mine, kt + kk) + g4 * L::kPiece;
-#pragma unroll
-    for (int i = 0; i < L::kLoads; ++i) load_words<L::kPiece>(kr + 4 * i * L::kPiece, t.k[u][i]);
-    if constexpr (BITS < 16) {
-      const char* pr = pg.row(pg.k_par, pg.par_stride, pg.par_token, mine, kt + kk);
-#pragma unroll
-      for (int i = 0; i < L::kLoads; ++i) t.k_par[u][i] = *(const uint32_t*)(pr + (4 * i + g4) * L::kPieceCh / 32 * 4);
+      for (int h = 0; h < 2; ++h) {
+        const int p = __builtin_amdgcn_readlane(page, 16 * h), in_page = (kt + 16 * h) & pg.mask;
+        off[h] = p * pg.stride + (uint32_t)(in_page * pg.token);
+        if (par) par_off[h] = p * pg.par_stride + (uint32_t)(in_page * pg.par_token);
+      }
+    } else {
+      const int in_page = (kt + (lane & 31)) & pg.mask;
+      off[0] = page * pg.stride + (uint32_t)(in_page * pg.token);
+      if (par) par_off[0] = page * pg.par_stride + (uint32_t)(in_page * pg.par_token);
     }
+  }
+  __device__ __forceinline__ static int64_t shuffled(int64_t v, int from) {
+    return (int64_t)(uint32_t)__shfl((int)(uint32_t)v, from) | (int64_t)__shfl((int)(v >> 32), from) << 32;
+  }
+};
+
+// Words of rows of one half of a tile: of row `row`, which is `lane_row` + a constant, from byte `byte` on.
+template <int BYTES, bool UNI>
+__device__ __forceinline__ void load_row(const char* base, const int64_t* off, int token, int half, int lane_row, int row, int byte, uint32_t* w) {
+  if constexpr (UNI) {
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(base + off[half]), 0, 16 * token, 0x00020000);
+    const int voff = lane_row * token + byte, soff = (row - lane_row) * token;
+    if constexpr (BYTES == 16) {
+      const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, voff, soff, 0);
+      w[0] = v[0], w[1] = v[1], w[2] = v[2], w[3] = v[3];
+    } else if constexpr (BYTES == 8) {
+      const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(r, voff, soff, 0);
+      w[0] = v[0], w[1] = v[1];
+    } else {
+      w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, voff, soff, 0);
+    }
+  } else {
+    load_words<BYTES>(base + Rows<false>::shuffled(off[0], 16 * half + row) + byte, w);
   }
 }
 
-template <int DIM, int BITS>
-__device__ __forceinline__ void load_values(Tile<DIM, BITS>& t, const Pages& pg, int page, int kt, int lane) {
+template <int DIM, int BITS, bool UNI>
+__device__ __forceinline__ void load_keys(Tile<DIM, BITS>& t, const Pages& pg, const Rows<UNI>& rows, int lane) {
+  typedef Lay<DIM, BITS> L;
+  const int col = lane & 15, g4 = lane >> 4;
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int i = 0; i < L::kLoads; ++i) {
+      load_row<L::kPiece, UNI>(pg.k, rows.off, pg.token, u, col, col, (4 * i + g4) * L::kPiece, t.k[u][i]);
+      if constexpr (BITS < 16)
+        load_row<4, UNI>(pg.k_par, rows.par_off, pg.par_token, u, col, col, g4 * L::kPieceCh / 32 * 4 + i * L::kPieceCh / 8 * 4, &t.k_par[u][i]);
+    }
+}
+
+template <int DIM, int BITS, bool UNI>
+__device__ __forceinline__ void load_values(Tile<DIM, BITS>& t, const Pages& pg, const Rows<UNI>& rows, int lane) {
   typedef Lay<DIM, BITS> L;
 #pragma unroll
-  for (int i = 0; i < L::kVLoads; ++i) {
-    const int p = lane + 64 * i, kk = p / L::kVPer, piece = p % L::kVPer, mine = __shfl(page, kk);
-    load_words<L::kVPiece>(pg.row(pg.v, pg.stride, pg.token, mine, kt + kk) + piece * L::kVPiece, t.v[i]);
+  for (int i = 0; i < 2 * L::kVLoads; ++i) {
+    const int half = i / L::kVLoads, row = L::v_row(lane, i % L::kVLoads), piece = L::v_piece(lane, i % L::kVLoads);
+    const int lane_row = 64 % L::kVPer ? row : lane / L::kVPer;
+    load_row<L::kVPiece, UNI>(pg.v, rows.off, pg.token, half, lane_row, row, piece * L::kVPiece, t.v[i]);
     if constexpr (BITS < 16)
-      t.v_par[i] = *(const uint32_t*)(pg.row(pg.v_par, pg.par_stride, pg.par_token, mine, kt + kk) + piece / 2 * 4);
+      load_row<4, UNI>(pg.v_par, rows.par_off, pg.par_token, half, lane_row, row, piece * L::kVCh / 32 * 4, &t.v_par[i]);
   }
 }
+
 // Keys that a workgroup's rows see: [k_lo, k_hi) at most, of them each row those in (pos - window, pos].
 struct Span {
   int k_lo, k_hi, p_lo, p_hi, window;
@@ -198,8 +249,10 @@ __device__ __forceinline__ f32x4 odd_values(Span s, Pages pg, const int32_t* pag
 // What bounds it: HBM reads of the pages. Each wave keeps one tile of keys and values in flight in registers while
 // it works on the one before, and a SIMD holds two to four such waves; the 16 rows that a product has cost the same
 // whether one query head or 16 share the kv head. The page numbers of a tile are loaded two tiles ahead.
-template <int DIM, int BITS, int NB>
-__global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 4 : DIM * NB <= 128 ? 2 : 1)) void k_attn(AttnArgs a) {
+template <int DIM, int BITS, int NB, bool UNI>
+__global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 4 : DIM * NB <= 128 ? 2 : 1)) void k_attn(AttnArgs) {
+  // read where they are used: kept for the whole kernel, the arguments would push the loop's scalars out of their registers
+  const AttnArgs& a = *(const AttnArgs*)__builtin_amdgcn_kernarg_segment_ptr();
   typedef Lay<DIM, BITS> L;
   constexpr int kRows = 16 * NB;
   constexpr int kVBytes = kTile * L::kVStride, kOStride = DIM + 4;
@@ -267,14 +320,17 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 4 : DIM * NB <= 128 ? 2
     int page = page_of(kt), next = page_of(nt);
     uint64_t gone = __ballot((unsigned)page >= (unsigned)n_pages);
     page = (unsigned)page < (unsigned)n_pages ? page : 0;
-    load_keys(T, pg, page, kt, lane);
-    load_values(T, pg, page, kt, lane);
+    Rows<UNI> at;
+    at.set(pg, page, kt, lane, BITS < 16);
+    load_keys<DIM, BITS, UNI>(T, pg, at, lane);
+    load_values<DIM, BITS, UNI>(T, pg, at, lane);
     while (true) {
       const bool last = kt + kTile * kWaves >= k_hi;
       // every row sees the whole tile
       const bool whole = span.whole(kt) && !gone;
       const uint64_t next_gone = __ballot((unsigned)next >= (unsigned)n_pages);
       page = (unsigned)next < (unsigned)n_pages ? next : 0;
+      at.set(pg, page, nt, lane, BITS < 16);
       // scores
       f32x4 st[NB][2] = {};
 #pragma unroll
@@ -295,27 +351,27 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 4 : DIM * NB <= 128 ? 2
           }
       // not above the products: the loads would take registers of their own beside those that they refill
       __builtin_amdgcn_sched_barrier(0);
-      load_keys(T, pg, page, nt, lane);
+      load_keys<DIM, BITS, UNI>(T, pg, at, lane);
       __builtin_amdgcn_sched_barrier(0);
       // values into LDS
 #pragma unroll
-      for (int i = 0; i < L::kVLoads; ++i) {
-        const int p = lane + 64 * i, kk = p / L::kVPer, piece = p % L::kVPer;
+      for (int i = 0; i < 2 * L::kVLoads; ++i) {
+        const int kk = i / L::kVLoads * 16 + L::v_row(lane, i % L::kVLoads), piece = L::v_piece(lane, i % L::kVLoads);
         f16x8 v[L::kVCh / 8];
-        if constexpr (BITS == 16) {
-          v[0] = __builtin_bit_cast(f16x8, make_uint4(T.v[i][0], T.v[i][1], T.v[i][2], T.v[i][3]));
-        } else if constexpr (BITS == 8) {
-          v[0] = decode8w<8>(T.v[i][0], T.v[i][1], T.v_par[i]);
-          v[1] = decode8w<8>(T.v[i][2], T.v[i][3], T.v_par[i]);
-        } else {
-          v[0] = decode8w<4>(T.v[i][0], 0, T.v_par[i]);
-          v[1] = decode8w<4>(T.v[i][1], 0, T.v_par[i]);
+#pragma unroll
+        for (int j = 0; j < L::kVCh / 8; ++j) {
+          if constexpr (BITS == 16)
+            v[j] = __builtin_bit_cast(f16x8, make_uint4(T.v[i][0], T.v[i][1], T.v[i][2], T.v[i][3]));
+          else if constexpr (BITS == 8)
+            v[j] = decode8w<8>(T.v[i][2 * j], T.v[i][2 * j + 1], T.v_par[i]);
+          else
+            v[j] = decode8w<4>(T.v[i][j], 0, T.v_par[i]);
         }
 #pragma unroll
         for (int j = 0; j < L::kVCh / 8; ++j) *(f16x8*)(vs + kk * L::kVStride + (piece * L::kVCh + 8 * j) * 2) = v[j];
       }
       __builtin_amdgcn_sched_barrier(0);
-      load_values(T, pg, page, nt, lane);
+      load_values<DIM, BITS, UNI>(T, pg, at, lane);
       __builtin_amdgcn_sched_barrier(0);
       const int nnt = nt + kTile * kWaves < k_hi ? nt + kTile * kWaves : nt;
       next = page_of(nnt);
@@ -330,10 +386,12 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 4 : DIM * NB <= 128 ? 2
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[n][i] = st[n][i >> 2][i & 3] * a.scale;
         if (!whole) {
+          int at_pos = pos[n];
+          asm volatile("" : "+v"(at_pos));  // keeps the branch: the tests are 60 instructions that few tiles need
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const int key = kt + 8 * g4 + i;
-            x[n][i] = !span.seen(key, pos[n]) ? -INFINITY : (gone >> (8 * g4 + i) & 1) ? __builtin_nanf("") : x[n][i];
+            const int kk = 16 * (i >> 2) + 4 * g4 + (i & 3);
+            x[n][i] = !span.seen(kt + kk, at_pos) ? -INFINITY : (gone >> kk & 1) ? __builtin_nanf("") : x[n][i];
           }
         }
 #pragma unroll
@@ -387,7 +445,7 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 4 : DIM * NB <= 128 ? 2
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const s16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) s16x4*)(vs + (8 * g4 + 4 * j + (col >> 2)) * L::kVStride + 32 * i + 8 * (col & 3)));
+              (__attribute__((address_space(3))) s16x4*)(vs + (16 * j + 4 * g4 + (col >> 2)) * L::kVStride + 32 * i + 8 * (col & 3)));
           const f16x4 f = __builtin_bit_cast(f16x4, w);
 #pragma unroll
           for (int e = 0; e < 4; ++e) vt[4 * j + e] = f[e];
@@ -533,18 +591,18 @@ sph_status check_sizes(const sph_kv_cache* c, int64_t batch, int64_t tokens, int
   return SPH_OK;
 }
 
-template <int BITS, int NB>
+template <int BITS, int NB, bool UNI>
 const void* kernel_for(int dim) {
-  if (dim == 64) return (const void*)k_attn<64, BITS, NB>;
-  if (dim == 96) return (const void*)k_attn<96, BITS, NB>;
-  if (dim == 128) return (const void*)k_attn<128, BITS, NB>;
-  if constexpr (NB == 1) return dim == 192 ? (const void*)k_attn<192, BITS, 1> : (const void*)k_attn<256, BITS, 1>;
+  if (dim == 64) return (const void*)k_attn<64, BITS, NB, UNI>;
+  if (dim == 96) return (const void*)k_attn<96, BITS, NB, UNI>;
+  if (dim == 128) return (const void*)k_attn<128, BITS, NB, UNI>;
+  if constexpr (NB == 1) return dim == 192 ? (const void*)k_attn<192, BITS, 1, UNI> : (const void*)k_attn<256, BITS, 1, UNI>;
   return nullptr;
 }
 
-template <int NB>
+template <int NB, bool UNI>
 const void* kernel_for(int bits, int dim) {
-  return bits == 16 ? kernel_for<16, NB>(dim) : bits == 8 ? kernel_for<8, NB>(dim) : kernel_for<4, NB>(dim);
+  return bits == 16 ? kernel_for<16, NB, UNI>(dim) : bits == 8 ? kernel_for<8, NB, UNI>(dim) : kernel_for<4, NB, UNI>(dim);
 }
 
 bool launch_ok(const void* fn, dim3 grid, hipStream_t s, AttnArgs& a) {
@@ -599,7 +657,9 @@ sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t token
   if (p.bytes) a.ml = (float2*)((float*)d_ws + (size_t)p.splits * tokens * q_heads * cache->head_dim);
   const int64_t grid = (int64_t)cache->kv_heads * p.splits * p.tiles * batch, rows = tokens * q_heads;
   if (grid >= (1 << 24) || (p.splits > 1 && rows >= (1 << 26))) return SPH_ERR_SHAPE;
-  const void* fn = p.nb == 1 ? kernel_for<1>(cache->bits, cache->head_dim) : kernel_for<2>(cache->bits, cache->head_dim);
+  const int bits = cache->bits, dim = cache->head_dim;
+  const void* fn = cache->page_size >= 16 ? (p.nb == 1 ? kernel_for<1, true>(bits, dim) : kernel_for<2, true>(bits, dim))
+                                          : (p.nb == 1 ? kernel_for<1, false>(bits, dim) : kernel_for<2, false>(bits, dim));
   if (!launch_ok(fn, dim3((unsigned)grid), (hipStream_t)stream, a)) return SPH_ERR_HIP;
   if (p.splits > 1 && !launch_ok((const void*)k_attn_join, dim3((unsigned)rows, cache->head_dim / kJoinCh), (hipStream_t)stream, a)) return SPH_ERR_HIP;
   return SPH_OK;

@@ -23,10 +23,10 @@ struct CacheView {
 int sph_cache_check(const sph_kv_cache* c);
 CacheView sph_cache_view(const sph_kv_cache* c);
 
-// Two codes as fp16 numbers: a code below 1024 in the mantissa of 1024.0 (0x6400) is 1024 + code exactly, so the
-// packed subtraction gives the code exactly, and one packed multiply-add rounds offset + code * step once.
-__device__ __forceinline__ f16x2 decode2(uint32_t mantissas, f16x2 step, f16x2 off) {
-  const f16x2 q = __builtin_bit_cast(f16x2, mantissas | 0x64006400u) - (f16x2){(_Float16)1024.0f, (_Float16)1024.0f};
+// Two codes as fp16 numbers, from halves that hold `one` + code (a power of two with the code in its mantissa): the packed
+// subtraction gives the code exactly, and one packed multiply-add rounds offset + code * step once.
+__device__ __forceinline__ f16x2 decode2(uint32_t halves, float one, f16x2 step, f16x2 off) {
+  const f16x2 q = __builtin_bit_cast(f16x2, halves) - (f16x2){(_Float16)one, (_Float16)one};
   return __builtin_elementwise_fma(q, step, off);
 }
 
@@ -37,14 +37,21 @@ __device__ __forceinline__ f16x8 decode8w(uint32_t w0, uint32_t w1, uint32_t par
   const f16x2 off = {p[0], p[0]}, step = {p[1], p[1]};
   f16x2 r[4];
   if constexpr (BITS == 8) {
-    // bytes 0 and 1 (2 and 3) of a word to the low bytes of two halves
-    r[0] = decode2(__builtin_amdgcn_perm(0, w0, 0x0C010C00u), step, off);
-    r[1] = decode2(__builtin_amdgcn_perm(0, w0, 0x0C030C02u), step, off);
-    r[2] = decode2(__builtin_amdgcn_perm(0, w1, 0x0C010C00u), step, off);
-    r[3] = decode2(__builtin_amdgcn_perm(0, w1, 0x0C030C02u), step, off);
+    // two bytes of a word below the high byte of 1024.0 (0x6400), whose last bit is worth 1
+    r[0] = decode2(__builtin_amdgcn_perm(0x64646464u, w0, 0x04010400u), 1024.0f, step, off);
+    r[1] = decode2(__builtin_amdgcn_perm(0x64646464u, w0, 0x04030402u), 1024.0f, step, off);
+    r[2] = decode2(__builtin_amdgcn_perm(0x64646464u, w1, 0x04010400u), 1024.0f, step, off);
+    r[3] = decode2(__builtin_amdgcn_perm(0x64646464u, w1, 0x04030402u), 1024.0f, step, off);
   } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = decode2((w0 >> (4 * i)) & 0x000F000Fu, step, off);
+    // bits 4..7 are worth 1..8 in 64.0 (0x5400), which spares every other shift
+    uint32_t low = 0x000F000Fu, high = 0x00F000F0u, m1024 = 0x64006400u, m64 = 0x54005400u;
+    // in registers, one of each pair scalar: v_and_or_b32 takes no literals
+    asm("" : "+s"(low), "+s"(high), "+v"(m1024), "+v"(m64));
+    const uint32_t w8 = w0 >> 8;
+    r[0] = decode2((w0 & low) | m1024, 1024.0f, step, off);
+    r[1] = decode2((w0 & high) | m64, 64.0f, step, off);
+    r[2] = decode2((w8 & low) | m1024, 1024.0f, step, off);
+    r[3] = decode2((w8 & high) | m64, 64.0f, step, off);
   }
   f16x8 y;
 #pragma unroll
