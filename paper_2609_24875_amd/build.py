@@ -11,7 +11,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 SOURCES = [os.path.join(CSRC, "sph_kernels.hip"), os.path.join(CSRC, "sph_encode.hip"),
            os.path.join(CSRC, "sph_train.hip"), os.path.join(CSRC, "sph_cache.hip"),
-           os.path.join(CSRC, "sph_attn.hip"), os.path.join(CSRC, "sph_pack.cpp")]
+           os.path.join(CSRC, "sph_attn.hip"), os.path.join(CSRC, "sph_attn_wide.hip"),
+           os.path.join(CSRC, "sph_pack.cpp")]
 OUT = os.path.join(HERE, "libsph.so")
 # A separate measurement probe (plain streaming read), loaded by the benchmark only.
 PROBE_SOURCES = [os.path.join(CSRC, "sph_probe.hip")]

@@ -1,0 +1,157 @@
+// What the attention's kernels share: their arguments, the pages of a kv head, which keys rows see, and how rows are written.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "sph_cache.h"
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+struct AttnArgs {
+  CacheView c;
+  const char* q;
+  char* o;
+  int64_t qt, qh, ot, oh;  // strides in bytes
+  const int32_t* q_start;
+  const int32_t* pages;
+  int64_t pages_stride;
+  const int32_t* lens;
+  float* lse;
+  float* part;             // [splits][tokens][q_heads][dim], then (m, l) pairs [splits][tokens][q_heads]
+  float2* ml;
+  int64_t tokens;
+  int batch, q_heads, group, max_q, max_len, window, tiles, splits, chunk;
+  float scale;             // times log2 e
+};
+
+// The kernel for more rows a kv head than k_attn takes, and its rows a workgroup and keys a tile.
+const void* sph_attn_wide_kernel(int bits, int dim);
+constexpr int kWideRows = 128;
+static inline int sph_attn_wide_tile(int dim) { return dim <= 128 ? 64 : 32; }
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+
+// The queries of one sequence.
+struct Seq {
+  int start, n, len;
+  bool bad;
+  __device__ __forceinline__ void load(const AttnArgs& a, int b) {
+    start = a.q_start ? a.q_start[b] : b;
+    const int end = a.q_start ? a.q_start[b + 1] : b + 1;
+    n = end - start;
+    len = a.lens[b];
+    bad = len < 0 || len > a.max_len || start < 0 || end > a.tokens || n < 0 || n > a.max_q;
+  }
+};
+
+__device__ __forceinline__ void write_out(const AttnArgs& a, int split, int64_t token, int head, int ch, f32x4 acc, float m, float l) {
+  if (a.splits > 1) {
+    const int64_t row = (split * a.tokens + token) * a.q_heads + head;
+    *(f32x4*)(a.part + row * a.c.dim + ch) = acc;
+    if (ch == 0) a.ml[row] = make_float2(m, l);
+    return;
+  }
+  // l is NaN for poisoned rows; 0 where nothing is seen
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  f16x4 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = (_Float16)(l == 0.0f ? 0.0f : acc[i] * inv);
+  *(f16x4*)(a.o + token * a.ot + head * a.oh + 2 * ch) = y;
+  if (ch == 0 && a.lse) a.lse[token * a.q_heads + head] = l == 0.0f ? -INFINITY : (m + __builtin_log2f(l)) * kLn2;
+}
+
+// Every row of a sequence that the device found to be outside its bounds becomes NaN.
+__device__ void write_bad(const AttnArgs& a, const Seq& s, int kvh, int split) {
+  const int64_t t0 = max(s.start, 0), t1 = min((int64_t)s.start + s.n, a.tokens);
+  const float nan = __builtin_nanf("");
+  const int per = a.group * (a.c.dim / 4);
+  for (int64_t t = t0; t < t1; ++t)
+    for (int i = threadIdx.x; i < per; i += blockDim.x)
+      write_out(a, split, t, kvh * a.group + i / (a.c.dim / 4), i % (a.c.dim / 4) * 4, f32x4{nan, nan, nan, nan}, 0.0f, nan);
+}
+
+template <int BYTES>
+__device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
+  if constexpr (BYTES == 16) {
+    const uint4 v = *(const uint4*)p;
+    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+  } else if constexpr (BYTES == 8) {
+    const uint2 v = *(const uint2*)p;
+    w[0] = v.x, w[1] = v.y;
+  } else {
+    w[0] = *(const uint32_t*)p;
+  }
+}
+
+// One kv head's pages.
+struct Pages {
+  const char *k, *v, *k_par, *v_par;
+  int64_t stride, par_stride;
+  int token, par_token;      // bytes between tokens of a page
+  int mask, shift, count;
+  __device__ __forceinline__ void set(const CacheView& c, int head) {
+    k = c.k + head * c.head_stride, v = c.v + head * c.head_stride;
+    k_par = c.k_par + head * c.par_head_stride, v_par = c.v_par + head * c.par_head_stride;
+    stride = c.page_stride, par_stride = c.par_page_stride;
+    token = (int)c.token_stride, par_token = (int)c.par_token_stride;
+    shift = c.page_shift, mask = (1 << shift) - 1, count = (int)c.n_pages;
+  }
+  __device__ __forceinline__ bool there(int page) const { return (unsigned)page < (unsigned)count; }
+  __device__ __forceinline__ const char* row(const char* base, int64_t page_stride, int token_stride, int page, int key) const {
+    return base + page * page_stride + (uint32_t)((key & mask) * token_stride);
+  }
+};
+
+// Keys that a workgroup's rows see: [k_lo, k_hi) at most, of them each row those in (pos - window, pos].
+struct Span {
+  int k_lo, k_hi, p_lo, p_hi, window, tile;
+  // every row sees the whole tile at kt
+  __device__ __forceinline__ bool whole(int kt) const {
+    return kt >= k_lo && kt + tile <= k_hi && kt + tile - 1 <= p_lo && (!window || kt > p_hi - window);
+  }
+  __device__ __forceinline__ bool seen(int key, int pos) const { return key >= k_lo && key < k_hi && key <= pos && (!window || key > pos - window); }
+};
+
+// Two values in LDS: zero if no row sees them, otherwise with infinities and NaN taken out. Returns whether there was one.
+__device__ __forceinline__ bool clean_word(uint32_t* w, bool unseen) {
+  uint32_t v = unseen ? 0 : *w;
+  const bool low = (v & 0x7C00u) == 0x7C00u, high = (v & 0x7C000000u) == 0x7C000000u;
+  if (low) v &= 0xFFFF0000u;
+  if (high) v &= 0xFFFFu;
+  *w = v;
+  return low || high;
+}
+
+// The sum of the infinities and NaN among channels ch .. ch + 3 of the values that a row at position pos sees in tiles that not
+// every row sees: a weight is positive, so it leaves them what they are. Only called where there are some.
+template <int DIM, int BITS>
+__device__ __forceinline__ f32x4 odd_values(const Span& s, const Pages& pg, const int32_t* pages, int pos, int ch) {
+  f32x4 sum = {};
+#pragma unroll 1
+  for (int key = s.k_lo; key < s.k_hi; ++key) {
+    const int page = pages[key >> pg.shift];
+    if (s.whole(key & ~(s.tile - 1)) || !s.seen(key, pos) || !pg.there(page)) continue;
+    const char* row = pg.row(pg.v, pg.stride, pg.token, page, key);
+    f16x8 v;
+    if constexpr (BITS == 16)
+      v = *(const f16x8*)(row + 2 * (ch & ~7));
+    else
+      v = decode8<BITS>(row + (ch & ~7) * BITS / 8, *(const uint32_t*)(pg.row(pg.v_par, pg.par_stride, pg.par_token, page, key) + ch / 32 * 4));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float f = (float)(ch & 4 ? v[4 + e] : v[e]);
+      if (!__builtin_isfinite(f)) sum[e] += f;
+    }
+  }
+  return sum;
+}
+
+}  // namespace

@@ -15,74 +15,11 @@
 
 #include <algorithm>
 
-#include "sph_cache.h"
+#include "sph_attn.h"
 
 namespace {
 
-constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kLn2 = 0.69314718055994530942f;
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kTile = 32;                 // keys of a wave's step
-
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-struct AttnArgs {
-  CacheView c;
-  const char* q;
-  char* o;
-  int64_t qt, qh, ot, oh;  // strides in bytes
-  const int32_t* q_start;
-  const int32_t* pages;
-  int64_t pages_stride;
-  const int32_t* lens;
-  float* lse;
-  float* part;             // [splits][tokens][q_heads][dim], then (m, l) pairs [splits][tokens][q_heads]
-  float2* ml;
-  int64_t tokens;
-  int batch, q_heads, group, max_q, max_len, window, tiles, splits, chunk;
-  float scale;             // times log2 e
-};
-
-// The queries of one sequence.
-struct Seq {
-  int start, n, len;
-  bool bad;
-  __device__ __forceinline__ void load(const AttnArgs& a, int b) {
-    start = a.q_start ? a.q_start[b] : b;
-    const int end = a.q_start ? a.q_start[b + 1] : b + 1;
-    n = end - start;
-    len = a.lens[b];
-    bad = len < 0 || len > a.max_len || start < 0 || end > a.tokens || n < 0 || n > a.max_q;
-  }
-};
-
-__device__ __forceinline__ void write_out(const AttnArgs& a, int split, int64_t token, int head, int ch, f32x4 acc, float m, float l) {
-  if (a.splits > 1) {
-    const int64_t row = (split * a.tokens + token) * a.q_heads + head;
-    *(f32x4*)(a.part + row * a.c.dim + ch) = acc;
-    if (ch == 0) a.ml[row] = make_float2(m, l);
-    return;
-  }
-  // l is NaN for poisoned rows; 0 where nothing is seen
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  f16x4 y;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) y[i] = (_Float16)(l == 0.0f ? 0.0f : acc[i] * inv);
-  *(f16x4*)(a.o + token * a.ot + head * a.oh + 2 * ch) = y;
-  if (ch == 0 && a.lse) a.lse[token * a.q_heads + head] = l == 0.0f ? -INFINITY : (m + __builtin_log2f(l)) * kLn2;
-}
-
-// Every row of a sequence that the device found to be outside its bounds becomes NaN.
-__device__ void write_bad(const AttnArgs& a, const Seq& s, int kvh, int split) {
-  const int64_t t0 = max(s.start, 0), t1 = min((int64_t)s.start + s.n, a.tokens);
-  const float nan = __builtin_nanf("");
-  const int per = a.group * (a.c.dim / 4);
-  for (int64_t t = t0; t < t1; ++t)
-    for (int i = threadIdx.x; i < per; i += blockDim.x)
-      write_out(a, split, t, kvh * a.group + i / (a.c.dim / 4), i % (a.c.dim / 4) * 4, f32x4{nan, nan, nan, nan}, 0.0f, nan);
-}
 
 template <int DIM, int BITS>
 struct Lay {
@@ -113,30 +50,6 @@ struct Tile {
   typedef Lay<DIM, BITS> L;
   uint32_t k[2][L::kLoads][L::kPiece / 4], v[2 * L::kVLoads][L::kVPiece / 4];
   uint32_t k_par[2][L::kLoads], v_par[2 * L::kVLoads];
-};
-
-template <int BYTES>
-__device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
-  if constexpr (BYTES == 16) {
-    const uint4 v = *(const uint4*)p;
-    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-  } else if constexpr (BYTES == 8) {
-    const uint2 v = *(const uint2*)p;
-    w[0] = v.x, w[1] = v.y;
-  } else {
-    w[0] = *(const uint32_t*)p;
-  }
-}
-
-// One kv head's pages.
-struct Pages {
-  const char *k, *v, *k_par, *v_par;
-  int64_t stride, par_stride;
-  int token, par_token;      // bytes between tokens of a page
-  int mask;
-  __device__ __forceinline__ const char* row(const char* base, int64_t page_stride, int token_stride, int page, int key) const {
-    return base + page * page_stride + (uint32_t)((key & mask) * token_stride);
-  }
 };
 
 // Where a tile's rows are. Pages of 16 tokens and more (UNI): each half of the tile lies in one page, so a scalar buffer
@@ -212,40 +125,6 @@ __device__ __forceinline__ void load_values(Tile<DIM, BITS>& t, const Pages& pg,
   }
 }
 
-// Keys that a workgroup's rows see: [k_lo, k_hi) at most, of them each row those in (pos - window, pos].
-struct Span {
-  int k_lo, k_hi, p_lo, p_hi, window;
-  // every row sees the whole tile at kt
-  __device__ __forceinline__ bool whole(int kt) const {
-    return kt >= k_lo && kt + kTile <= k_hi && kt + kTile - 1 <= p_lo && (!window || kt > p_hi - window);
-  }
-  __device__ __forceinline__ bool seen(int key, int pos) const { return key >= k_lo && key < k_hi && key <= pos && (!window || key > pos - window); }
-};
-
-// The sum of the infinities and NaN among channels ch .. ch + 3 of the values that a row at position pos sees in tiles that not
-// every row sees: a weight is positive, so it leaves them what they are. Only called where there are some.
-template <int DIM, int BITS>
-__device__ __forceinline__ f32x4 odd_values(Span s, Pages pg, const int32_t* pages, int shift, int n_pages, int pos, int ch) {
-  f32x4 sum = {};
-#pragma unroll 1
-  for (int key = s.k_lo; key < s.k_hi; ++key) {
-    const int page = pages[key >> shift];
-    if (s.whole(key & ~(kTile - 1)) || !s.seen(key, pos) || (unsigned)page >= (unsigned)n_pages) continue;
-    const char* row = pg.row(pg.v, pg.stride, pg.token, page, key);
-    f16x8 v;
-    if constexpr (BITS == 16)
-      v = *(const f16x8*)(row + 2 * (ch & ~7));
-    else
-      v = decode8<BITS>(row + (ch & ~7) * BITS / 8, *(const uint32_t*)(pg.row(pg.v_par, pg.par_stride, pg.par_token, page, key) + ch / 32 * 4));
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float f = (float)(ch & 4 ? v[4 + e] : v[e]);
-      if (!__builtin_isfinite(f)) sum[e] += f;
-    }
-  }
-  return sum;
-}
-
 // What bounds it: HBM reads of the pages. Each wave keeps one tile of keys and values in flight in registers while
 // it works on the one before, and a SIMD holds two to four such waves; the 16 rows that a product has cost the same
 // whether one query head or 16 share the kv head. The page numbers of a tile are loaded two tiles ahead.
@@ -280,15 +159,10 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 4 : DIM * NB <= 128 ? 2
   const int p_lo = first + r0 / a.group, p_hi = first + (r0 + nrow - 1) / a.group;  // positions of the rows
   const int lo = a.window ? max(0, p_lo - a.window + 1) : 0, hi = p_hi + 1;
   const int k_lo = max(lo, (lo & ~(kTile - 1)) + split * a.chunk), k_hi = min(hi, (lo & ~(kTile - 1)) + (split + 1) * a.chunk);
-  const Span span = {k_lo, k_hi, p_lo, p_hi, a.window};
+  const Span span = {k_lo, k_hi, p_lo, p_hi, a.window, kTile};
   const int32_t* pages = a.pages + b * a.pages_stride;
   Pages pg;
-  pg.k = a.c.k + kvh * a.c.head_stride, pg.v = a.c.v + kvh * a.c.head_stride;
-  pg.k_par = a.c.k_par + kvh * a.c.par_head_stride, pg.v_par = a.c.v_par + kvh * a.c.par_head_stride;
-  pg.stride = a.c.page_stride, pg.par_stride = a.c.par_page_stride;
-  pg.token = (int)a.c.token_stride, pg.par_token = (int)a.c.par_token_stride;
-  const int shift = a.c.page_shift, n_pages = (int)a.c.n_pages;
-  pg.mask = (1 << shift) - 1;
+  pg.set(a.c, kvh);
 
   int pos[NB];
   bool odd = false;
@@ -310,16 +184,16 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 4 : DIM * NB <= 128 ? 2
         for (int j = 0; j < L::kBlocks; ++j)
           q[n][i * L::kBlocks + j] = *(const f16x8*)(qr + 2 * ((4 * i + g4) * L::kPieceCh + 8 * j));
     }
-    const int e_lo = k_lo >> shift, e_hi = (k_hi - 1) >> shift;
+    const int e_lo = k_lo >> pg.shift, e_hi = (k_hi - 1) >> pg.shift;
     // keys outside the stretch take a page inside it: their rows are read and not used
-    auto page_of = [&](int kt) { return pages[min(max((kt + (lane & 31)) >> shift, e_lo), e_hi)]; };
+    auto page_of = [&](int kt) { return pages[min(max((kt + (lane & 31)) >> pg.shift, e_lo), e_hi)]; };
     char* vs = lds + wave * kVBytes;
 
     Tile<DIM, BITS> T;
     int kt = t0, nt = t0 + kTile * kWaves < k_hi ? t0 + kTile * kWaves : t0;
     int page = page_of(kt), next = page_of(nt);
-    uint64_t gone = __ballot((unsigned)page >= (unsigned)n_pages);
-    page = (unsigned)page < (unsigned)n_pages ? page : 0;
+    uint64_t gone = __ballot(!pg.there(page));
+    page = pg.there(page) ? page : 0;
     Rows<UNI> at;
     at.set(pg, page, kt, lane, BITS < 16);
     load_keys<DIM, BITS, UNI>(T, pg, at, lane);
@@ -328,8 +202,8 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 4 : DIM * NB <= 128 ? 2
       const bool last = kt + kTile * kWaves >= k_hi;
       // every row sees the whole tile
       const bool whole = span.whole(kt) && !gone;
-      const uint64_t next_gone = __ballot((unsigned)next >= (unsigned)n_pages);
-      page = (unsigned)next < (unsigned)n_pages ? next : 0;
+      const uint64_t next_gone = __ballot(!pg.there(next));
+      page = pg.there(next) ? next : 0;
       at.set(pg, page, nt, lane, BITS < 16);
       // scores
       f32x4 st[NB][2] = {};
@@ -428,13 +302,7 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 4 : DIM * NB <= 128 ? 2
 #pragma unroll 1
         for (int i = lane; i < kTile * (DIM / 2); i += 64) {
           const int kk = i / (DIM / 2);
-          uint32_t* w = (uint32_t*)(vs + kk * L::kVStride + i % (DIM / 2) * 4);
-          uint32_t v = *w;
-          if (kt + kk < k_lo || kt + kk >= k_hi || (gone >> kk & 1)) v = 0;
-          if ((v & 0x7C00u) == 0x7C00u || (v & 0x7C000000u) == 0x7C000000u) odd = true;
-          if ((v & 0x7C00u) == 0x7C00u) v &= 0xFFFF0000u;
-          if ((v & 0x7C000000u) == 0x7C000000u) v &= 0xFFFFu;
-          *w = v;
+          odd |= clean_word((uint32_t*)(vs + kk * L::kVStride + i % (DIM / 2) * 4), kt + kk < k_lo || kt + kk >= k_hi || (gone >> kk & 1));
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -492,7 +360,7 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 4 : DIM * NB <= 128 ? 2
       acc += f * *(const f32x4*)((float*)lds + (w * kRows + row) * kOStride + ch);
     }
     const int rr = r0 + row;
-    if (any_odd) acc += odd_values<DIM, BITS>(span, pg, pages, shift, n_pages, first + rr / a.group, ch);
+    if (any_odd) acc += odd_values<DIM, BITS>(span, pg, pages, first + rr / a.group, ch);
     write_out(a, split, s.start + rr / a.group, kvh * a.group + rr % a.group, ch, acc, mm, ll);
   }
 }
@@ -557,22 +425,26 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(AttnArgs a) {
 // ------------------------------------------------------------------ host side
 
 struct Plan {
-  int nb, tiles, splits, chunk;
+  int wide, nb, rows, tiles, splits, chunk;
   size_t bytes;
 };
 
-constexpr int kWant = 1024;
+constexpr int kWant = 768;
 
-// Stretches of at least 128 keys (one tile a wave), and few enough workgroups that each has work for a while.
+// Workgroups take stretches of at least 128 keys (one tile a wave), and few enough of them that each has work for a while.
 Plan plan_of(const sph_kv_cache* c, int64_t batch, int64_t tokens, int q_heads, int64_t max_q, int64_t max_len, int64_t window) {
   Plan p{};
   const int group = q_heads / c->kv_heads;
-  p.nb = max_q * group <= 16 || c->head_dim > 128 ? 1 : 2;  // two blocks of rows of wider heads do not fit the registers
-  const int rows = 16 * p.nb;
-  p.tiles = (int)((max_q * group + rows - 1) / rows);
-  const int64_t span = window > 0 ? std::min<int64_t>(max_len, window + rows / group + 1 + kTile) : max_len;
-  const int64_t units = (int64_t)c->kv_heads * batch * p.tiles, step = kTile * kWaves;
-  const int64_t want = std::min<int64_t>(kMaxSplits, std::max<int64_t>(1, kWant / units));
+  const int64_t asked = max_q * group;
+  // two blocks of rows of wider heads do not fit the registers
+  p.nb = asked <= 16 || c->head_dim > 128 ? 1 : 2;
+  p.wide = asked > 16 * p.nb;
+  p.rows = p.wide ? kWideRows : 16 * p.nb;
+  p.tiles = (int)((asked + p.rows - 1) / p.rows);
+  const int64_t tile = p.wide ? sph_attn_wide_tile(c->head_dim) : kTile;
+  const int64_t span = window > 0 ? std::min<int64_t>(max_len, window + p.rows / group + 1 + tile) : max_len;
+  const int64_t units = (int64_t)c->kv_heads * batch * p.tiles, step = p.wide ? 4 * tile : tile * kWaves;
+  const int64_t want = std::min<int64_t>(kMaxSplits, std::max<int64_t>(1, (p.wide ? 512 : kWant) / units));
   int64_t chunk = (span + want - 1) / want;
   chunk = std::max<int64_t>(step, (chunk + step - 1) / step * step);
   p.chunk = (int)chunk;
@@ -658,7 +530,8 @@ sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t token
   const int64_t grid = (int64_t)cache->kv_heads * p.splits * p.tiles * batch, rows = tokens * q_heads;
   if (grid >= (1 << 24) || (p.splits > 1 && rows >= (1 << 26))) return SPH_ERR_SHAPE;
   const int bits = cache->bits, dim = cache->head_dim;
-  const void* fn = cache->page_size >= 16 ? (p.nb == 1 ? kernel_for<1, true>(bits, dim) : kernel_for<2, true>(bits, dim))
+  const void* fn = p.wide ? sph_attn_wide_kernel(bits, dim)
+                   : cache->page_size >= 16 ? (p.nb == 1 ? kernel_for<1, true>(bits, dim) : kernel_for<2, true>(bits, dim))
                                           : (p.nb == 1 ? kernel_for<1, false>(bits, dim) : kernel_for<2, false>(bits, dim));
   if (!launch_ok(fn, dim3((unsigned)grid), (hipStream_t)stream, a)) return SPH_ERR_HIP;
   if (p.splits > 1 && !launch_ok((const void*)k_attn_join, dim3((unsigned)rows, cache->head_dim / kJoinCh), (hipStream_t)stream, a)) return SPH_ERR_HIP;
