@@ -12,11 +12,12 @@ import math
 
 import numpy as np
 
-from .sph import SPH_F16, SPH_F32, SphError, _check, _stream_handle, load_library
+from .sph import SPH_F16, SPH_F32, _check, _stream_handle, load_library
 
 ROPE_INTERLEAVED, ROPE_INVERSE = 1, 2
 KV_BITS = (16, 8, 4)
 KV_HEAD_DIMS = (64, 96, 128, 192, 256)
+SPH_ERR_NULL, SPH_ERR_BUFFER_TOO_SMALL = 1, 6
 KV_GROUP = 32                       # channels that share an offset and a step
 
 
@@ -103,40 +104,51 @@ def rope_table(rot_dim: int, max_pos: int, device="cuda", stream=None, **scaling
 
 def _ints(t, name: str, device, count: int | None = None):
     import torch
+    if isinstance(t, torch.Tensor) and t.dtype is torch.int32 and t.device == device and t.dim() == 1 and t.is_contiguous() and \
+            (count is None or t.shape[0] == count):
+        return t.data_ptr()
     if not isinstance(t, torch.Tensor) or t.dtype != torch.int32:
         raise TypeError(f"{name} must be a torch.int32 tensor")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, the rows on {device}")
-    if t.dim() != 1 or (count is not None and t.shape[0] != count) or (t.shape[0] > 1 and t.stride(0) != 1):
-        raise ValueError(f"{name} must be contiguous [{count}], got shape {tuple(t.shape)} and strides {tuple(t.stride())}")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be contiguous [{'n' if count is None else count}], got shape {tuple(t.shape)} and strides {tuple(t.stride())}")
 
 
 def _rows(t, name: str, device, dtypes, shape=None):
     """Checks [tokens][heads][channels] rows with unit channel stride; (pointer, token stride, head stride)."""
     import torch
+    if isinstance(t, torch.Tensor) and t.dtype in dtypes and (device is None or t.device == device):
+        sh = t.shape
+        if len(sh) == 3 and (shape is None or sh == shape):
+            s0, s1, s2 = t.stride()
+            if s2 == 1 or sh[2] <= 1 or t.numel() == 0:
+                # the stride of a dimension of one element is never used and may hold anything
+                return t.data_ptr(), s0 if sh[0] > 1 else 0, s1 if sh[1] > 1 else 0
     if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
         raise TypeError(f"{name} must be a tensor of {' or '.join(str(d) for d in dtypes)}")
     if device is not None and t.device != device:
         raise ValueError(f"{name} is on {t.device}, expected {device}")
-    if t.dim() != 3 or (shape is not None and tuple(t.shape) != shape) or (t.numel() > 0 and t.shape[2] > 1 and t.stride(2) != 1):
-        raise ValueError(f"{name} must be {list(shape) if shape else '[tokens][heads][channels]'} with unit channel stride, got "
-                         f"shape {tuple(t.shape)} and strides {tuple(t.stride())}")
-    n, h, _ = t.shape
-    # the stride of a dimension of one element is never used and may hold anything
-    return t.data_ptr(), t.stride(0) if n > 1 else 0, t.stride(1) if h > 1 else 0
+    raise ValueError(f"{name} must be {list(shape) if shape else '[tokens][heads][channels]'} with unit channel stride, got "
+                     f"shape {tuple(t.shape)} and strides {tuple(t.stride())}")
 
 
 def _rope_desc(table, device, interleaved: bool, inverse: bool) -> CRope:
     import torch
-    if not isinstance(table, torch.Tensor) or table.dtype != torch.float32:
+    if not isinstance(table, torch.Tensor) or table.dtype is not torch.float32:
         raise TypeError("table must be a torch.float32 tensor")
     if table.device != device:
         raise ValueError(f"table is on {table.device}, the rows on {device}")
-    if table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous():
+    n, pairs, two = table.shape if table.dim() == 3 else (0, 0, 0)
+    if two != 2 or not table.is_contiguous():
         raise ValueError(f"table must be contiguous [positions][pairs][2], got shape {tuple(table.shape)}")
-    return CRope(table.data_ptr(), table.shape[0], 2 * table.shape[1],
+    return CRope(table.data_ptr(), n, 2 * pairs,
                  (ROPE_INTERLEAVED if interleaved else 0) | (ROPE_INVERSE if inverse else 0))
+
+
+def _new(x):
+    """A contiguous tensor like x (``empty_like`` takes half of ``empty``'s time)."""
+    import torch
+    return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
 
 
 def aligned_rows(t):
@@ -153,14 +165,16 @@ def rope(x, positions, table, interleaved: bool = False, inverse: bool = False, 
     copied. ``inverse`` turns back and is the gradient (``train.rope`` is the differentiable form).
     ``out`` may be x."""
     import torch
-    px, xt, xh = _rows(x, "x", None, (torch.float16, torch.float32))
-    desc = _rope_desc(table, x.device, interleaved, inverse)
-    pos = _ints(positions, "positions", x.device, x.shape[0])
-    if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    py, yt, yh = _rows(out, "out", x.device, (x.dtype,), tuple(x.shape))
-    _check(_library().sph_rope(ctypes.byref(desc), SPH_F16 if x.dtype == torch.float16 else SPH_F32, x.shape[0], x.shape[1],
-                               x.shape[2], px, xt, xh, pos, py, yt, yh, _stream_handle(stream)), "sph_rope")
+    half = (torch.float16, torch.float32)
+    px, xt, xh = _rows(x, "x", None, half)
+    dev, n = x.device, x.shape[0]
+    desc = _rope_desc(table, dev, interleaved, inverse)
+    pos = _ints(positions, "positions", dev, n)
+    out = _new(x) if out is None else out
+    py, yt, yh = _rows(out, "out", dev, (x.dtype,), x.shape)
+    st = _library().sph_rope(ctypes.byref(desc), SPH_F16 if x.dtype is torch.float16 else SPH_F32, n, x.shape[1], x.shape[2],
+                             px, xt, xh, pos, py, yt, yh, _stream_handle(stream))
+    _check(st, "sph_rope")
     return out
 
 
@@ -244,28 +258,31 @@ def kv_append(cache: KVCache, k, v, slots, positions=None, table=None, interleav
     ``table`` and ``positions`` the keys are rotated on the way, and so are the queries q [tokens][q heads][channels] in
     the same launch. Returns the rotated queries in fp16 (``q_out`` or a new tensor; None without q)."""
     import torch
+    dev = cache.device
+    dt = (k.dtype,) if isinstance(k, torch.Tensor) and k.dtype is torch.float16 else (torch.float32,)
     n = k.shape[0] if isinstance(k, torch.Tensor) and k.dim() else 0
     shape = (n, cache.kv_heads, cache.head_dim)
-    dt = (k.dtype,) if isinstance(k, torch.Tensor) and k.dtype in (torch.float16, torch.float32) else (torch.float16, torch.float32)
-    pk, kt, kh = _rows(k, "k", cache.device, dt, shape)
-    pv, vt, vh = _rows(v, "v", cache.device, dt, shape)
-    ps = _ints(slots, "slots", cache.device, n)
+    pk, kt, kh = _rows(k, "k", dev, dt, shape)
+    pv, vt, vh = _rows(v, "v", dev, dt, shape)
+    ps = _ints(slots, "slots", dev, n)
     desc = pos = None
     if table is not None:
-        desc = ctypes.byref(_rope_desc(table, cache.device, interleaved, False))
-        pos = _ints(positions, "positions", cache.device, n)
+        desc = ctypes.byref(_rope_desc(table, dev, interleaved, False))
+        pos = _ints(positions, "positions", dev, n)
     elif positions is not None or q is not None:
         raise ValueError("positions and q need a table")
     pq = po = None
     heads = qt = qh = ot = oh = 0
     if q is not None:
         heads = q.shape[1] if q.dim() == 3 else 0
-        pq, qt, qh = _rows(q, "q", cache.device, dt, (n, heads, cache.head_dim))
+        shape = (n, heads, cache.head_dim)
+        pq, qt, qh = _rows(q, "q", dev, dt, shape)
         if q_out is None:
-            q_out = torch.empty((n, heads, cache.head_dim), dtype=torch.float16, device=cache.device)
-        po, ot, oh = _rows(q_out, "q_out", cache.device, (torch.float16,), (n, heads, cache.head_dim))
-    _check(_library().sph_kv_append(cache._ref, desc, SPH_F16 if dt[0] == torch.float16 else SPH_F32, n, pk, kt, kh, pv, vt, vh, ps,
-                                    heads, pq, qt, qh, po, ot, oh, pos, _stream_handle(stream)), "sph_kv_append")
+            q_out = torch.empty(shape, dtype=torch.float16, device=dev)
+        po, ot, oh = _rows(q_out, "q_out", dev, (torch.float16,), shape)
+    st = _library().sph_kv_append(cache._ref, desc, SPH_F16 if dt[0] is torch.float16 else SPH_F32, n, pk, kt, kh, pv, vt, vh, ps,
+                                  heads, pq, qt, qh, po, ot, oh, pos, _stream_handle(stream))
+    _check(st, "sph_kv_append")
     return q_out if q is not None else None
 
 
@@ -273,15 +290,19 @@ def kv_read(cache: KVCache, slots, out=None, stream=None):
     """The keys and values of int32 ``slots`` as two fp16 tensors [tokens][kv heads][channels]
     (sph_kv_read); rows of slots outside the pool are zero. ``out``: a pair of contiguous tensors."""
     import torch
-    ps = _ints(slots, "slots", cache.device)
+    dev = cache.device
+    ps = _ints(slots, "slots", dev)
     shape = (slots.shape[0], cache.kv_heads, cache.head_dim)
     if out is None:
-        out = tuple(torch.empty(shape, dtype=torch.float16, device=cache.device) for _ in range(2))
-    for t in out:
-        if t.dtype != torch.float16 or t.device != cache.device or tuple(t.shape) != shape or not t.is_contiguous():
-            raise ValueError(f"out must be two contiguous fp16 tensors of shape {shape} on {cache.device}")
-    _check(_library().sph_kv_read(cache._ref, shape[0], ps, out[0].data_ptr(), out[1].data_ptr(), _stream_handle(stream)), "sph_kv_read")
-    return out
+        k = torch.empty(shape, dtype=torch.float16, device=dev)
+        v = torch.empty_like(k)
+    else:
+        k, v = out
+        for t in out:
+            if t.dtype != torch.float16 or t.device != dev or t.shape != shape or not t.is_contiguous():
+                raise ValueError(f"out must be two contiguous fp16 tensors of shape {shape} on {dev}")
+    _check(_library().sph_kv_read(cache._ref, shape[0], ps, k.data_ptr(), v.data_ptr(), _stream_handle(stream)), "sph_kv_read")
+    return k, v
 
 
 # ------------------------------------------------------------------ attention
@@ -294,22 +315,18 @@ def attention_workspace_bytes(cache: KVCache, batch: int, tokens: int, q_heads: 
 
 
 def _attention_workspace(cache: KVCache, need: int, handle: int, stream):
-    """A workspace of at least ``need`` bytes for calls on the stream ``handle``, kept with the cache and grown when a
-    call needs more; streams do not share one, since their calls may run together."""
+    """A workspace of at least ``need`` bytes for calls on the stream ``handle``, kept with the cache; streams do not share
+    one, since their calls may run together."""
     import torch
-    if need == 0:
-        return None, 0
-    ws = cache.workspaces.get(handle)
-    if ws is None or ws.numel() < need:
-        if torch.cuda.is_current_stream_capturing():
-            # memory of the graph's own pool must not serve later calls outside it
-            raise RuntimeError("no workspace of this size on this stream yet: make one call on the capture stream before "
-                               "capturing a graph")
-        # allocated on the stream that uses it, so that the one it replaces is freed behind that stream's calls
-        with torch.cuda.stream(stream):
-            ws = torch.empty(need, dtype=torch.uint8, device=cache.device)
-        cache.workspaces[handle] = ws
-    return ws.data_ptr(), ws.numel()
+    if torch.cuda.is_current_stream_capturing():
+        # memory of the graph's own pool must not serve later calls outside it
+        raise RuntimeError("no workspace of this size on this stream yet: make one call on the capture stream before "
+                           "capturing a graph")
+    # allocated on the stream that uses it, so that the one it replaces is freed behind that stream's calls
+    with torch.cuda.stream(stream):
+        ws = torch.empty(need, dtype=torch.uint8, device=cache.device)
+    cache.workspaces[handle] = ws
+    return ws
 
 
 def attention(q, cache: KVCache, pages, seq_lens, q_start=None, max_q: int = 1, max_len: int | None = None, window: int = 0,
@@ -323,34 +340,46 @@ def attention(q, cache: KVCache, pages, seq_lens, q_start=None, max_q: int = 1, 
     (default: what the pages' columns hold). scale: default channels^-0.5. Returns fp16 o like q, with ``return_lse`` also fp32
     [tokens][q heads], the logarithm of each softmax's sum."""
     import torch
-    pq, qt, qh = _rows(q, "q", cache.device, (torch.float16,))
+    dev, half = cache.device, (torch.float16,)
+    pq, qt, qh = _rows(q, "q", dev, half)
     n, heads, dim = q.shape
     if dim != cache.head_dim:
         raise ValueError(f"q has {dim} channels a head, the cache {cache.head_dim}")
-    if not isinstance(pages, torch.Tensor) or pages.dtype != torch.int32:
+    if not isinstance(pages, torch.Tensor) or pages.dtype is not torch.int32:
         raise TypeError("pages must be a torch.int32 tensor")
-    if pages.dim() != 2 or pages.device != cache.device or (pages.numel() > 0 and pages.shape[1] > 1 and pages.stride(1) != 1):
-        raise ValueError(f"pages must be [batch][columns] on {cache.device} with unit stride along the columns")
-    batch, cols = pages.shape
-    lens = _ints(seq_lens, "seq_lens", cache.device, batch)
-    start = None
-    if q_start is not None:
-        start = _ints(q_start, "q_start", cache.device, batch + 1)
+    batch, cols = pages.shape if pages.dim() == 2 else (-1, 0)
+    if batch < 0 or pages.device != dev or (cols > 1 and batch > 0 and pages.stride(1) != 1):
+        raise ValueError(f"pages must be [batch][columns] on {dev} with unit stride along the columns")
+    lens = _ints(seq_lens, "seq_lens", dev, batch)
+    start = None if q_start is None else _ints(q_start, "q_start", dev, batch + 1)
     held = cols * cache.page_size
     if max_len is None:
         max_len = held
     elif max_len > held:
         raise ValueError(f"max_len {max_len} is more than the {cols} columns of pages hold")
-    stride = pages.stride(0) if batch > 1 else cols
-    if stride < cols:
+    row = pages.stride(0) if batch > 1 else cols
+    if row < cols:
         raise ValueError("rows of pages must not overlap")
     if out is None:
-        out = torch.empty((n, heads, dim), dtype=torch.float16, device=cache.device)
-    po, ot, oh = _rows(out, "out", cache.device, (torch.float16,), (n, heads, dim))
-    lse = torch.empty((n, heads), dtype=torch.float32, device=cache.device) if return_lse else None
+        out = _new(q)
+        po, ot, oh = out.data_ptr(), heads * dim, dim
+    else:
+        po, ot, oh = _rows(out, "out", dev, half, (n, heads, dim))
+    lse = torch.empty((n, heads), dtype=torch.float32, device=dev) if return_lse else None
     handle = _stream_handle(stream)
-    ws, nb = _attention_workspace(cache, attention_workspace_bytes(cache, batch, n, heads, max_q, max_len, window), handle, stream)
-    _check(_library().sph_attention(cache._ref, batch, n, heads, pq, qt, qh, start, max_q, pages.data_ptr(), stride, lens, max_len,
-                                    window, dim ** -0.5 if scale is None else scale, po, ot, oh,
-                                    lse.data_ptr() if return_lse else None, ws, nb, handle), "sph_attention")
+    ws = cache.workspaces.get(handle)
+
+    def call(ws):
+        return _library().sph_attention(cache._ref, batch, n, heads, pq, qt, qh, start, max_q, pages.data_ptr(), row, lens, max_len,
+                                        window, dim ** -0.5 if scale is None else scale, po, ot, oh,
+                                        None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(),
+                                        0 if ws is None else ws.numel(), handle)
+
+    st = call(ws)
+    if st in (SPH_ERR_NULL, SPH_ERR_BUFFER_TOO_SMALL):
+        # the library found, before it launched anything, that it needs a workspace or a larger one
+        need = attention_workspace_bytes(cache, batch, n, heads, max_q, max_len, window)
+        if need > (0 if ws is None else ws.numel()):
+            st = call(_attention_workspace(cache, need, handle, stream))
+    _check(st, "sph_attention")
     return (out, lse) if return_lse else out

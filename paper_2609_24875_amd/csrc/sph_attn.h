@@ -21,10 +21,13 @@ struct AttnArgs {
   int64_t pages_stride;
   const int32_t* lens;
   float* lse;
-  float* part;             // [splits][tokens][q_heads][dim], then (m, l) pairs [splits][tokens][q_heads]
+  // Parts of rows whose keys several workgroups share: [slot][kv head][row of the sequence] of dim fp32 sums, of (m, l) pairs, and
+  // for k_attn each sequence's (first slot, slots).
+  float* part;
   float2* ml;
+  int2* where;
   int64_t tokens;
-  int batch, q_heads, group, max_q, max_len, window, tiles, splits, chunk;
+  int batch, q_heads, group, max_q, max_len, window, tiles, splits, chunk, shares;
   float scale;             // times log2 e
 };
 
@@ -50,17 +53,18 @@ struct Seq {
     len = a.lens[b];
     bad = len < 0 || len > a.max_len || start < 0 || end > a.tokens || n < 0 || n > a.max_q;
   }
+  // k_attn's tiles of 32 keys, from the first that its rows see on: at least one where there are rows to write
+  __device__ __forceinline__ int tiles(int window) const {
+    if (bad) return 1;
+    const int lo = window ? max(0, len - n - window + 1) : 0;
+    return n == 0 ? 0 : max(1, (len - (lo & ~31) + 31) >> 5);
+  }
 };
 
-__device__ __forceinline__ void write_out(const AttnArgs& a, int split, int64_t token, int head, int ch, f32x4 acc, float m, float l) {
-  if (a.splits > 1) {
-    const int64_t row = (split * a.tokens + token) * a.q_heads + head;
-    *(f32x4*)(a.part + row * a.c.dim + ch) = acc;
-    if (ch == 0) a.ml[row] = make_float2(m, l);
-    return;
-  }
-  // l is NaN for poisoned rows; 0 where nothing is seen
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+// Four channels of a row: normalised, or as the part `slot` of it.
+__device__ __forceinline__ void write_out(const AttnArgs& a, int64_t token, int head, int ch, f32x4 acc, float m, float l) {
+  // l is NaN for poisoned rows, 0 where nothing is seen
+  const float inv = 1.0f / l;
   f16x4 y;
 #pragma unroll
   for (int i = 0; i < 4; ++i) y[i] = (_Float16)(l == 0.0f ? 0.0f : acc[i] * inv);
@@ -68,14 +72,24 @@ __device__ __forceinline__ void write_out(const AttnArgs& a, int split, int64_t 
   if (ch == 0 && a.lse) a.lse[token * a.q_heads + head] = l == 0.0f ? -INFINITY : (m + __builtin_log2f(l)) * kLn2;
 }
 
+__device__ __forceinline__ int64_t part_at(const AttnArgs& a, int slot, int kvh, int row) {
+  return ((int64_t)slot * a.c.kv_heads + kvh) * ((int64_t)a.max_q * a.group) + row;
+}
+
+__device__ __forceinline__ void write_part(const AttnArgs& a, int slot, int kvh, int row, int ch, f32x4 acc, float m, float l) {
+  const int64_t at = part_at(a, slot, kvh, row);
+  *(f32x4*)(a.part + at * a.c.dim + ch) = acc;
+  if (ch == 0) a.ml[at] = make_float2(m, l);
+}
+
 // Every row of a sequence that the device found to be outside its bounds becomes NaN.
-__device__ void write_bad(const AttnArgs& a, const Seq& s, int kvh, int split) {
+__device__ inline void write_bad(const AttnArgs& a, const Seq& s, int kvh) {
   const int64_t t0 = max(s.start, 0), t1 = min((int64_t)s.start + s.n, a.tokens);
   const float nan = __builtin_nanf("");
   const int per = a.group * (a.c.dim / 4);
   for (int64_t t = t0; t < t1; ++t)
     for (int i = threadIdx.x; i < per; i += blockDim.x)
-      write_out(a, split, t, kvh * a.group + i / (a.c.dim / 4), i % (a.c.dim / 4) * 4, f32x4{nan, nan, nan, nan}, 0.0f, nan);
+      write_out(a, t, kvh * a.group + i / (a.c.dim / 4), i % (a.c.dim / 4) * 4, f32x4{nan, nan, nan, nan}, 0.0f, nan);
 }
 
 template <int BYTES>
@@ -120,14 +134,21 @@ struct Span {
   __device__ __forceinline__ bool seen(int key, int pos) const { return key >= k_lo && key < k_hi && key <= pos && (!window || key > pos - window); }
 };
 
-// Two values in LDS: zero if no row sees them, otherwise with infinities and NaN taken out. Returns whether there was one.
-__device__ __forceinline__ bool clean_word(uint32_t* w, bool unseen) {
-  uint32_t v = unseen ? 0 : *w;
-  const bool low = (v & 0x7C00u) == 0x7C00u, high = (v & 0x7C000000u) == 0x7C000000u;
-  if (low) v &= 0xFFFF0000u;
-  if (high) v &= 0xFFFFu;
-  *w = v;
-  return low || high;
+// Eight values in LDS: zero if no row sees them, otherwise with infinities and NaN taken out. Returns whether there was one.
+__device__ __forceinline__ bool clean_piece(char* at, bool unseen) {
+  u32x4 v = *(const u32x4*)at;
+  uint32_t odd = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t w = unseen ? 0u : v[i];
+    // a half's exponent bits all set: adding one to the exponent carries into the sign's place
+    const uint32_t low = ((w & 0x7C00u) + 0x400u) >> 15 & 1u, high = (((w >> 16) & 0x7C00u) + 0x400u) >> 15;
+    w &= ~((0u - low) & 0xFFFFu) & ~((0u - high) << 16);
+    odd |= low | high;
+    v[i] = w;
+  }
+  *(u32x4*)at = v;
+  return odd != 0;
 }
 
 // The sum of the infinities and NaN among channels ch .. ch + 3 of the values that a row at position pos sees in tiles that not

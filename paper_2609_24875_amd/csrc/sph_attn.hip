@@ -20,6 +20,7 @@
 namespace {
 
 constexpr int kTile = 32;                 // keys of a wave's step
+constexpr int kEvenBatch = 512;           // sequences that are cut into equal shares
 
 template <int DIM, int BITS>
 struct Lay {
@@ -125,11 +126,22 @@ __device__ __forceinline__ void load_values(Tile<DIM, BITS>& t, const Pages& pg,
   }
 }
 
+// Inclusive sum over the lanes of a wave: within rows of 16 by shifts, then the rows' last lanes to the rows behind.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+  return v;
+}
+
 // What bounds it: HBM reads of the pages. Each wave keeps one tile of keys and values in flight in registers while
 // it works on the one before, and a SIMD holds two to four such waves; the 16 rows that a product has cost the same
 // whether one query head or 16 share the kv head. The page numbers of a tile are loaded two tiles ahead.
 template <int DIM, int BITS, int NB, bool UNI>
-__global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 4 : DIM * NB <= 128 ? 2 : 1)) void k_attn(AttnArgs) {
+__global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 3 : DIM * NB <= 128 ? (BITS == 4 ? 3 : 2) : 1)) void k_attn(AttnArgs) {
   // read where they are used: kept for the whole kernel, the arguments would push the loop's scalars out of their registers
   const AttnArgs& a = *(const AttnArgs*)__builtin_amdgcn_kernarg_segment_ptr();
   typedef Lay<DIM, BITS> L;
@@ -138,27 +150,76 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 4 : DIM * NB <= 128 ? 2
   constexpr int kLds = kWaves * (kVBytes > kRows * kOStride * 4 ? kVBytes : kRows * kOStride * 4);
   __shared__ __attribute__((aligned(16))) char lds[kLds];
   __shared__ float2 ml_s[kWaves][kRows];
+  __shared__ int before[kEvenBatch + 1], sums[kEvenBatch / 64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, g4 = lane >> 4;
-  uint32_t id = blockIdx.x;
-  const int kvh = id % a.c.kv_heads;
-  id /= a.c.kv_heads;
-  const int b = id % a.batch;
-  id /= a.batch;
-  const int tile = id % a.tiles, split = id / a.tiles;
+  const int kvh = blockIdx.x % a.c.kv_heads, share = blockIdx.x / a.c.kv_heads;
+  int b = share, pos_tile = 0, end_tile = 0, per = 0;
+  if (a.shares) {
+    // The tiles of all sequences in a row, cut into equal shares: `before` says where each sequence's begin.
+    const int rounds = (a.batch + kThreads - 1) / kThreads;
+    int mine[kEvenBatch / kThreads] = {};
+#pragma unroll
+    for (int i = 0; i < kEvenBatch / kThreads; ++i) {
+      if (i < rounds) {
+        const int bb = threadIdx.x + i * kThreads;
+        if (bb < a.batch) {
+          Seq s;
+          s.load(a, bb);
+          mine[i] = s.tiles(a.window);
+        }
+        mine[i] = wave_scan(mine[i]);
+        if (lane == 63) sums[i * kWaves + wave] = mine[i];
+      }
+    }
+    if (threadIdx.x == 0) before[0] = 0;
+    __syncthreads();
+    int total = 0;
+#pragma unroll
+    for (int i = 0; i < kEvenBatch / kThreads; ++i) {
+      if (i < rounds) {
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          if (w == wave) before[threadIdx.x + i * kThreads + 1] = total + mine[i];
+          total += sums[i * kWaves + w];
+        }
+      }
+    }
+    total = __builtin_amdgcn_readfirstlane(total);
+    per = max(kWaves, (total + a.shares - 1) / a.shares);
+    pos_tile = share * per;
+    if (pos_tile >= total) return;
+    end_tile = min(total, pos_tile + per);
+    __syncthreads();
+    for (int i = 0; i < rounds; ++i) {
+      const int bb = threadIdx.x + i * kThreads;
+      if (before[bb] <= pos_tile && pos_tile < before[bb + 1]) sums[0] = bb;
+    }
+    __syncthreads();
+    b = __builtin_amdgcn_readfirstlane(sums[0]);
+  }
+  for (;; ++b) {
+  // the share's part of sequence b: its tiles from c_lo on
+  int c_lo = 0, c_hi = (1 << 30) / kTile;
+  bool alone = true;
+  if (a.shares) {
+    const int b_lo = __builtin_amdgcn_readfirstlane(before[b]), b_hi = __builtin_amdgcn_readfirstlane(before[b + 1]);
+    if (b_hi == b_lo) continue;                             // no queries
+    c_lo = pos_tile - b_lo, c_hi = min(end_tile, b_hi) - b_lo;
+    pos_tile = b_lo + c_hi;
+    const int s_lo = b_lo / per, s_hi = (b_hi - 1) / per;
+    alone = s_lo == s_hi;
+    if (c_lo == 0 && kvh == 0 && threadIdx.x == 0) a.where[b] = make_int2(s_lo + b, s_hi - s_lo + 1);
+  }
   Seq s;
   s.load(a, b);
-  if (s.bad) {
-    if (tile == 0) write_bad(a, s, kvh, split);
-    return;
-  }
-  const int rows = s.n * a.group, r0 = tile * kRows;
-  if (r0 >= rows) return;
-  const int nrow = min(kRows, rows - r0);
+  if (s.bad) write_bad(a, s, kvh);
+  if (!s.bad && s.n > 0) {
+  const int nrow = s.n * a.group;
   const int first = s.len - s.n;                            // position of the first new token
-  const int p_lo = first + r0 / a.group, p_hi = first + (r0 + nrow - 1) / a.group;  // positions of the rows
-  const int lo = a.window ? max(0, p_lo - a.window + 1) : 0, hi = p_hi + 1;
-  const int k_lo = max(lo, (lo & ~(kTile - 1)) + split * a.chunk), k_hi = min(hi, (lo & ~(kTile - 1)) + (split + 1) * a.chunk);
+  const int p_lo = first, p_hi = s.len - 1;                 // positions of the rows
+  const int lo = a.window ? max(0, p_lo - a.window + 1) : 0, hi = s.len;
+  const int k_lo = max(lo, (lo & ~(kTile - 1)) + c_lo * kTile), k_hi = min(hi, (lo & ~(kTile - 1)) + c_hi * kTile);
   const Span span = {k_lo, k_hi, p_lo, p_hi, a.window, kTile};
   const int32_t* pages = a.pages + b * a.pages_stride;
   Pages pg;
@@ -175,7 +236,7 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 4 : DIM * NB <= 128 ? 2
     f16x8 q[NB][L::kSteps];
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
-      const int r = r0 + min(16 * n + col, nrow - 1), t = r / a.group, h = kvh * a.group + r % a.group;
+      const int r = min(16 * n + col, nrow - 1), t = r / a.group, h = kvh * a.group + r % a.group;
       pos[n] = first + t;
       const char* qr = a.q + (s.start + t) * a.qt + h * a.qh;
 #pragma unroll
@@ -299,10 +360,10 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 4 : DIM * NB <= 128 ? 2
       if (!whole) {
         // A weight of 0 does not hide an infinity or a NaN in a value that its row does not see: values that no row sees
         // become zeros here, and so do infinities and NaN, which the rows that see them get at the end.
-#pragma unroll 1
-        for (int i = lane; i < kTile * (DIM / 2); i += 64) {
-          const int kk = i / (DIM / 2);
-          odd |= clean_word((uint32_t*)(vs + kk * L::kVStride + i % (DIM / 2) * 4), kt + kk < k_lo || kt + kk >= k_hi || (gone >> kk & 1));
+#pragma unroll 2
+        for (int i = lane; i < kTile * (DIM / 8); i += 64) {
+          const int kk = i / (DIM / 8);
+          odd |= clean_piece(vs + kk * L::kVStride + i % (DIM / 8) * 16, kt + kk < k_lo || kt + kk >= k_hi || (gone >> kk & 1));
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -359,14 +420,20 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 4 : DIM * NB <= 128 ? 2
       ll += f * ml_s[w][row].y;
       acc += f * *(const f32x4*)((float*)lds + (w * kRows + row) * kOStride + ch);
     }
-    const int rr = r0 + row;
-    if (any_odd) acc += odd_values<DIM, BITS>(span, pg, pages, first + rr / a.group, ch);
-    write_out(a, split, s.start + rr / a.group, kvh * a.group + rr % a.group, ch, acc, mm, ll);
+    if (any_odd) acc += odd_values<DIM, BITS>(span, pg, pages, first + row / a.group, ch);
+    if (alone)
+      write_out(a, s.start + row / a.group, kvh * a.group + row % a.group, ch, acc, mm, ll);
+    else
+      write_part(a, share + b, kvh, row, ch, acc, mm, ll);
+  }
+  }
+  if (!a.shares || pos_tile >= end_tile) return;
+  __syncthreads();
   }
 }
 
-// Joins the stretches of a row, 32 channels a workgroup: the stretches' factors first, then each group of eight threads adds every
-// 32nd stretch in order, and the groups' sums are added in order. Stretches without a seen key have l = 0 and hold nothing.
+// Joins the parts of a row, 32 channels a workgroup: the parts' factors first, then each group of eight threads adds every
+// 32nd part in order, and the groups' sums are added in order. A part without a seen key has l = 0.
 constexpr int kMaxSplits = 512, kJoinCh = 32;
 
 __global__ __launch_bounds__(kThreads) void k_attn_join(AttnArgs a) {
@@ -374,14 +441,27 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(AttnArgs a) {
   __shared__ float factor[kMaxSplits];
   __shared__ float2 red[kWaves];
   __shared__ __attribute__((aligned(16))) float sums[kThreads * 4];
-  const int64_t row = blockIdx.x, rows = a.tokens * a.q_heads;
+  uint32_t id = blockIdx.x;
+  const int kvh = id % a.c.kv_heads;
+  id /= a.c.kv_heads;
+  const int row = id % (a.max_q * a.group), b = id / (a.max_q * a.group);
+  Seq s;
+  s.load(a, b);
+  if (s.bad || row >= s.n * a.group) return;
+  // k_attn's parts follow each other, k_attn_wide's are `batch` apart
+  int slot = b, apart = a.batch, parts = a.splits;
+  if (a.shares) {
+    const int2 w = a.where[b];
+    slot = w.x, apart = 1, parts = w.y;
+    if (parts == 1) return;                                  // written already
+  }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float mm = -INFINITY;
   float2 mine[kMaxSplits / kThreads];
 #pragma unroll
   for (int i = 0; i < kMaxSplits / kThreads; ++i) {
-    const int s = threadIdx.x + i * kThreads;
-    mine[i] = s < a.splits ? a.ml[s * rows + row] : make_float2(-INFINITY, 0.0f);
+    const int p = threadIdx.x + i * kThreads;
+    mine[i] = p < parts ? a.ml[part_at(a, slot + p * apart, kvh, row)] : make_float2(-INFINITY, 0.0f);
     mm = fmaxf(mm, mine[i].x);
   }
 #pragma unroll
@@ -394,9 +474,9 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(AttnArgs a) {
   float l = 0.0f;
 #pragma unroll
   for (int i = 0; i < kMaxSplits / kThreads; ++i) {
-    const int s = threadIdx.x + i * kThreads;
+    const int p = threadIdx.x + i * kThreads;
     const float f = mine[i].y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(mine[i].x - ref);
-    if (s < a.splits) factor[s] = f;
+    if (p < parts) factor[p] = f;
     l += f * mine[i].y;
   }
 #pragma unroll
@@ -409,47 +489,67 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(AttnArgs a) {
   const int group = threadIdx.x / kPer, ch = blockIdx.y * kJoinCh + threadIdx.x % kPer * 4;
   f32x4 acc = {};
 #pragma unroll 4
-  for (int s = group; s < a.splits; s += kGroups) {
-    const float f = factor[s];
-    // a part without a seen key is not read: what it holds is not defined
-    if (f != 0.0f) acc += f * *(const f32x4*)(a.part + (s * rows + row) * a.c.dim + ch);
+  for (int p = group; p < parts; p += kGroups) {
+    const float f = factor[p];
+    if (f != 0.0f) acc += f * *(const f32x4*)(a.part + part_at(a, slot + p * apart, kvh, row) * a.c.dim + ch);
   }
   *(f32x4*)(sums + threadIdx.x * 4) = acc;
   __syncthreads();
   if (group) return;
-  for (int g = 1; g < min(kGroups, a.splits); ++g) acc += *(const f32x4*)(sums + (g * kPer + threadIdx.x) * 4);
-  a.splits = 1;
-  write_out(a, 0, row / a.q_heads, (int)(row % a.q_heads), ch, acc, mm, l);
+  for (int g = 1; g < min(kGroups, parts); ++g) acc += *(const f32x4*)(sums + (g * kPer + threadIdx.x) * 4);
+  write_out(a, s.start + row / a.group, kvh * a.group + row % a.group, ch, acc, mm, l);
 }
 
 // ------------------------------------------------------------------ host side
 
 struct Plan {
-  int wide, nb, rows, tiles, splits, chunk;
+  int wide, nb, tiles, splits, chunk, shares;
+  size_t parts;                            // rows of partial sums
   size_t bytes;
 };
 
-constexpr int kWant = 768;
+// k_attn: a workgroup a sequence and kv head where sequences are short (a few tiles a wave; joining would cost as much) or so many
+// that they fill the chip; otherwise as many workgroups as are resident at once, with equal shares of all keys.
+// k_attn_wide: stretches of at least four tiles where the rows alone would leave the chip idle.
+constexpr int kShort = 4;
+constexpr int kCus = 256;
 
-// Workgroups take stretches of at least 128 keys (one tile a wave), and few enough of them that each has work for a while.
-Plan plan_of(const sph_kv_cache* c, int64_t batch, int64_t tokens, int q_heads, int64_t max_q, int64_t max_len, int64_t window) {
+// Workgroups of k_attn on a CU: as many as keep about 64 KiB of pages on their way to it, a tile a wave. More only lengthens the queue
+// that every dependent load waits in: 64 ragged sequences of up to 8192 tokens at 8 bits take 97 us with two workgroups a CU, 113 with
+// three and 110 with one; 16 of 32768 tokens at 4 bits 200, 148 and 144 us with one, two and three.
+int workgroups_per_cu(const sph_kv_cache* c) {
+  const int tile = kTile * 2 * c->head_dim * c->bits / 8;
+  return std::max(1, std::min(3, (64 << 10) / (kWaves * tile)));
+}
+
+Plan plan_of(const sph_kv_cache* c, int64_t batch, int q_heads, int64_t max_q, int64_t max_len, int64_t window) {
   Plan p{};
   const int group = q_heads / c->kv_heads;
-  const int64_t asked = max_q * group;
+  const int64_t rows = max_q * group;
   // two blocks of rows of wider heads do not fit the registers
-  p.nb = asked <= 16 || c->head_dim > 128 ? 1 : 2;
-  p.wide = asked > 16 * p.nb;
-  p.rows = p.wide ? kWideRows : 16 * p.nb;
-  p.tiles = (int)((asked + p.rows - 1) / p.rows);
-  const int64_t tile = p.wide ? sph_attn_wide_tile(c->head_dim) : kTile;
-  const int64_t span = window > 0 ? std::min<int64_t>(max_len, window + p.rows / group + 1 + tile) : max_len;
-  const int64_t units = (int64_t)c->kv_heads * batch * p.tiles, step = p.wide ? 4 * tile : tile * kWaves;
-  const int64_t want = std::min<int64_t>(kMaxSplits, std::max<int64_t>(1, (p.wide ? 512 : kWant) / units));
-  int64_t chunk = (span + want - 1) / want;
-  chunk = std::max<int64_t>(step, (chunk + step - 1) / step * step);
-  p.chunk = (int)chunk;
-  p.splits = (int)std::max<int64_t>(1, (span + chunk - 1) / chunk);
-  if (p.splits > 1) p.bytes = (size_t)p.splits * tokens * q_heads * (c->head_dim + 2) * sizeof(float);
+  p.nb = rows <= 16 || c->head_dim > 128 ? 1 : 2;
+  p.wide = rows > 16 * p.nb;
+  p.splits = 1;
+  int64_t slots = 0;
+  if (!p.wide) {
+    p.tiles = 1;
+    const int64_t span = window > 0 ? std::min<int64_t>(max_len, window + max_q + kTile) : max_len;
+    if (batch <= kEvenBatch && span > kTile * kWaves * kShort && batch * (span / kTile + 2) < (1 << 30)) {
+      p.shares = (int)std::min<int64_t>(kMaxSplits - 1, std::max<int64_t>(1, kCus * workgroups_per_cu(c) / c->kv_heads));
+      p.shares = (int)std::min<int64_t>(p.shares, batch * ((span + kTile * kWaves - 1) / (kTile * kWaves) + 1));
+      slots = p.shares + batch;
+    }
+  } else {
+    p.tiles = (int)((rows + kWideRows - 1) / kWideRows);
+    const int64_t tile = sph_attn_wide_tile(c->head_dim), step = 4 * tile;
+    const int64_t span = window > 0 ? std::min<int64_t>(max_len, window + kWideRows / group + 1 + tile) : max_len;
+    const int64_t want = std::min<int64_t>(kMaxSplits, std::max<int64_t>(1, 512 / (c->kv_heads * batch * p.tiles)));
+    p.chunk = (int)std::max<int64_t>(step, ((span + want - 1) / want + step - 1) / step * step);
+    p.splits = (int)std::max<int64_t>(1, (span + p.chunk - 1) / p.chunk);
+    if (p.splits > 1) slots = p.splits * batch;
+  }
+  p.parts = (size_t)slots * c->kv_heads * rows;
+  if (slots) p.bytes = p.parts * (c->head_dim + 2) * sizeof(float) + (size_t)batch * sizeof(int2);
   return p;
 }
 
@@ -490,7 +590,7 @@ sph_status sph_attention_workspace_bytes(const sph_kv_cache* cache, int64_t batc
                                          int64_t max_q, int64_t max_len, int64_t window, size_t* bytes) {
   if (!bytes) return SPH_ERR_NULL;
   if (const sph_status st = check_sizes(cache, batch, tokens, q_heads, max_q, max_len, window)) return st;
-  *bytes = batch && tokens ? plan_of(cache, batch, tokens, q_heads, max_q, max_len, window).bytes : 0;
+  *bytes = batch && tokens ? plan_of(cache, batch, q_heads, max_q, max_len, window).bytes : 0;
   return SPH_OK;
 }
 
@@ -513,7 +613,7 @@ sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t token
       (uintptr_t)d_lse % 4 || (uintptr_t)d_ws % 256)
     return SPH_ERR_SHAPE;
   if ((tokens > 1 && o_token_stride == 0) || (q_heads > 1 && o_head_stride == 0)) return SPH_ERR_SHAPE;  // rows written twice
-  const Plan p = plan_of(cache, batch, tokens, q_heads, max_q, max_len, window);
+  const Plan p = plan_of(cache, batch, q_heads, max_q, max_len, window);
   if (p.bytes && !d_ws) return SPH_ERR_NULL;
   if (ws_bytes < p.bytes) return SPH_ERR_BUFFER_TOO_SMALL;
   AttnArgs a{};
@@ -523,18 +623,22 @@ sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t token
   a.q_start = d_q_start, a.pages = d_pages, a.pages_stride = pages_stride, a.lens = d_seq_lens, a.lse = d_lse;
   a.tokens = tokens, a.batch = (int)batch, a.q_heads = q_heads, a.group = q_heads / cache->kv_heads;
   a.max_q = (int)max_q, a.max_len = (int)max_len, a.window = (int)std::min<int64_t>(window, INT32_MAX);
-  a.tiles = p.tiles, a.splits = p.splits, a.chunk = p.chunk;
+  a.tiles = p.tiles, a.splits = p.splits, a.chunk = p.chunk, a.shares = p.shares;
   a.scale = scale * kLog2e;
-  a.part = (float*)d_ws;
-  if (p.bytes) a.ml = (float2*)((float*)d_ws + (size_t)p.splits * tokens * q_heads * cache->head_dim);
-  const int64_t grid = (int64_t)cache->kv_heads * p.splits * p.tiles * batch, rows = tokens * q_heads;
-  if (grid >= (1 << 24) || (p.splits > 1 && rows >= (1 << 26))) return SPH_ERR_SHAPE;
+  if (p.bytes) {
+    a.part = (float*)d_ws;
+    a.ml = (float2*)(a.part + p.parts * cache->head_dim);
+    a.where = (int2*)(a.ml + p.parts);
+  }
+  const int64_t heads = cache->kv_heads;
+  const int64_t grid = p.wide ? heads * batch * p.tiles * p.splits : heads * (p.shares ? p.shares : batch), joins = heads * batch * max_q * a.group;
+  if (grid >= (1 << 24) || (p.bytes && joins >= (1 << 24))) return SPH_ERR_SHAPE;
   const int bits = cache->bits, dim = cache->head_dim;
   const void* fn = p.wide ? sph_attn_wide_kernel(bits, dim)
                    : cache->page_size >= 16 ? (p.nb == 1 ? kernel_for<1, true>(bits, dim) : kernel_for<2, true>(bits, dim))
                                           : (p.nb == 1 ? kernel_for<1, false>(bits, dim) : kernel_for<2, false>(bits, dim));
   if (!launch_ok(fn, dim3((unsigned)grid), (hipStream_t)stream, a)) return SPH_ERR_HIP;
-  if (p.splits > 1 && !launch_ok((const void*)k_attn_join, dim3((unsigned)rows, cache->head_dim / kJoinCh), (hipStream_t)stream, a)) return SPH_ERR_HIP;
+  if (p.bytes && !launch_ok((const void*)k_attn_join, dim3((unsigned)joins, dim / kJoinCh), (hipStream_t)stream, a)) return SPH_ERR_HIP;
   return SPH_OK;
 }
 

@@ -89,10 +89,7 @@ __device__ __forceinline__ bool clean_share(char* lds, int kt, int k_lo, int k_h
 #pragma unroll 1
   for (int i = 0; i < W::kPieces; ++i) {
     const int idx = threadIdx.x + kThreads * i, row = idx / W::kPer, piece = idx % W::kPer;
-    uint32_t* w = (uint32_t*)(lds + W::kHalf + W::value_at(row, piece));
-    const bool unseen = kt + row < k_lo || kt + row >= k_hi || (gone >> row & 1);
-#pragma unroll 1
-    for (int j = 0; j < 4; ++j) odd |= clean_word(w + j, unseen);
+    odd |= clean_piece(lds + W::kHalf + W::value_at(row, piece), kt + row < k_lo || kt + row >= k_hi || (gone >> row & 1));
   }
   return odd;
 }
@@ -114,7 +111,7 @@ __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(At
   Seq s;
   s.load(a, b);
   if (s.bad) {
-    if (tile == 0) write_bad(a, s, kvh, split);
+    if (tile == 0 && split == 0) write_bad(a, s, kvh);
     return;
   }
   const int rows = s.n * a.group, r0 = tile * kWideRows;
@@ -253,7 +250,10 @@ __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(At
       const int ch = 32 * i + 8 * j + 4 * h;
       f32x4 acc = {o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]};
       if (any_odd) acc += odd_values<DIM, BITS>(span, pg, pages, pos, ch);
-      write_out(a, split, s.start + t, head, ch, acc, m, l);
+      if (a.splits > 1)
+        write_part(a, split * a.batch + b, kvh, r, ch, acc, m, l);
+      else
+        write_out(a, s.start + t, head, ch, acc, m, l);
     }
 }
 
