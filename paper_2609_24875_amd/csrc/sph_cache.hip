@@ -177,7 +177,9 @@ struct AppendArgs {
   int64_t tokens;
   int rot;
   float sign;
-  uint32_t q_blocks;       // the first blocks rotate queries
+  // The blocks that write the cache, bound by arithmetic when they quantise, are spread evenly among those that rotate queries, which
+  // are bound by memory: block i is the (i kv_share / 2^32)-th of them if that number changes behind it.
+  uint32_t kv_share;       // 0: all blocks write the cache
   uint32_t q_head_blocks;
   RopeArgs q;
 };
@@ -246,23 +248,28 @@ __device__ __forceinline__ void append_unit(const AppendArgs& a, int64_t token, 
     store8((_Float16*)out + ch, x);
   } else {
     constexpr float kTop = BITS == 8 ? 255.0f : 15.0f;
-    float lo = x[0], hi = x[0], big = 0.0f;
+    float lo = x[0], hi = x[0], zero = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       lo = fminf(lo, x[i]);
       hi = fmaxf(hi, x[i]);
-      big = fabsf(x[i]) <= 65504.0f ? big : 1.0f;
+      zero = fmaf(x[i], 0.0f, zero);  // NaN from an infinity or a NaN on
     }
-    lo = quad_min(lo), hi = quad_max(hi), big = quad_max(big);
-    _Float16 off = (_Float16)lo, step = (_Float16)(fmaxf(hi - (float)off, 0.0f) / kTop);
-    if (big != 0.0f) off = __builtin_bit_cast(_Float16, (uint16_t)0x7E00), step = (_Float16)0.0f;
+    lo = quad_min(lo), hi = quad_max(hi);
+    const bool fits = quad_max(zero == 0.0f ? 0.0f : 1.0f) == 0.0f && lo >= -65504.0f && hi <= 65504.0f;
+    _Float16 off = (_Float16)lo;
+    float wide = fmaxf(hi - (float)off, 0.0f) * (1.0f / kTop);
+    // an fp32 number, not a product rounded to fp16 at once: as in turn(), codes do not depend on what the compiler fuses
+    asm("" : "+v"(wide));
+    _Float16 step = (_Float16)wide;
+    if (!fits) off = __builtin_bit_cast(_Float16, (uint16_t)0x7E00), step = (_Float16)0.0f;
     const float o = (float)off, d = (float)step, inv = d > 0.0f ? 1.0f / d : 0.0f;
     uint32_t q[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       // the quotient to its last bit, since fp16 inputs often lie exactly between two levels: one correction by the exact remainder
       const float y = x[i] - o, t = y * inv;
-      q[i] = (uint32_t)fminf(fmaxf(rintf(fmaf(fmaf(-t, d, y), inv, t)), 0.0f), kTop);
+      q[i] = (uint32_t)__builtin_amdgcn_fmed3f(rintf(fmaf(fmaf(-t, d, y), inv, t)), 0.0f, kTop);
     }
     if constexpr (BITS == 8) {
       const uint32_t w0 = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24, w1 = q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24;
@@ -284,45 +291,52 @@ template <typename T, int BITS, bool INTER>
 __global__ __launch_bounds__(kThreads) void k_kv_append(AppendArgs a) {
   int64_t token;
   uint32_t unit;
-  if (blockIdx.x < a.q_blocks) {
-    place(blockIdx.x / a.q_head_blocks, (uint32_t)a.c.dim / 16, token, unit);
-    if (token >= a.tokens) return;
-    rope_unit<T, _Float16, INTER>(a.q, token, (int)unit, (int)(blockIdx.x % a.q_head_blocks) * a.q.hpt);
-    return;
+  uint32_t kv_block = blockIdx.x;
+  if (a.kv_share) {
+    kv_block = __umulhi(blockIdx.x, a.kv_share);
+    if (__umulhi(blockIdx.x + 1, a.kv_share) == kv_block) {
+      const uint32_t q_block = blockIdx.x - kv_block;
+      place(q_block / a.q_head_blocks, (uint32_t)a.c.dim / 16, token, unit);
+      if (token >= a.tokens) return;
+      rope_unit<T, _Float16, INTER>(a.q, token, (int)unit, (int)(q_block % a.q_head_blocks) * a.q.hpt);
+      return;
+    }
   }
-  place(blockIdx.x - a.q_blocks, (uint32_t)(a.c.dim / 8) * 2 * a.c.kv_heads, token, unit);
+  place(kv_block, (uint32_t)(a.c.dim / 8) * 2 * a.c.kv_heads, token, unit);
   if (token >= a.tokens) return;
   append_unit<T, BITS, INTER>(a, token, unit);
 }
 
 // ------------------------------------------------------------------ reading
 
-// One thread reads eight channels of one key or value row.
+// One thread reads eight channels of one key row and of the value row beside it.
 template <int BITS>
 __global__ __launch_bounds__(kThreads) void k_kv_read(CacheView c, int64_t tokens, const int32_t* __restrict__ slots,
                                                       _Float16* __restrict__ ko, _Float16* __restrict__ vo) {
   int64_t token;
   uint32_t unit;
-  const uint32_t per_row = (uint32_t)c.dim / 8, per_kind = per_row * c.kv_heads;
-  place(blockIdx.x, 2 * per_kind, token, unit);
+  const uint32_t per_row = (uint32_t)c.dim / 8;
+  place(blockIdx.x, per_row * c.kv_heads, token, unit);
   if (token >= tokens) return;
-  const bool is_v = unit >= per_kind;
-  unit -= is_v ? per_kind : 0;
   const int head = unit / per_row, ch = 8 * (unit % per_row);
   const int slot = slots[token];
-  f16x8 y = {};
+  f16x8 k = {}, v = {};
   if ((unsigned)slot < (uint64_t)c.n_slots) {
     const int64_t page = slot >> c.page_shift;
     const int in_page = slot & ((1 << c.page_shift) - 1);
-    const char* row = (is_v ? c.v : c.k) + page * c.page_stride + head * c.head_stride + in_page * c.token_stride;
+    const int64_t at = page * c.page_stride + head * c.head_stride + in_page * c.token_stride + ch * BITS / 8;
     if constexpr (BITS == 16) {
-      y = *(const f16x8*)(row + 2 * ch);
+      k = *(const f16x8*)(c.k + at);
+      v = *(const f16x8*)(c.v + at);
     } else {
-      const char* par = (is_v ? c.v_par : c.k_par) + page * c.par_page_stride + head * c.par_head_stride + in_page * c.par_token_stride;
-      y = decode8<BITS>(row + ch * BITS / 8, *(const uint32_t*)(par + ch / 32 * 4));
+      const int64_t par = page * c.par_page_stride + head * c.par_head_stride + in_page * c.par_token_stride + ch / 32 * 4;
+      k = decode8<BITS>(c.k + at, *(const uint32_t*)(c.k_par + par));
+      v = decode8<BITS>(c.v + at, *(const uint32_t*)(c.v_par + par));
     }
   }
-  *(f16x8*)((is_v ? vo : ko) + (token * c.kv_heads + head) * c.dim + ch) = y;
+  const int64_t to = (token * c.kv_heads + head) * c.dim + ch;
+  *(f16x8*)(ko + to) = k;
+  *(f16x8*)(vo + to) = v;
 }
 
 // ------------------------------------------------------------------ host side
@@ -488,6 +502,7 @@ sph_status sph_kv_append(const sph_kv_cache* cache, const sph_rope_desc* rope, s
     inter = rope->flags & SPH_ROPE_INTERLEAVED;
   }
   uint32_t kv_blocks, unit_blocks = 0;
+  uint64_t q_blocks = 0;
   if (!blocks_for(tokens, (int64_t)cache->head_dim / 8 * 2 * cache->kv_heads, &kv_blocks)) return SPH_ERR_SHAPE;
   if (q_heads) {
     RopeArgs& q = a.q;
@@ -498,9 +513,10 @@ sph_status sph_kv_append(const sph_kv_cache* cache, const sph_rope_desc* rope, s
     q.hpt = heads_per_thread(tokens, q_heads, cache->head_dim);
     if (!blocks_for(tokens, cache->head_dim / 16, &unit_blocks)) return SPH_ERR_SHAPE;
     a.q_head_blocks = (uint32_t)((q_heads + q.hpt - 1) / q.hpt);
-    const uint64_t qb = (uint64_t)unit_blocks * a.q_head_blocks;
-    if (qb + kv_blocks >= (1u << 24)) return SPH_ERR_SHAPE;
-    a.q_blocks = (uint32_t)qb;
+    q_blocks = (uint64_t)unit_blocks * a.q_head_blocks;
+    if (q_blocks + kv_blocks >= (1u << 24)) return SPH_ERR_SHAPE;
+    // rounded up: floor(total * share / 2^32) is kv_blocks, since total < 2^32
+    a.kv_share = (uint32_t)((((uint64_t)kv_blocks << 32) + q_blocks + kv_blocks - 1) / (q_blocks + kv_blocks));
   }
   const void* fn = nullptr;
 #define SPH_PICK(B)                                                                                                    \
@@ -510,7 +526,7 @@ sph_status sph_kv_append(const sph_kv_cache* cache, const sph_rope_desc* rope, s
   if (cache->bits == 8) SPH_PICK(8);
   if (cache->bits == 4) SPH_PICK(4);
 #undef SPH_PICK
-  return launch(fn, dim3(a.q_blocks + kv_blocks), (hipStream_t)stream, a);
+  return launch(fn, dim3((uint32_t)q_blocks + kv_blocks), (hipStream_t)stream, a);
 }
 
 sph_status sph_kv_read(const sph_kv_cache* cache, int64_t tokens, const int32_t* d_slots, void* d_k_out, void* d_v_out,
@@ -522,7 +538,7 @@ sph_status sph_kv_read(const sph_kv_cache* cache, int64_t tokens, const int32_t*
   if (!d_slots || !d_k_out || !d_v_out) return SPH_ERR_NULL;
   if ((uintptr_t)d_slots % 4 || (uintptr_t)d_k_out % 16 || (uintptr_t)d_v_out % 16) return SPH_ERR_SHAPE;
   uint32_t blocks;
-  if (!blocks_for(tokens, (int64_t)cache->head_dim / 8 * 2 * cache->kv_heads, &blocks)) return SPH_ERR_SHAPE;
+  if (!blocks_for(tokens, (int64_t)cache->head_dim / 8 * cache->kv_heads, &blocks)) return SPH_ERR_SHAPE;
   const CacheView v = sph_cache_view(cache);
   const void* fn = cache->bits == 16 ? (const void*)k_kv_read<16> : cache->bits == 8 ? (const void*)k_kv_read<8> : (const void*)k_kv_read<4>;
   return launch(fn, dim3(blocks), (hipStream_t)stream, v, tokens, d_slots, (_Float16*)d_k_out, (_Float16*)d_v_out);
