@@ -321,12 +321,14 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 3 : DIM * NB <= 128 ? (
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[n][i] = st[n][i >> 2][i & 3] * a.scale;
         if (!whole) {
-          int at_pos = pos[n];
-          asm volatile("" : "+v"(at_pos));  // keeps the branch: the tests are 60 instructions that few tiles need
+          // (opaque here: a branch stays, and what its tests compare with is not kept in registers around the loop)
+          int at_pos = pos[n], key = kt + 4 * g4;
+          uint32_t lost = (uint32_t)gone >> (4 * g4);
+          asm volatile("" : "+v"(at_pos), "+v"(key), "+v"(lost));
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const int kk = 16 * (i >> 2) + 4 * g4 + (i & 3);
-            x[n][i] = !span.seen(kt + kk, at_pos) ? -INFINITY : (gone >> kk & 1) ? __builtin_nanf("") : x[n][i];
+            const int kk = 16 * (i >> 2) + (i & 3);
+            x[n][i] = !span.seen(key + kk, at_pos) ? -INFINITY : (lost >> kk & 1) ? __builtin_nanf("") : x[n][i];
           }
         }
 #pragma unroll

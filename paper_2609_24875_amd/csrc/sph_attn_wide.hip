@@ -18,18 +18,22 @@ struct Wide {
   static constexpr int kRow = DIM * 2;                       // bytes of a row in LDS
   static constexpr int kHalf = kTile * kRow;                 // keys, then values
   static_assert(kTile * kPer % kThreads == 0, "whole shares");
-  // Where a row's piece lies in its LDS row. Keys: eight lanes read one piece of eight rows at once; values: 16 lanes read two
-  // neighbouring pieces of four rows. Rows of a power of two would share their banks, so their pieces are permuted.
-  __device__ static __forceinline__ int key_at(int row, int piece) {
-    if constexpr (DIM == 64) return row * kRow + ((piece ^ ((row >> 1) & 7)) << 4);
-    if constexpr (DIM == 128 || DIM == 256) return row * kRow + ((piece ^ (row & 15)) << 4);
-    return row * kRow + (piece << 4);
+  // A row's pieces are permuted within it, piece p to place p ^ turn(row), so that lanes that read together find 16 different 16-byte
+  // places of the 256 bytes of banks: for keys, one piece of 16 rows or two neighbouring pieces of eight; for values, four neighbouring
+  // pieces of four rows. kSkip is what a row adds to the place.
+  static constexpr int kSkip = kPer % 16;
+  __device__ static __forceinline__ int key_turn(int row) {
+    if constexpr (kSkip == 0) return (row & 7) << 1 | (row >> 3 & 1);
+    if constexpr (kSkip == 8) return (row >> 1 & 3) << 1 | (row >> 3 & 1);
+    return (row >> 2 & 1) << 1 | (row >> 3 & 1);
   }
-  __device__ static __forceinline__ int value_at(int row, int piece) {
-    if constexpr (DIM == 64) return row * kRow + ((piece ^ (((row >> 1) & 3) << 1)) << 4);
-    if constexpr (DIM == 128 || DIM == 256) return row * kRow + ((piece ^ ((row & 7) << 1)) << 4);
-    return row * kRow + (piece << 4);
+  __device__ static __forceinline__ int value_turn(int row) {
+    if constexpr (kSkip == 0) return (row & 3) << 2;
+    if constexpr (kSkip == 8) return (row >> 1 & 1) << 2;
+    return 0;
   }
+  __device__ static __forceinline__ int key_at(int row, int piece) { return row * kRow + ((piece ^ key_turn(row)) << 4); }
+  __device__ static __forceinline__ int value_at(int row, int piece) { return row * kRow + ((piece ^ value_turn(row)) << 4); }
 };
 
 template <int DIM, int BITS>
@@ -70,6 +74,24 @@ __device__ __forceinline__ void load_share(Share<DIM, BITS>& s, const Pages& pg,
   }
 }
 
+// fp16 pages go to LDS without passing registers: the wave's lanes fill 1 KiB in order, so each takes the piece that belongs there.
+template <int DIM>
+__device__ __forceinline__ void load_direct(char* lds, const Pages& pg, int page, int kt, int wave) {
+  typedef Wide<DIM, 16> W;
+  const int in_page = (kt + ((threadIdx.x & 63) & (W::kTile - 1))) & pg.mask;
+  const int64_t off = page * pg.stride + (uint32_t)(in_page * pg.token);
+#pragma unroll
+  for (int i = 0; i < W::kPieces; ++i) {
+    const int idx = threadIdx.x + kThreads * i, row = idx / W::kPer, piece = idx % W::kPer;
+    const int64_t at = shuffled(off, row);
+    char* to = lds + (kThreads * i + 64 * wave) * 16;
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(pg.k + at + ((piece ^ W::key_turn(row)) << 4)),
+                                     (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(pg.v + at + ((piece ^ W::value_turn(row)) << 4)),
+                                     (__attribute__((address_space(3))) void*)(to + W::kHalf), 16, 0, 0);
+  }
+}
+
 template <int DIM, int BITS>
 __device__ __forceinline__ void store_share(const Share<DIM, BITS>& s, char* lds) {
   typedef Wide<DIM, BITS> W;
@@ -99,7 +121,8 @@ __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(At
   const AttnArgs& a = *(const AttnArgs*)__builtin_amdgcn_kernarg_segment_ptr();
   typedef Wide<DIM, BITS> W;
   constexpr int kTile = W::kTile, kSteps = DIM / 16, kBlocks = DIM / 32, kKeys = kTile / 32;
-  __shared__ __attribute__((aligned(16))) char lds[2][2 * W::kHalf];
+  // two arrays, not one of two: loads on their way into one do not hold up reads of the other
+  __shared__ __attribute__((aligned(16))) char lds_a[2 * W::kHalf], lds_b[2 * W::kHalf];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, h = lane >> 5;
   uint32_t id = blockIdx.x;
@@ -147,52 +170,73 @@ __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(At
     const int e_lo = k_lo >> pg.shift, e_hi = (k_hi - 1) >> pg.shift;
     auto page_of = [&](int kt) { return pages[min(max((kt + (lane & (kTile - 1))) >> pg.shift, e_lo), e_hi)]; };
     Share<DIM, BITS> S;
-    const int k0 = k_lo & ~(kTile - 1);
-    int page = page_of(k0), next = page_of(min(k0 + kTile, k_hi - 1));
+    constexpr bool kDirect = BITS == 16;
+    const int k0 = k_lo & ~(kTile - 1), k_last = (k_hi - 1) & ~(kTile - 1);
+    int page = page_of(k0), next = page_of(min(k0 + kTile, k_last));
     uint64_t gone = __ballot(!pg.there(page));
-    load_share(S, pg, pg.there(page) ? page : 0, k0);
-    store_share(S, lds[0]);
-    if (!span.whole(k0) || gone) odd |= clean_share<DIM, BITS>(lds[0], k0, k_lo, k_hi, gone);
-    uint64_t next_gone = __ballot(!pg.there(next));
-    load_share(S, pg, pg.there(next) ? next : 0, min(k0 + kTile, (k_hi - 1) & ~(kTile - 1)));
+    page = pg.there(page) ? page : 0;
+    if constexpr (kDirect) {
+      load_direct<DIM>(lds_a, pg, page, k0, wave);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    } else {
+      load_share(S, pg, page, k0);
+      store_share(S, lds_a);
+    }
+    if (!span.whole(k0) || gone) odd |= clean_share<DIM, BITS>(lds_a, k0, k_lo, k_hi, gone);
+    if constexpr (!kDirect) load_share(S, pg, pg.there(next) ? next : 0, min(k0 + kTile, k_last));
     __syncthreads();
-    int buf = 0;
-    for (int kt = k0; kt < k_hi; kt += kTile, buf ^= 1) {
-      const char* ks = lds[buf];
-      const char* vs = lds[buf] + W::kHalf;
+    auto tile_at = [&](int kt, const char* ks, char* to) __attribute__((always_inline)) {
+      const char* vs = ks + W::kHalf;
       const bool more = kt + kTile < k_hi;
-      const int nn = min(kt + 2 * kTile, (k_hi - 1) & ~(kTile - 1));
-      next = page_of(nn);
+      const uint64_t now_gone = gone;
+      gone = __ballot(!pg.there(next));
+      page = pg.there(next) ? next : 0;
+      next = page_of(min(kt + 2 * kTile, k_last));
       const bool work = w0 < nrow && kt <= wave_hi && (!a.window || kt + kTile > wave_lo - a.window + 1);
       f32x16 st[kKeys] = {};
       if (work) {
+        // keys are read two steps before their products, in this order
+        f16x8 kf[kSteps][kKeys];
+        auto read = [&](int i) {
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i)
+          for (int u = 0; u < kKeys; ++u) kf[i][u] = *(const f16x8*)(ks + W::key_at(32 * u + col, 2 * i + h));
+        };
+        read(0);
+        read(1);
 #pragma unroll
-          for (int u = 0; u < kKeys; ++u)
-            st[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const f16x8*)(ks + W::key_at(32 * u + col, 2 * i + h)), q[i], st[u], 0, 0, 0);
+        for (int i = 0; i < kSteps; ++i) {
+          if (i + 2 < kSteps) read(i + 2);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int u = 0; u < kKeys; ++u) st[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[i][u], q[i], st[u], 0, 0, 0);
+        }
       }
-      const uint64_t now_gone = gone;
-      if (more) {
-        char* to = lds[buf ^ 1];
-        store_share(S, to);
-        gone = next_gone;
-        if (!span.whole(kt + kTile) || gone) odd |= clean_share<DIM, BITS>(to, kt + kTile, k_lo, k_hi, gone);
-        next_gone = __ballot(!pg.there(next));
-        load_share(S, pg, pg.there(next) ? next : 0, nn);
+      // everyone left the other buffer at the last barrier; behind the products, whose time hides the addresses' arithmetic
+      if constexpr (kDirect) {
+        if (more) load_direct<DIM>(to, pg, page, kt + kTile, wave);
+      }
+      if constexpr (!kDirect) {
+        if (more) {
+          store_share(S, to);
+          load_share(S, pg, pg.there(next) ? next : 0, min(kt + 2 * kTile, k_last));
+        }
       }
       if (work) {
         const bool whole = kt >= k_lo && kt + kTile <= k_hi && kt + kTile - 1 <= wave_lo && (!a.window || kt > wave_hi - a.window) && !now_gone;
         if (!whole) {
-          int at_pos = pos;
-          asm volatile("" : "+v"(at_pos));  // keeps the branch
+          // (opaque here: a branch stays, and what its tests compare with is not kept in registers around the loop)
+          int at_pos = pos, key = kt + 4 * h;
+          asm volatile("" : "+v"(at_pos), "+v"(key));
 #pragma unroll
-          for (int u = 0; u < kKeys; ++u)
+          for (int u = 0; u < kKeys; ++u) {
+            uint32_t lost = (uint32_t)(now_gone >> (32 * u)) >> (4 * h);
+            asm volatile("" : "+v"(lost));
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const int kk = 32 * u + 8 * (i >> 2) + 4 * h + (i & 3);
-              st[u][i] = !span.seen(kt + kk, at_pos) ? -INFINITY : (now_gone >> kk & 1) ? __builtin_nanf("") : st[u][i];
+              const int kk = 8 * (i >> 2) + (i & 3);
+              st[u][i] = !span.seen(key + 32 * u + kk, at_pos) ? -INFINITY : (lost >> kk & 1) ? __builtin_nanf("") : st[u][i];
             }
+          }
         }
         float top = -INFINITY;
 #pragma unroll
@@ -210,34 +254,49 @@ __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(At
 #pragma unroll
           for (int i = 0; i < kBlocks; ++i) o[i] *= keep;
         }
+        // In steps of 16 keys: while a step's products run, the values of the next are read and its weights computed.
+        constexpr int kGroups = 2 * kKeys;
+        f16x8 vt[kGroups][kBlocks], p[kGroups];
+        auto read_values = [&](int g) {
 #pragma unroll
-        for (int u = 0; u < kKeys; ++u)
+          for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            f16x8 p;
+            for (int j = 0; j < 2; ++j) {
+              const int row = 16 * g + 8 * j + 4 * h + ((lane & 15) >> 2), piece = 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+              const s16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                  (__attribute__((address_space(3))) s16x4*)(vs + W::value_at(row, piece) + 8 * (lane & 1)));
+              const f16x4 f = __builtin_bit_cast(f16x4, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float x = __builtin_amdgcn_exp2f(fmaf(st[u][8 * e + i], scale, -base));
-              l += x;
-              p[i] = (_Float16)x;
+              for (int x = 0; x < 4; ++x) vt[g][i][4 * j + x] = f[x];
             }
+        };
+        auto weights = [&](int g) {
 #pragma unroll
-            for (int i = 0; i < kBlocks; ++i) {
-              f16x8 vt;
-#pragma unroll
-              for (int j = 0; j < 2; ++j) {
-                const int row = 32 * u + 16 * e + 8 * j + 4 * h + ((lane & 15) >> 2), piece = 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-                const s16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) s16x4*)(vs + W::value_at(row, piece) + 8 * (lane & 1)));
-                const f16x4 f = __builtin_bit_cast(f16x4, w);
-#pragma unroll
-                for (int x = 0; x < 4; ++x) vt[4 * j + x] = f[x];
-              }
-              o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vt, p, o[i], 0, 0, 0);
-            }
+          for (int i = 0; i < 8; ++i) {
+            const float x = __builtin_amdgcn_exp2f(fmaf(st[g >> 1][8 * (g & 1) + i], scale, -base));
+            l += x;
+            p[g][i] = (_Float16)x;
           }
+        };
+        read_values(0);
+        weights(0);
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+          if (g + 1 < kGroups) read_values(g + 1);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int i = 0; i < kBlocks; ++i) o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vt[g][i], p[g], o[i], 0, 0, 0);
+          if (g + 1 < kGroups) weights(g + 1);
+        }
       }
+      if constexpr (kDirect) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      if (more && (!span.whole(kt + kTile) || gone)) odd |= clean_share<DIM, BITS>(to, kt + kTile, k_lo, k_hi, gone);
       __syncthreads();
+    };
+    for (int kt = k0; kt < k_hi; kt += 2 * kTile) {
+      tile_at(kt, lds_a, lds_b);
+      if (kt + kTile >= k_hi) break;
+      tile_at(kt + kTile, lds_b, lds_a);
     }
     l += __shfl_xor(l, 32);
   }
