@@ -359,7 +359,8 @@ typedef struct {
  * rope, if not NULL, rotates the keys on the way, and the queries d_q -> d_q_out (q_heads rows a token; both
  * NULL and q_heads 0 for none; without rope no queries are taken) in the same launch. d_k, d_v, d_q: device rows of dtype (fp16 or
  * fp32); d_q_out: fp16 rows, may be an fp16 d_q with the same strides. Quantising, per row and 32 channels of the
- * fp32 (rotated) values x: offset = fp16(min x), step = fp16((max x - offset)/(2^bits - 1)) (by the fp32 reciprocal),
+ * fp32 (rotated) values x: offset = fp16(min x), step = fp16((max x - offset)/(2^bits - 1)) (by the fp32 reciprocal; the next smaller number if
+ * offset + (2^bits - 1) step would pass 65504),
  * q = clip(round((x - offset)/step), 0, 2^bits - 1), half to even, 0 for a step of 0; 32 channels with an entry that is not finite (or
  * too large for fp16) all read back as NaN. A slot outside the pool (such as -1 for padding) writes nothing; a position outside the
  * table rotates to NaN. Two tokens of one call must not share a slot. Asynchronous. */

@@ -145,6 +145,11 @@ def _rope_desc(table, device, interleaved: bool, inverse: bool) -> CRope:
                  (ROPE_INTERLEAVED if interleaved else 0) | (ROPE_INVERSE if inverse else 0))
 
 
+def _on_gpu(t):
+    if not t.is_cuda:
+        raise ValueError(f"tensors must be on a GPU, not on {t.device}")
+
+
 def _new(x):
     """A contiguous tensor like x (``empty_like`` takes half of ``empty``'s time)."""
     import torch
@@ -172,6 +177,7 @@ def rope(x, positions, table, interleaved: bool = False, inverse: bool = False, 
     pos = _ints(positions, "positions", dev, n)
     out = _new(x) if out is None else out
     py, yt, yh = _rows(out, "out", dev, (x.dtype,), x.shape)
+    _on_gpu(x)
     st = _library().sph_rope(ctypes.byref(desc), SPH_F16 if x.dtype is torch.float16 else SPH_F32, n, x.shape[1], x.shape[2],
                              px, xt, xh, pos, py, yt, yh, _stream_handle(stream))
     _check(st, "sph_rope")
@@ -280,6 +286,7 @@ def kv_append(cache: KVCache, k, v, slots, positions=None, table=None, interleav
         if q_out is None:
             q_out = torch.empty(shape, dtype=torch.float16, device=dev)
         po, ot, oh = _rows(q_out, "q_out", dev, (torch.float16,), shape)
+    _on_gpu(k)
     st = _library().sph_kv_append(cache._ref, desc, SPH_F16 if dt[0] is torch.float16 else SPH_F32, n, pk, kt, kh, pv, vt, vh, ps,
                                   heads, pq, qt, qh, po, ot, oh, pos, _stream_handle(stream))
     _check(st, "sph_kv_append")
@@ -301,6 +308,7 @@ def kv_read(cache: KVCache, slots, out=None, stream=None):
         for t in out:
             if t.dtype != torch.float16 or t.device != dev or t.shape != shape or not t.is_contiguous():
                 raise ValueError(f"out must be two contiguous fp16 tensors of shape {shape} on {dev}")
+    _on_gpu(slots)
     _check(_library().sph_kv_read(cache._ref, shape[0], ps, k.data_ptr(), v.data_ptr(), _stream_handle(stream)), "sph_kv_read")
     return k, v
 
@@ -366,6 +374,7 @@ def attention(q, cache: KVCache, pages, seq_lens, q_start=None, max_q: int = 1, 
     else:
         po, ot, oh = _rows(out, "out", dev, half, (n, heads, dim))
     lse = torch.empty((n, heads), dtype=torch.float32, device=dev) if return_lse else None
+    _on_gpu(q)
     handle = _stream_handle(stream)
     ws = cache.workspaces.get(handle)
 

@@ -42,16 +42,18 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 
-// The queries of one sequence.
+// The queries of one sequence: tokens start .. end - 1.
 struct Seq {
-  int start, n, len;
+  int start, end, n, len;
   bool bad;
   __device__ __forceinline__ void load(const AttnArgs& a, int b) {
     start = a.q_start ? a.q_start[b] : b;
-    const int end = a.q_start ? a.q_start[b + 1] : b + 1;
-    n = end - start;
+    end = a.q_start ? a.q_start[b + 1] : b + 1;
     len = a.lens[b];
-    bad = len < 0 || len > a.max_len || start < 0 || end > a.tokens || n < 0 || n > a.max_q;
+    // (compared before they are subtracted: the difference of two arbitrary numbers need not fit)
+    bad = len < 0 || len > a.max_len || start < 0 || end < start || end > a.tokens;
+    n = bad ? 0 : end - start;
+    bad |= n > a.max_q;
   }
   // k_attn's tiles of 32 keys, from the first that its rows see on: at least one where there are rows to write
   __device__ __forceinline__ int tiles(int window) const {
@@ -84,7 +86,7 @@ __device__ __forceinline__ void write_part(const AttnArgs& a, int slot, int kvh,
 
 // Every row of a sequence that the device found to be outside its bounds becomes NaN.
 __device__ inline void write_bad(const AttnArgs& a, const Seq& s, int kvh) {
-  const int64_t t0 = max(s.start, 0), t1 = min((int64_t)s.start + s.n, a.tokens);
+  const int64_t t0 = max(s.start, 0), t1 = min((int64_t)s.end, a.tokens);
   const float nan = __builtin_nanf("");
   const int per = a.group * (a.c.dim / 4);
   for (int64_t t = t0; t < t1; ++t)

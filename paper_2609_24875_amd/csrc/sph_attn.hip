@@ -505,7 +505,7 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(AttnArgs a) {
 // ------------------------------------------------------------------ host side
 
 struct Plan {
-  int wide, nb, tiles, splits, chunk, shares;
+  int wide, nb, tiles, splits, chunk, shares, window;
   size_t parts;                            // rows of partial sums
   size_t bytes;
 };
@@ -526,6 +526,9 @@ int workgroups_per_cu(const sph_kv_cache* c) {
 
 Plan plan_of(const sph_kv_cache* c, int64_t batch, int q_heads, int64_t max_q, int64_t max_len, int64_t window) {
   Plan p{};
+  // one that hides nothing is none (and positions minus a window stay inside 32 bits)
+  p.window = window > max_len ? 0 : (int)window;
+  window = p.window;
   const int group = q_heads / c->kv_heads;
   const int64_t rows = max_q * group;
   // two blocks of rows of wider heads do not fit the registers
@@ -624,7 +627,7 @@ sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t token
   a.qt = 2 * q_token_stride, a.qh = 2 * q_head_stride, a.ot = 2 * o_token_stride, a.oh = 2 * o_head_stride;
   a.q_start = d_q_start, a.pages = d_pages, a.pages_stride = pages_stride, a.lens = d_seq_lens, a.lse = d_lse;
   a.tokens = tokens, a.batch = (int)batch, a.q_heads = q_heads, a.group = q_heads / cache->kv_heads;
-  a.max_q = (int)max_q, a.max_len = (int)max_len, a.window = (int)std::min<int64_t>(window, INT32_MAX);
+  a.max_q = (int)max_q, a.max_len = (int)max_len, a.window = p.window;
   a.tiles = p.tiles, a.splits = p.splits, a.chunk = p.chunk, a.shares = p.shares;
   a.scale = scale * kLog2e;
   if (p.bytes) {

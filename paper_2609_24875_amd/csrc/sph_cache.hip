@@ -262,6 +262,8 @@ __device__ __forceinline__ void append_unit(const AppendArgs& a, int64_t token, 
     // an fp32 number, not a product rounded to fp16 at once: as in turn(), codes do not depend on what the compiler fuses
     asm("" : "+v"(wide));
     _Float16 step = (_Float16)wide;
+    // rounded up, the step can carry the last level past fp16's range: then the next smaller one
+    if ((float)off + kTop * (float)step > 65504.0f) step = __builtin_bit_cast(_Float16, (uint16_t)(__builtin_bit_cast(uint16_t, step) - 1));
     if (!fits) off = __builtin_bit_cast(_Float16, (uint16_t)0x7E00), step = (_Float16)0.0f;
     const float o = (float)off, d = (float)step, inv = d > 0.0f ? 1.0f / d : 0.0f;
     uint32_t q[8];

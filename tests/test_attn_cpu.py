@@ -1,0 +1,291 @@
+"""CPU checks of the rotary positions, the paged cache and its attention: refusals of the C ABI and of the
+binding (before any HIP call), the rotary frequencies, and models of the launches' arithmetic: equal shares of
+ragged sequences, and cache blocks spread among query blocks."""
+from __future__ import annotations
+
+import ctypes
+import math
+import os
+import random
+
+import numpy as np
+import pytest
+
+import paper_2609_24875_amd as pkg
+from paper_2609_24875_amd import attn as A
+
+torch = pytest.importorskip("torch")
+
+needs_lib = pytest.mark.skipif(not os.path.exists(pkg.LIB_PATH), reason="libsph.so not built")
+OK, NULL, SHAPE, FORMAT, VALUE, SMALL = 0, 1, 2, 3, 5, 6
+P = 1 << 20                                       # stands for a device pointer; no call here gets as far as using one
+
+
+def _cache(**kw):
+    bits, heads, dim, page = kw.get("bits", 8), kw.get("kv_heads", 2), kw.get("head_dim", 128), kw.get("page_size", 16)
+    row = dim * bits // 8
+    d = dict(bits=bits, kv_heads=heads, head_dim=dim, page_size=page, n_pages=4, d_k=P, d_v=P, page_stride=heads * page * row,
+             head_stride=page * row, token_stride=row, d_k_par=P, d_v_par=P, par_page_stride=heads * page * dim // 8,
+             par_head_stride=page * dim // 8, par_token_stride=dim // 8)
+    d.update(kw)
+    return A.CKVCache(*[d[n] for n, _ in A.CKVCache._fields_])
+
+
+def _rope(**kw):
+    d = dict(d_table=P, max_pos=100, rot_dim=64, flags=0)
+    d.update(kw)
+    return A.CRope(*[d[n] for n, _ in A.CRope._fields_])
+
+
+# ------------------------------------------------------------------ refusals
+
+CACHE_FAULTS = [(dict(bits=5), FORMAT), (dict(bits=32), FORMAT), (dict(head_dim=80, token_stride=80), FORMAT), (dict(d_k=0), NULL),
+                (dict(d_v=None), NULL), (dict(d_k_par=0), NULL), (dict(d_v_par=0), NULL), (dict(page_size=0), SHAPE),
+                (dict(page_size=24), SHAPE), (dict(page_size=1 << 17), SHAPE), (dict(kv_heads=0), SHAPE), (dict(kv_heads=1025), SHAPE),
+                (dict(n_pages=0), SHAPE), (dict(n_pages=1 << 28), SHAPE), (dict(d_k=P + 8), SHAPE), (dict(token_stride=64), SHAPE),
+                (dict(token_stride=136), SHAPE), (dict(page_stride=0), SHAPE), (dict(head_stride=-16), SHAPE),
+                (dict(page_size=65536, token_stride=1 << 16), SHAPE), (dict(d_k_par=P + 2), SHAPE), (dict(par_token_stride=8), SHAPE),
+                (dict(par_page_stride=18), SHAPE)]
+
+
+@needs_lib
+@pytest.mark.parametrize("fault,want", CACHE_FAULTS)
+def test_every_call_refuses_a_wrong_cache(fault, want):
+    lib, c = A._library(), _cache(**fault)
+    r = ctypes.byref(c)
+    assert lib.sph_kv_read(r, 1, P, P, P, None) == want
+    assert lib.sph_kv_append(r, None, 0, 1, P, 256, 128, P, 256, 128, P, 0, None, 0, 0, None, 0, 0, None, None) == want
+    n = ctypes.c_size_t(0)
+    assert lib.sph_attention_workspace_bytes(r, 1, 1, 8, 1, 64, 0, ctypes.byref(n)) == want
+    assert lib.sph_attention(r, 1, 1, 8, P, 1024, 128, None, 1, P, 4, P, 64, 0, 1.0, P, 1024, 128, None, P, 1 << 30, None) == want
+
+
+ROPE_FAULTS = [(dict(), dict(dtype=2), SHAPE), (dict(), dict(tokens=-1), SHAPE), (dict(), dict(tokens=(1 << 26) + 1), SHAPE),
+               (dict(), dict(heads=0), SHAPE), (dict(), dict(dim=72), SHAPE), (dict(), dict(dim=528), SHAPE), (dict(), dict(x=None), NULL),
+               (dict(), dict(y=None), NULL), (dict(), dict(pos=None), NULL), (dict(), dict(x=P + 4), SHAPE), (dict(), dict(xt=1020), SHAPE),
+               (dict(), dict(xh=-128), SHAPE), (dict(), dict(yt=0), SHAPE), (dict(), dict(yh=0), SHAPE), (dict(), dict(pos=P + 2), SHAPE),
+               (dict(d_table=None), {}, NULL), (dict(d_table=P + 4), {}, SHAPE), (dict(max_pos=0), {}, SHAPE), (dict(max_pos=1 << 31), {}, SHAPE),
+               (dict(rot_dim=144), {}, SHAPE), (dict(rot_dim=24), {}, SHAPE), (dict(rot_dim=0), {}, SHAPE), (dict(flags=4), {}, SHAPE)]
+
+
+@needs_lib
+@pytest.mark.parametrize("desc,args,want", ROPE_FAULTS)
+def test_rope_refusals(desc, args, want):
+    a = dict(dtype=0, tokens=2, heads=8, dim=128, x=P, xt=1024, xh=128, pos=P, y=P, yt=1024, yh=128)
+    a.update(args)
+    st = A._library().sph_rope(ctypes.byref(_rope(**desc)), a["dtype"], a["tokens"], a["heads"], a["dim"], a["x"], a["xt"], a["xh"], a["pos"],
+                               a["y"], a["yt"], a["yh"], None)
+    assert st == want
+
+
+@needs_lib
+def test_rope_table_refusals():
+    lib = A._library()
+    f = (ctypes.c_double * 32)(*[0.5] * 32)
+    assert lib.sph_rope_table(64, 10, None, 1.0, P, None) == NULL
+    assert lib.sph_rope_table(64, 10, f, 1.0, None, None) == NULL
+    for rot, n, out in ((0, 10, P), (24, 10, P), (528, 10, P), (64, 0, P), (64, 1 << 31, P), (64, 10, P + 8)):
+        assert lib.sph_rope_table(rot, n, f, 1.0, out, None) == SHAPE
+    assert lib.sph_rope_table(64, 10, f, math.inf, P, None) == VALUE
+    f[31] = math.nan
+    assert lib.sph_rope_table(64, 10, f, 1.0, P, None) == VALUE
+
+
+@needs_lib
+@pytest.mark.parametrize("args,want", [
+    (dict(dtype=3), SHAPE), (dict(tokens=-1), SHAPE), (dict(k=None), NULL), (dict(v=None), NULL), (dict(slots=None), NULL), (dict(pos=None), NULL),
+    (dict(q=None), NULL), (dict(qo=None), NULL), (dict(heads=-1), SHAPE), (dict(rope=None), NULL), (dict(k=P + 2), SHAPE), (dict(vt=100), SHAPE),
+    (dict(qt=100), SHAPE), (dict(qot=0), SHAPE), (dict(qoh=4), SHAPE), (dict(slots=P + 1), SHAPE), (dict(desc=dict(rot_dim=256)), SHAPE),
+    (dict(tokens=0, k=None, v=None, slots=None), OK)])
+def test_append_refusals(args, want):
+    a = dict(dtype=0, tokens=2, k=P, kt=256, kh=128, v=P, vt=256, vh=128, slots=P, heads=8, q=P, qt=1024, qh=128, qo=P, qot=1024, qoh=128,
+             pos=P, rope=True, desc={})
+    a.update(args)
+    st = A._library().sph_kv_append(ctypes.byref(_cache()), ctypes.byref(_rope(**a["desc"])) if a["rope"] else None, a["dtype"], a["tokens"],
+                                    a["k"], a["kt"], a["kh"], a["v"], a["vt"], a["vh"], a["slots"], a["heads"], a["q"], a["qt"], a["qh"],
+                                    a["qo"], a["qot"], a["qoh"], a["pos"], None)
+    assert st == want
+
+
+@needs_lib
+@pytest.mark.parametrize("args,want", [
+    (dict(batch=-1), SHAPE), (dict(batch=70000), SHAPE), (dict(tokens=-1), SHAPE), (dict(heads=0), SHAPE), (dict(heads=7), SHAPE),
+    (dict(max_q=0), SHAPE), (dict(max_len=-1), SHAPE), (dict(max_len=(1 << 30) + 1), SHAPE), (dict(window=-1), SHAPE),
+    (dict(scale=math.nan), VALUE), (dict(scale=math.inf), VALUE), (dict(start=None), SHAPE), (dict(cols=3), SHAPE), (dict(cols=1 << 31), SHAPE),
+    (dict(q=None), NULL), (dict(o=None), NULL), (dict(lens=None), NULL), (dict(pages=None), NULL), (dict(q=P + 8), SHAPE), (dict(qt=1028), SHAPE),
+    (dict(oh=-128), SHAPE), (dict(ot=0), SHAPE), (dict(oh=0), SHAPE), (dict(lens=P + 1), SHAPE), (dict(lse=P + 2), SHAPE), (dict(ws=P + 16), SHAPE),
+    (dict(max_len=4096, cols=256, ws=None), NULL), (dict(max_len=4096, cols=256, nws=64), SMALL), (dict(batch=0, q=None), OK),
+    (dict(tokens=0, lens=None), OK)])
+def test_attention_refusals(args, want):
+    a = dict(batch=2, tokens=4, heads=8, q=P, qt=1024, qh=128, start=P, max_q=2, pages=P, cols=4, lens=P, max_len=64, window=0, scale=0.1, o=P,
+             ot=1024, oh=128, lse=None, ws=P, nws=1 << 30)
+    a.update(args)
+    st = A._library().sph_attention(ctypes.byref(_cache()), a["batch"], a["tokens"], a["heads"], a["q"], a["qt"], a["qh"], a["start"], a["max_q"],
+                                    a["pages"], a["cols"], a["lens"], a["max_len"], a["window"], a["scale"], a["o"], a["ot"], a["oh"], a["lse"],
+                                    a["ws"], a["nws"], None)
+    assert st == want
+
+
+@needs_lib
+def test_attention_workspace():
+    def need(**kw):
+        a = dict(batch=1, tokens=1, heads=8, max_q=1, max_len=64, window=0)
+        a.update(kw)
+        n = ctypes.c_size_t(1)
+        assert A._library().sph_attention_workspace_bytes(ctypes.byref(_cache()), a["batch"], a["tokens"], a["heads"], a["max_q"], a["max_len"],
+                                                          a["window"], ctypes.byref(n)) == OK
+        return n.value
+    assert need() == 0                                          # short: one workgroup a sequence and head
+    assert need(max_len=1 << 20) > 0
+    assert need(max_len=1 << 20, window=64) == 0
+    assert need(batch=513, tokens=513, max_len=1 << 20) == 0     # enough sequences to fill the chip
+    assert need(batch=0, max_len=1 << 20) == 0 and need(tokens=0, max_len=1 << 20) == 0
+    assert need(batch=64, tokens=64 * 512, max_q=512, max_len=1 << 14) == 0   # enough rows
+    assert need(batch=1, tokens=64, max_q=64, max_len=1 << 14) > 0
+    assert A._library().sph_attention_workspace_bytes(ctypes.byref(_cache()), 1, 1, 8, 1, 64, 0, None) == NULL
+
+
+# ------------------------------------------------------------------ the binding
+
+def _cpu_cache(bits=8, **kw):
+    a = dict(n_pages=4, kv_heads=2, head_dim=64, page_size=16, bits=bits, device="cpu")
+    a.update(kw)
+    return pkg.KVCache.empty(**a)
+
+
+def test_cache_checks_its_tensors():
+    c = _cpu_cache()
+    assert (c.n_pages, c.kv_heads, c.page_size, c.head_dim, c.bits) == (4, 2, 16, 64, 8)
+    assert c.nbytes == 2 * 4 * 2 * 16 * (64 + 8)
+    d = c.desc
+    assert (d.page_stride, d.head_stride, d.token_stride) == (2 * 16 * 64, 16 * 64, 64)
+    assert (d.par_page_stride, d.par_head_stride, d.par_token_stride) == (2 * 16 * 8, 16 * 8, 8)
+    assert _cpu_cache(4).head_dim == 64 and _cpu_cache(4).k.shape[3] == 32
+    k16 = torch.zeros(4, 16, 2, 64, dtype=torch.float16).transpose(1, 2)      # token-major pages
+    d = pkg.KVCache(k16, k16.clone(memory_format=torch.preserve_format)).desc
+    assert (d.page_stride, d.head_stride, d.token_stride) == (2 * 16 * 128, 128, 256)
+    one = torch.zeros(1, 1, 1, 64, dtype=torch.float16).as_strided((1, 1, 1, 64), (0, 7, 3, 1))
+    d = pkg.KVCache(one, one).desc                              # strides that are never used
+    assert (d.page_stride, d.head_stride, d.token_stride) == (128, 128, 128)
+    for f in (lambda: pkg.KVCache(c.k, c.v, c.k_par, c.v_par, bits=7), lambda: pkg.KVCache(c.k[..., ::2], c.v, c.k_par, c.v_par, bits=8),
+              lambda: pkg.KVCache(c.k, c.v[:2], c.k_par, c.v_par, bits=8), lambda: pkg.KVCache(c.k, c.v, c.k_par[:, :, :, :1], c.v_par, bits=8),
+              lambda: pkg.KVCache(k16, k16.contiguous()), lambda: pkg.KVCache(k16, k16, c.k_par, None),
+              lambda: pkg.KVCache.empty(2, 2, 80, device="cpu"), lambda: pkg.KVCache.empty(2, 2, 64, bits=2, device="cpu")):
+        with pytest.raises(ValueError):
+            f()
+    for f in (lambda: pkg.KVCache(c.k, c.v, bits=16), lambda: pkg.KVCache(c.k, c.v, bits=8), lambda: pkg.KVCache(k16, None)):
+        with pytest.raises(TypeError):
+            f()
+
+
+@needs_lib
+def test_binding_refusals():
+    c = _cpu_cache(16)
+    x, pos, tab = torch.zeros(3, 4, 64), torch.zeros(3, dtype=torch.int32), torch.zeros(10, 32, 2)
+    h, kv = torch.zeros(3, 4, 64).half(), torch.zeros(3, 2, 64).half()
+    pages, lens = torch.zeros(3, 4, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    wrong_type = (lambda: pkg.rope(x.double(), pos, tab), lambda: pkg.rope(x, pos.long(), tab), lambda: pkg.rope(x, pos, tab.double()),
+                  lambda: pkg.kv_append(c, kv.double(), kv, pos), lambda: pkg.kv_append(c, kv, kv.float(), pos),
+                  lambda: pkg.kv_append(c, kv, kv, pos.long()), lambda: pkg.kv_append(c, kv, kv, pos, positions=pos, table=tab, q=h.float()),
+                  lambda: pkg.kv_read(c, pos.long()), lambda: pkg.attention(x, c, pages, lens), lambda: pkg.attention(h, c, pages.long(), lens),
+                  lambda: pkg.attention(h, c, pages, lens.long()))
+    wrong_value = (lambda: pkg.rope(x[..., ::2], pos, tab), lambda: pkg.rope(x[0], pos, tab), lambda: pkg.rope(x, pos[:2], tab),
+                   lambda: pkg.rope(x, pos, tab[..., :1]), lambda: pkg.rope(x, pos, tab, out=torch.zeros(3, 4, 32)),
+                   lambda: pkg.kv_append(c, kv[:, :1], kv, pos), lambda: pkg.kv_append(c, kv, kv[:2], pos), lambda: pkg.kv_append(c, kv, kv, pos[:2]),
+                   lambda: pkg.kv_append(c, kv, kv, pos, q=h), lambda: pkg.kv_append(c, kv, kv, pos, positions=pos),
+                   lambda: pkg.kv_append(c, kv, kv, pos, positions=pos, table=tab, q=h[:2]),
+                   lambda: pkg.kv_read(c, pos[None]), lambda: pkg.kv_read(c, pos, out=(kv[:2], kv[:2])),
+                   lambda: pkg.attention(h[..., :32], c, pages, lens), lambda: pkg.attention(h, c, pages[0], lens),
+                   lambda: pkg.attention(h, c, pages, lens[:2]), lambda: pkg.attention(h, c, pages, lens, q_start=lens),
+                   lambda: pkg.attention(h, c, pages, lens, max_len=65), lambda: pkg.attention(h, c, pages.t(), lens),
+                   lambda: pkg.attention(h, c, pages[:1].expand(3, 4), lens), lambda: pkg.attention(h, c, pages, lens, out=h[:2]))
+    for f in wrong_type:
+        with pytest.raises(TypeError):
+            f()
+    for f in wrong_value:
+        with pytest.raises(ValueError):
+            f()
+    # what would be right on a GPU does not reach the library from the CPU
+    for f in (lambda: pkg.rope(x, pos, tab), lambda: pkg.kv_append(c, kv, kv, pos, positions=pos, table=tab, q=h), lambda: pkg.kv_read(c, pos),
+              lambda: pkg.attention(h, c, pages, lens)):
+        with pytest.raises(ValueError, match="GPU"):
+            f()
+
+
+# ------------------------------------------------------------------ rotary frequencies
+
+def test_rope_frequencies():
+    f, m = pkg.rope_frequencies(64, base=10000.0)
+    assert m == 1.0 and f[0] == 1.0 and np.allclose(f, [10000.0 ** (-2 * i / 64) for i in range(32)], rtol=1e-14)
+    lin, _ = pkg.rope_frequencies(64, scaling="linear", factor=4.0)
+    assert np.allclose(lin, f / 4, rtol=1e-15)
+    ntk, m = pkg.rope_frequencies(64, scaling="ntk", factor=4.0)
+    assert m == 1.0 and ntk[0] == 1.0 and np.isclose(ntk[-1], f[-1] / 4, rtol=1e-12) and np.all(ntk <= f)
+    yarn, m = pkg.rope_frequencies(64, scaling="yarn", factor=4.0, original_max_pos=4096)
+    assert np.isclose(m, 0.1 * math.log(4.0) + 1.0)
+    turns = 4096 * f / (2 * math.pi)
+    assert np.allclose(yarn[turns > 40], f[turns > 40]) and np.allclose(yarn[turns < 0.7], f[turns < 0.7] / 4)
+    assert np.all(yarn <= f * (1 + 1e-15)) and np.all(yarn >= f / 4 * (1 - 1e-15)) and np.all(np.diff(yarn) < 0)
+    for kw in (dict(scaling="no"), dict(factor=0.5), dict(base=1.0)):
+        with pytest.raises(ValueError):
+            pkg.rope_frequencies(64, **kw)
+    for rot in (0, 24, -16):
+        with pytest.raises(ValueError):
+            pkg.rope_frequencies(rot)
+
+
+# ------------------------------------------------------------------ launch arithmetic
+
+def test_cache_blocks_are_spread_evenly_and_each_runs_once():
+    """Block i of total writes the cache if floor((i + 1) f / 2^32) passes floor(i f / 2^32), f = ceil(kv 2^32 / total)."""
+    rng = random.Random(3)
+    for _ in range(200):
+        kv, q = rng.randint(1, 3000), rng.randint(1, 3000)
+        total = kv + q
+        f = ((kv << 32) + total - 1) // total
+        assert f < 1 << 32
+        at = [(i * f) >> 32 for i in range(total + 1)]
+        kvs = [at[i] for i in range(total) if at[i + 1] != at[i]]
+        qs = [i - at[i] for i in range(total) if at[i + 1] == at[i]]
+        assert kvs == list(range(kv)) and qs == list(range(q))
+    for kv, q in ((1, (1 << 24) - 2), ((1 << 24) - 2, 1), (8388607, 8388608)):
+        total = kv + q
+        f = ((kv << 32) + total - 1) // total
+        assert (total * f) >> 32 == kv and f < 1 << 32
+
+
+def test_equal_shares_cover_every_tile_once():
+    """The shares of k_attn: every sequence's tiles are covered once and in order, and the parts' slots
+    (share + sequence) are distinct, follow each other and stay below shares + batch."""
+    rng = random.Random(4)
+    for _ in range(300):
+        batch, shares = rng.choice([1, 2, 7, 64, 512]), rng.choice([1, 3, 32, 96, 511])
+        tiles = [rng.choice([0, 1, 1, 5, rng.randint(1, 400)]) for _ in range(batch)]
+        before = np.concatenate([[0], np.cumsum(tiles)])
+        total = int(before[-1])
+        if total == 0:
+            continue
+        per = max(4, -(-total // shares))
+        got, slots, where = [[] for _ in range(batch)], [], {}
+        for w in range(shares):
+            pos, end = w * per, min(total, (w + 1) * per)
+            if pos >= total:
+                continue
+            b = int(np.searchsorted(before, pos, side="right")) - 1
+            while pos < end:
+                if before[b + 1] == before[b]:
+                    b += 1
+                    continue
+                lo, hi = pos - before[b], min(end, before[b + 1]) - before[b]
+                got[b] += list(range(lo, hi))
+                s_lo, s_hi = int(before[b]) // per, (int(before[b + 1]) - 1) // per
+                if lo == 0:
+                    where[b] = (s_lo + b, s_hi - s_lo + 1)
+                slots.append((w + b, b))
+                pos = int(before[b] + hi)
+                b += 1
+        assert all(got[b] == list(range(tiles[b])) for b in range(batch))
+        assert len({s for s, _ in slots}) == len(slots) and max(s for s, _ in slots) < shares + batch
+        for b in range(batch):
+            mine = [s for s, x in slots if x == b]
+            assert mine == ([] if not tiles[b] else list(range(where[b][0], where[b][0] + where[b][1])))
