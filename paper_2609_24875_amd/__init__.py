@@ -5,3 +5,4 @@ from .sph import (EXPORTS, FORMATS, LIB_PATH, SphError, SphLibraryMissing, SphWe
                   unpack, workspace_bytes)
 from .attn import (KVCache, attention, attention_workspace_bytes, kv_append, kv_read, rope,  # noqa: F401
                    rope_frequencies, rope_table)
+from .block import AttentionBlock  # noqa: F401
