@@ -137,84 +137,25 @@ __device__ __forceinline__ int wave_scan(int v) {
   return v;
 }
 
+// Tiles c_lo .. c_hi - 1 of sequence b, as seen from the first that its rows see, under one kv head: its rows' outputs, or their part
+// `slot`.
+//
 // What bounds it: HBM reads of the pages. Each wave keeps one tile of keys and values in flight in registers while
 // it works on the one before, and a SIMD holds two to four such waves; the 16 rows that a product has cost the same
 // whether one query head or 16 share the kv head. The page numbers of a tile are loaded two tiles ahead.
 template <int DIM, int BITS, int NB, bool UNI>
-__global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 3 : DIM * NB <= 128 ? (BITS == 4 ? 3 : 2) : 1)) void k_attn(AttnArgs) {
-  // read where they are used: kept for the whole kernel, the arguments would push the loop's scalars out of their registers
-  const AttnArgs& a = *(const AttnArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+__device__ __forceinline__ void attend(const AttnArgs& a, char* lds, float2 (*ml_s)[16 * NB], int kvh, int b, int c_lo, int c_hi, int slot) {
   typedef Lay<DIM, BITS> L;
-  constexpr int kRows = 16 * NB;
-  constexpr int kVBytes = kTile * L::kVStride, kOStride = DIM + 4;
-  constexpr int kLds = kWaves * (kVBytes > kRows * kOStride * 4 ? kVBytes : kRows * kOStride * 4);
-  __shared__ __attribute__((aligned(16))) char lds[kLds];
-  __shared__ float2 ml_s[kWaves][kRows];
-  __shared__ int before[kEvenBatch + 1], sums[kEvenBatch / 64];
+  constexpr int kRows = 16 * NB, kVBytes = kTile * L::kVStride, kOStride = DIM + 4;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, g4 = lane >> 4;
-  const int kvh = blockIdx.x % a.c.kv_heads, share = blockIdx.x / a.c.kv_heads;
-  int b = share, pos_tile = 0, end_tile = 0, per = 0;
-  if (a.shares) {
-    // The tiles of all sequences in a row, cut into equal shares: `before` says where each sequence's begin.
-    const int rounds = (a.batch + kThreads - 1) / kThreads;
-    int mine[kEvenBatch / kThreads] = {};
-#pragma unroll
-    for (int i = 0; i < kEvenBatch / kThreads; ++i) {
-      if (i < rounds) {
-        const int bb = threadIdx.x + i * kThreads;
-        if (bb < a.batch) {
-          Seq s;
-          s.load(a, bb);
-          mine[i] = s.tiles(a.window);
-        }
-        mine[i] = wave_scan(mine[i]);
-        if (lane == 63) sums[i * kWaves + wave] = mine[i];
-      }
-    }
-    if (threadIdx.x == 0) before[0] = 0;
-    __syncthreads();
-    int total = 0;
-#pragma unroll
-    for (int i = 0; i < kEvenBatch / kThreads; ++i) {
-      if (i < rounds) {
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-          if (w == wave) before[threadIdx.x + i * kThreads + 1] = total + mine[i];
-          total += sums[i * kWaves + w];
-        }
-      }
-    }
-    total = __builtin_amdgcn_readfirstlane(total);
-    per = max(kWaves, (total + a.shares - 1) / a.shares);
-    pos_tile = share * per;
-    if (pos_tile >= total) return;
-    end_tile = min(total, pos_tile + per);
-    __syncthreads();
-    for (int i = 0; i < rounds; ++i) {
-      const int bb = threadIdx.x + i * kThreads;
-      if (before[bb] <= pos_tile && pos_tile < before[bb + 1]) sums[0] = bb;
-    }
-    __syncthreads();
-    b = __builtin_amdgcn_readfirstlane(sums[0]);
-  }
-  for (;; ++b) {
-  // the share's part of sequence b: its tiles from c_lo on
-  int c_lo = 0, c_hi = (1 << 30) / kTile;
-  bool alone = true;
-  if (a.shares) {
-    const int b_lo = __builtin_amdgcn_readfirstlane(before[b]), b_hi = __builtin_amdgcn_readfirstlane(before[b + 1]);
-    if (b_hi == b_lo) continue;                             // no queries
-    c_lo = pos_tile - b_lo, c_hi = min(end_tile, b_hi) - b_lo;
-    pos_tile = b_lo + c_hi;
-    const int s_lo = b_lo / per, s_hi = (b_hi - 1) / per;
-    alone = s_lo == s_hi;
-    if (c_lo == 0 && kvh == 0 && threadIdx.x == 0) a.where[b] = make_int2(s_lo + b, s_hi - s_lo + 1);
-  }
   Seq s;
   s.load(a, b);
-  if (s.bad) write_bad(a, s, kvh);
-  if (!s.bad && s.n > 0) {
+  if (s.bad) {
+    write_bad(a, s, kvh);
+    return;
+  }
+  if (s.n == 0) return;
   const int nrow = s.n * a.group;
   const int first = s.len - s.n;                            // position of the first new token
   const int p_lo = first, p_hi = s.len - 1;                 // positions of the rows
@@ -423,30 +364,154 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 3 : DIM * NB <= 128 ? (
       acc += f * *(const f32x4*)((float*)lds + (w * kRows + row) * kOStride + ch);
     }
     if (any_odd) acc += odd_values<DIM, BITS>(span, pg, pages, first + row / a.group, ch);
-    if (alone)
+    if (slot < 0)
       write_out(a, s.start + row / a.group, kvh * a.group + row % a.group, ch, acc, mm, ll);
     else
-      write_part(a, share + b, kvh, row, ch, acc, mm, ll);
-  }
-  }
-  if (!a.shares || pos_tile >= end_tile) return;
-  __syncthreads();
+      write_part(a, slot, kvh, row, ch, acc, mm, ll);
   }
 }
 
-// Joins the parts of a row, 32 channels a workgroup: the parts' factors first, then each group of eight threads adds every
-// 32nd part in order, and the groups' sums are added in order. A part without a seen key has l = 0.
-constexpr int kMaxSplits = 512, kJoinCh = 32;
+// Inclusive sums over all sequences' counts: before[b + 1] = counts of 0 .. b. Returns their total.
+__device__ __forceinline__ int scan_counts(const int* counts, int rounds, int* before, int* sums) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int mine[kEvenBatch / kThreads] = {};
+#pragma unroll
+  for (int i = 0; i < kEvenBatch / kThreads; ++i) {
+    if (i < rounds) {
+      mine[i] = wave_scan(counts[i]);
+      if (lane == 63) sums[i * kWaves + wave] = mine[i];
+    }
+  }
+  if (threadIdx.x == 0) before[0] = 0;
+  __syncthreads();
+  int total = 0;
+#pragma unroll
+  for (int i = 0; i < kEvenBatch / kThreads; ++i) {
+    if (i < rounds) {
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        if (w == wave) before[threadIdx.x + i * kThreads + 1] = total + mine[i];
+        total += sums[i * kWaves + w];
+      }
+    }
+  }
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(total);
+}
 
+// The sequence whose counts hold place `at`.
+__device__ __forceinline__ int find_count(int at, int rounds, const int* before, int* sums) {
+  for (int i = 0; i < rounds; ++i) {
+    const int b = threadIdx.x + i * kThreads;
+    if (before[b] <= at && at < before[b + 1]) sums[0] = b;
+  }
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(sums[0]);
+}
+
+template <int DIM, int BITS, int NB, bool UNI>
+__global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 3 : DIM * NB <= 128 ? (BITS == 4 ? 3 : 2) : 1)) void k_attn(AttnArgs) {
+  // read where they are used: kept for the whole kernel, the arguments would push the loop's scalars out of their registers
+  const AttnArgs& a = *(const AttnArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  constexpr int kRows = 16 * NB, kVBytes = kTile * Lay<DIM, BITS>::kVStride, kOBytes = kRows * (DIM + 4) * 4;
+  __shared__ __attribute__((aligned(16))) char lds[kWaves * (kVBytes > kOBytes ? kVBytes : kOBytes)];
+  __shared__ float2 ml_s[kWaves][kRows];
+  __shared__ int before[kEvenBatch + 1], sums[kEvenBatch / 32];
+  const int kvh = blockIdx.x % a.c.kv_heads, share = blockIdx.x / a.c.kv_heads;
+  int b = share, c_lo = 0, c_hi = (1 << 30) / kTile, slot = -1;
+  int at = 0, end = 0, per = 0;
+  if (a.shares) {
+    const int rounds = (a.batch + kThreads - 1) / kThreads;
+    int tiles[kEvenBatch / kThreads] = {};
+#pragma unroll
+    for (int i = 0; i < kEvenBatch / kThreads; ++i) {
+      const int bb = threadIdx.x + i * kThreads;
+      if (bb < a.batch) {
+        Seq s;
+        s.load(a, bb);
+        tiles[i] = s.tiles(a.window);
+      }
+    }
+    const int total = scan_counts(tiles, rounds, before, sums);
+    if (a.shares >= 2 * a.batch) {
+      // Shares to spare: each is a stretch of one sequence, ceil(tiles / per) stretches a sequence. This many tiles always suffice:
+      per = max(kWaves, (total + a.shares - a.batch - 1) / (a.shares - a.batch));
+      // Where stretches are long, the least of four smaller numbers that does, too.
+      if (total > 16 * a.shares) {
+        constexpr int kTry[4] = {8, 9, 10, 12};              // eighths of the mean
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int each = (int)(((int64_t)total * kTry[t] + 8 * a.shares - 1) / (8 * a.shares));
+          int need = 0;
+#pragma unroll
+          for (int i = 0; i < kEvenBatch / kThreads; ++i) need += (tiles[i] + each - 1) / each;
+          need = wave_scan(need);
+          if ((threadIdx.x & 63) == 63) sums[t * kWaves + (threadIdx.x >> 6)] = need;
+        }
+        static_assert(4 * kWaves <= kEvenBatch / 32, "sums");
+        __syncthreads();
+#pragma unroll
+        for (int t = 3; t >= 0; --t) {
+          int need = 0;
+#pragma unroll
+          for (int w = 0; w < kWaves; ++w) need += sums[t * kWaves + w];
+          if (__builtin_amdgcn_readfirstlane(need) <= a.shares) per = min(per, (int)(((int64_t)total * kTry[t] + 8 * a.shares - 1) / (8 * a.shares)));
+        }
+        __syncthreads();
+      }
+#pragma unroll
+      for (int i = 0; i < kEvenBatch / kThreads; ++i) tiles[i] = (tiles[i] + per - 1) / per;
+      if (share >= scan_counts(tiles, rounds, before, sums)) return;
+      b = find_count(share, rounds, before, sums);
+      const int lo = __builtin_amdgcn_readfirstlane(before[b]), n = __builtin_amdgcn_readfirstlane(before[b + 1]) - lo;
+      Seq s;
+      s.load(a, b);
+      const int64_t all = s.tiles(a.window);
+      c_lo = (int)((share - lo) * all / n), c_hi = (int)((share - lo + 1) * all / n);
+      if (n > 1) slot = share;
+      if (share == lo && kvh == 0 && threadIdx.x == 0) a.where[b] = make_int2(lo, n);
+    } else {
+      // The tiles of all sequences in a row, cut into equal shares, which may hold the end of one sequence and the start of the next.
+      per = max(kWaves, (total + a.shares - 1) / a.shares);
+      at = share * per, end = min(total, at + per);
+      if (at >= total) return;
+      b = find_count(at, rounds, before, sums);
+    }
+  }
+  while (true) {
+    if (at < end) {
+      int lo, hi;
+      while ((lo = __builtin_amdgcn_readfirstlane(before[b])) == (hi = __builtin_amdgcn_readfirstlane(before[b + 1]))) ++b;  // no queries
+      c_lo = at - lo, c_hi = min(end, hi) - lo;
+      at = lo + c_hi;
+      const int s_lo = lo / per, s_hi = (hi - 1) / per;
+      slot = s_lo == s_hi ? -1 : share + b;
+      if (c_lo == 0 && kvh == 0 && threadIdx.x == 0) a.where[b] = make_int2(s_lo + b, s_hi - s_lo + 1);
+    }
+    attend<DIM, BITS, NB, UNI>(a, lds, ml_s, kvh, b, c_lo, c_hi, slot);
+    if (at >= end) return;
+    ++b;
+    __syncthreads();
+  }
+}
+
+constexpr int kMaxSplits = 512, kJoinCh = 32, kFewParts = 8;
+
+// Joins the parts of a row. Where a row may have many, a wave takes 32 channels of it: each group of eight lanes adds every eighth part
+// in order, and the groups' sums are added. Where rows are many and have few parts (FEW), a wave takes a whole row. (One way for
+// both cost: 96 parts of 32 rows 5 us against 11 by whole rows; 2 parts of 32000 rows 14 us against 58 by 32 channels.)
+// A part without a seen key has l = 0.
+template <bool FEW>
 __global__ __launch_bounds__(kThreads) void k_attn_join(AttnArgs a) {
-  constexpr int kPer = kJoinCh / 4, kGroups = kThreads / kPer;
-  __shared__ float factor[kMaxSplits];
-  __shared__ float2 red[kWaves];
-  __shared__ __attribute__((aligned(16))) float sums[kThreads * 4];
-  uint32_t id = blockIdx.x;
+  const int lane = threadIdx.x & 63;
+  const uint32_t per = FEW ? a.c.dim / 4 : kJoinCh / 4, groups = 64 / per, chunks = FEW ? 1 : a.c.dim / kJoinCh, rows = a.max_q * a.group;
+  uint32_t id = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (id >= chunks * a.c.kv_heads * rows * a.batch) return;
+  const uint32_t group = lane / per, ch = id % chunks * kJoinCh + lane % per * 4;
+  id /= chunks;
   const int kvh = id % a.c.kv_heads;
   id /= a.c.kv_heads;
-  const int row = id % (a.max_q * a.group), b = id / (a.max_q * a.group);
+  const int row = id % rows, b = id / rows;
   Seq s;
   s.load(a, b);
   if (s.bad || row >= s.n * a.group) return;
@@ -457,49 +522,36 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(AttnArgs a) {
     slot = w.x, apart = 1, parts = w.y;
     if (parts == 1) return;                                  // written already
   }
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t first = part_at(a, slot, kvh, row), step = part_at(a, slot + apart, kvh, row) - first;
   float mm = -INFINITY;
-  float2 mine[kMaxSplits / kThreads];
-#pragma unroll
-  for (int i = 0; i < kMaxSplits / kThreads; ++i) {
-    const int p = threadIdx.x + i * kThreads;
-    mine[i] = p < parts ? a.ml[part_at(a, slot + p * apart, kvh, row)] : make_float2(-INFINITY, 0.0f);
-    mm = fmaxf(mm, mine[i].x);
-  }
+  for (int p = lane; p < parts; p += 64) mm = fmaxf(mm, a.ml[first + p * step].x);
 #pragma unroll
   for (int d = 32; d; d >>= 1) mm = fmaxf(mm, __shfl_xor(mm, d));
-  if (lane == 0) red[wave].x = mm;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, red[w].x);
   const float ref = mm == -INFINITY ? 0.0f : mm;
-  float l = 0.0f;
-#pragma unroll
-  for (int i = 0; i < kMaxSplits / kThreads; ++i) {
-    const int p = threadIdx.x + i * kThreads;
-    const float f = mine[i].y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(mine[i].x - ref);
-    if (p < parts) factor[p] = f;
-    l += f * mine[i].y;
-  }
-#pragma unroll
-  for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
-  if (lane == 0) red[wave].y = l;
-  __syncthreads();
-  l = red[0].y;
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) l += red[w].y;
-  const int group = threadIdx.x / kPer, ch = blockIdx.y * kJoinCh + threadIdx.x % kPer * 4;
   f32x4 acc = {};
+  float l = 0.0f;
+  if (group < groups) {
 #pragma unroll 4
-  for (int p = group; p < parts; p += kGroups) {
-    const float f = factor[p];
-    if (f != 0.0f) acc += f * *(const f32x4*)(a.part + part_at(a, slot + p * apart, kvh, row) * a.c.dim + ch);
+    for (int p = group; p < parts; p += groups) {
+      const int64_t at = first + p * step;
+      const float2 ml = a.ml[at];
+      const f32x4 part = *(const f32x4*)(a.part + at * a.c.dim + ch);
+      const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+      l += f * ml.y;
+      acc += f * part;
+    }
   }
-  *(f32x4*)(sums + threadIdx.x * 4) = acc;
-  __syncthreads();
-  if (group) return;
-  for (int g = 1; g < min(kGroups, parts); ++g) acc += *(const f32x4*)(sums + (g * kPer + threadIdx.x) * 4);
-  write_out(a, s.start + row / a.group, kvh * a.group + row % a.group, ch, acc, mm, l);
+  // the groups' sums, in order, to the first
+  for (uint32_t g = 1; g < groups; ++g) {
+    const float more = __shfl(l, (int)(g * per + lane % per));
+    l += group ? 0.0f : more;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x = __shfl(acc[i], (int)(g * per + lane % per));
+      acc[i] += group ? 0.0f : x;
+    }
+  }
+  if (group == 0) write_out(a, s.start + row / a.group, kvh * a.group + row % a.group, ch, acc, mm, l);
 }
 
 // ------------------------------------------------------------------ host side
@@ -513,7 +565,6 @@ struct Plan {
 // k_attn: a workgroup a sequence and kv head where sequences are short (a few tiles a wave; joining would cost as much) or so many
 // that they fill the chip; otherwise as many workgroups as are resident at once, with equal shares of all keys.
 // k_attn_wide: stretches of at least four tiles where the rows alone would leave the chip idle.
-constexpr int kShort = 4;
 constexpr int kCus = 256;
 
 // Workgroups of k_attn on a CU: as many as keep about 64 KiB of pages on their way to it, a tile a wave. More only lengthens the queue
@@ -539,7 +590,10 @@ Plan plan_of(const sph_kv_cache* c, int64_t batch, int q_heads, int64_t max_q, i
   if (!p.wide) {
     p.tiles = 1;
     const int64_t span = window > 0 ? std::min<int64_t>(max_len, window + max_q + kTile) : max_len;
-    if (batch <= kEvenBatch && span > kTile * kWaves * kShort && batch * (span / kTile + 2) < (1 << 30)) {
+    // Up to 6 tiles a wave, or 16 where sequences and heads give every CU a workgroup: 517 keys of one sequence 12 us against 9 + 4
+    // for the shares and their join, 64 ragged sequences of up to 2000 keys 33 against 33 + 6; 1000 keys of one 16 against 9 + 4.
+    const int64_t rounds = batch * c->kv_heads >= kCus ? 16 : 6;
+    if (batch <= kEvenBatch && span > kTile * kWaves * rounds && batch * (span / kTile + 2) < (1 << 30)) {
       p.shares = (int)std::min<int64_t>(kMaxSplits - 1, std::max<int64_t>(1, kCus * workgroups_per_cu(c) / c->kv_heads));
       p.shares = (int)std::min<int64_t>(p.shares, batch * ((span + kTile * kWaves - 1) / (kTile * kWaves) + 1));
       slots = p.shares + batch;
@@ -548,7 +602,11 @@ Plan plan_of(const sph_kv_cache* c, int64_t batch, int q_heads, int64_t max_q, i
     p.tiles = (int)((rows + kWideRows - 1) / kWideRows);
     const int64_t tile = sph_attn_wide_tile(c->head_dim), step = 4 * tile;
     const int64_t span = window > 0 ? std::min<int64_t>(max_len, window + kWideRows / group + 1 + tile) : max_len;
-    const int64_t want = std::min<int64_t>(kMaxSplits, std::max<int64_t>(1, 512 / (c->kv_heads * batch * p.tiles)));
+    // None where the rows alone give half the CUs a workgroup: two parts save less than their join costs (900 rows of one prompt 35 us,
+    // in two parts 33 + 17). Otherwise two a CU, and four where sequences are several, since ragged ones leave many with little
+    // to do (8 of up to 8000 tokens, 40 of each new: 67 + 6 us with two, 40 + 7 with four).
+    const int64_t units = c->kv_heads * batch * p.tiles, per_cu = batch > 1 ? 4 : 2;
+    const int64_t want = 2 * units > kCus ? 1 : std::min<int64_t>(kMaxSplits, per_cu * kCus / units);
     p.chunk = (int)std::max<int64_t>(step, ((span + want - 1) / want + step - 1) / step * step);
     p.splits = (int)std::max<int64_t>(1, (span + p.chunk - 1) / p.chunk);
     if (p.splits > 1) slots = p.splits * batch;
@@ -636,14 +694,19 @@ sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t token
     a.where = (int2*)(a.ml + p.parts);
   }
   const int64_t heads = cache->kv_heads;
-  const int64_t grid = p.wide ? heads * batch * p.tiles * p.splits : heads * (p.shares ? p.shares : batch), joins = heads * batch * max_q * a.group;
-  if (grid >= (1 << 24) || (p.bytes && joins >= (1 << 24))) return SPH_ERR_SHAPE;
+  const int64_t grid = p.wide ? heads * batch * p.tiles * p.splits : heads * (p.shares ? p.shares : batch), rows = heads * batch * max_q * a.group;
+  // k_attn_wide's parts are few, and k_attn's where sequences share a workgroup rather than the other way round
+  const bool few = p.wide ? p.splits <= kFewParts : 2 * batch > p.shares && p.shares <= kFewParts * batch;
+  const int64_t joins = few ? rows : rows * (cache->head_dim / kJoinCh);
+  if (grid >= (1 << 24) || (p.bytes && joins >= (1 << 26))) return SPH_ERR_SHAPE;
   const int bits = cache->bits, dim = cache->head_dim;
   const void* fn = p.wide ? sph_attn_wide_kernel(bits, dim)
                    : cache->page_size >= 16 ? (p.nb == 1 ? kernel_for<1, true>(bits, dim) : kernel_for<2, true>(bits, dim))
                                           : (p.nb == 1 ? kernel_for<1, false>(bits, dim) : kernel_for<2, false>(bits, dim));
   if (!launch_ok(fn, dim3((unsigned)grid), (hipStream_t)stream, a)) return SPH_ERR_HIP;
-  if (p.bytes && !launch_ok((const void*)k_attn_join, dim3((unsigned)joins, dim / kJoinCh), (hipStream_t)stream, a)) return SPH_ERR_HIP;
+  if (p.bytes && !launch_ok(few ? (const void*)k_attn_join<true> : (const void*)k_attn_join<false>, dim3((unsigned)((joins + kWaves - 1) / kWaves)),
+                            (hipStream_t)stream, a))
+    return SPH_ERR_HIP;
   return SPH_OK;
 }
 

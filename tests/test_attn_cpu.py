@@ -289,3 +289,28 @@ def test_equal_shares_cover_every_tile_once():
         for b in range(batch):
             mine = [s for s, x in slots if x == b]
             assert mine == ([] if not tiles[b] else list(range(where[b][0], where[b][0] + where[b][1])))
+
+
+def test_spare_shares_cut_each_sequence_evenly():
+    """Where there are at least twice as many shares as sequences, each share is a stretch of one: every tile is covered once, no
+    stretch is longer than the common bound, and the shares suffice."""
+    rng = random.Random(5)
+    for _ in range(300):
+        batch = rng.choice([1, 2, 7, 64, 255])
+        shares = rng.randint(2 * batch, 511) if 2 * batch <= 511 else 511
+        tiles = [rng.choice([0, 1, 1, 5, rng.randint(1, 40000)]) for _ in range(batch)]
+        total = sum(tiles)
+        per = max(4, -(-total // (shares - batch)))
+        counts = [-(-t // per) for t in tiles]
+        before = np.concatenate([[0], np.cumsum(counts)])
+        assert before[-1] <= shares
+        got = [[] for _ in range(batch)]
+        for share in range(int(before[-1])):
+            b = int(np.searchsorted(before, share, side="right")) - 1
+            i, n = share - int(before[b]), counts[b]
+            lo, hi = i * tiles[b] // n, (i + 1) * tiles[b] // n
+            assert 0 < hi - lo <= per
+            got[b].append((lo, hi))
+        for b in range(batch):
+            edges = [0] + [hi for _, hi in got[b]]
+            assert edges[-1] == tiles[b] and [lo for lo, _ in got[b]] == edges[:-1]

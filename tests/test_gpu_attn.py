@@ -609,12 +609,12 @@ def test_streams_have_their_own_workspaces():
 
 def test_a_decode_step_replays_from_a_graph():
     """Append and attention captured once; replayed as lengths and slots move on, with eager work between."""
-    c, other = (_cache(8, 128, 16, 80, 2) for _ in range(2))
+    c, other = (_cache(8, 128, 16, 240, 2) for _ in range(2))
     table = pkg.rope_table(128, 2048)
-    lens0 = [600, 77]
+    lens0 = [1800, 77]
     for x in (c, other):
         _fill(x, 140)
-    pages, _ = _tables(c, [640, 640], 141)
+    pages, _ = _tables(c, [1920, 1920], 141)
     rows = _randn(2, 12, 128, seed=142)
     pos, slots, lens = _i32([0, 0]), _i32([0, 0]), _i32([0, 0])
 
@@ -626,7 +626,7 @@ def test_a_decode_step_replays_from_a_graph():
 
     def step_on(cache):
         q = pkg.kv_append(cache, rows[:, 8:10], rows[:, 10:], slots, positions=pos, table=table, q=rows[:, :8])
-        return pkg.attention(q, cache, pages, lens, max_len=640)
+        return pkg.attention(q, cache, pages, lens, max_len=1920)
 
     place(0)
     side = torch.cuda.Stream()
@@ -642,7 +642,7 @@ def test_a_decode_step_replays_from_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(out, step_on(other))
         torch.cuda.synchronize()
-    fresh = _cache(8, 128, 16, 80, 2)
+    fresh = _cache(8, 128, 16, 240, 2)
     with pytest.raises(RuntimeError, match="capture"):
         with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=side):
-            pkg.attention(rows[:, :8], fresh, pages, lens, max_len=640)
+            pkg.attention(rows[:, :8], fresh, pages, lens, max_len=1920)
