@@ -51,16 +51,14 @@ __device__ __forceinline__ void store8(float* p, const float* y) {
 struct Turn8 {
   float c[8], s[8];
   __device__ __forceinline__ void load(const float* table, int64_t max_pos, int half, int pos, int pair, float sign) {
-    if ((unsigned)pos < (uint64_t)max_pos) {
-      const f32x4* t = (const f32x4*)(table + ((int64_t)pos * half + pair) * 2);
+    // (as a factor: stored on two branches, the angles would not stay in registers)
+    const bool there = (unsigned)pos < (uint64_t)max_pos;
+    const float one = there ? 1.0f : __builtin_nanf(""), turned = sign * one;
+    const f32x4* t = (const f32x4*)(table + ((there ? (int64_t)pos : 0) * half + pair) * 2);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x4 w = t[i];
-        c[2 * i] = w[0], s[2 * i] = sign * w[1], c[2 * i + 1] = w[2], s[2 * i + 1] = sign * w[3];
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) c[i] = s[i] = __builtin_nanf("");
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 w = t[i];
+      c[2 * i] = one * w[0], s[2 * i] = turned * w[1], c[2 * i + 1] = one * w[2], s[2 * i + 1] = turned * w[3];
     }
   }
 };
