@@ -71,11 +71,11 @@ def _compile(sources, out: str, verbose: bool) -> str:
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("hipcc failed:\n" + res.stdout + res.stderr)
-    # The decode and prefill kernels keep everything in registers: a record buffer or an
-    # accumulator put in scratch memory (a spill, or an array the compiler could not promote)
+    # The products', the rotation's, the cache's and the attention's kernels keep everything in registers: a record
+    # buffer or an accumulator put in scratch memory (a spill, or an array the compiler could not promote)
     # halves their speed without any other sign, so the build refuses it.
     bad = {k: v for k, v in kernel_resources(res.stderr).items()
-           if "k_gemm" in k and (v.get("scratch", 0) or v.get("vgpr_spill", 0))}
+           if any(n in k for n in ("k_gemm", "k_rope", "k_kv_", "k_attn")) and (v.get("scratch", 0) or v.get("vgpr_spill", 0))}
     if bad:
         os.remove(tmp)
         raise RuntimeError(f"kernels using scratch memory: {bad}")

@@ -34,7 +34,7 @@ struct AttnArgs {
 // The kernel for more rows a kv head than k_attn takes, and its rows a workgroup and keys a tile.
 const void* sph_attn_wide_kernel(int bits, int dim);
 constexpr int kWideRows = 128;
-static inline int sph_attn_wide_tile(int dim) { return dim <= 128 ? 64 : 32; }
+static inline int sph_attn_wide_tile(int dim) { return dim <= 192 ? 64 : 32; }
 
 namespace {
 

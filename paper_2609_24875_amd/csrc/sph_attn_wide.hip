@@ -11,7 +11,13 @@ namespace {
 
 template <int DIM, int BITS>
 struct Wide {
-  static constexpr int kTile = DIM <= 128 ? 64 : 32;
+  // Keys of a tile: 64 where the scores of so many leave room for the output's registers (4096 tokens of 32 heads of 192 channels: 374 us,
+  // with 32 434).
+  static constexpr int kTile = DIM <= 192 ? 64 : 32;
+  // Codes are loaded a whole tile ahead where they fit the registers, else when the tile before begins: held through the weights'
+  // products, 8-bit codes of 128 and 256 channels spill, and at 64 channels cost the third wave a SIMD (4096 tokens of 32 heads with either:
+  // 4 bits, 64 channels 144 and 131 us, 128 212 and 222, 256 599 and 632; 8 bits, 128 228 and 224).
+  static constexpr bool kAhead = BITS == 4 && DIM > 64;
   static constexpr int kPer = DIM / 8;                       // pieces of eight channels in a row
   static constexpr int kPieces = kTile * kPer / kThreads;    // a thread's share of a tile's keys, and of its values
   static constexpr int kWords = BITS / 4;                    // of a piece as stored
@@ -95,9 +101,12 @@ __device__ __forceinline__ void load_direct(char* lds, const Pages& pg, int page
 template <int DIM, int BITS>
 __device__ __forceinline__ void store_share(const Share<DIM, BITS>& s, char* lds) {
   typedef Wide<DIM, BITS> W;
+  int thread = threadIdx.x;
+  // (opaque: places are computed here, not kept in registers around the loop)
+  if constexpr (!W::kAhead) asm volatile("" : "+v"(thread));
 #pragma unroll
   for (int i = 0; i < W::kPieces; ++i) {
-    const int idx = threadIdx.x + kThreads * i, row = idx / W::kPer, piece = idx % W::kPer;
+    const int idx = thread + kThreads * i, row = idx / W::kPer, piece = idx % W::kPer;
     *(f16x8*)(lds + W::key_at(row, piece)) = decoded<BITS>(s.k[i], s.k_par[i]);
     *(f16x8*)(lds + W::kHalf + W::value_at(row, piece)) = decoded<BITS>(s.v[i], s.v_par[i]);
   }
@@ -183,7 +192,7 @@ __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(At
       store_share(S, lds_a);
     }
     if (!span.whole(k0) || gone) odd |= clean_share<DIM, BITS>(lds_a, k0, k_lo, k_hi, gone);
-    if constexpr (!kDirect) load_share(S, pg, pg.there(next) ? next : 0, min(k0 + kTile, k_last));
+    if constexpr (W::kAhead) load_share(S, pg, pg.there(next) ? next : 0, min(k0 + kTile, k_last));
     __syncthreads();
     auto tile_at = [&](int kt, const char* ks, char* to) __attribute__((always_inline)) {
       const char* vs = ks + W::kHalf;
@@ -192,6 +201,9 @@ __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(At
       gone = __ballot(!pg.there(next));
       page = pg.there(next) ? next : 0;
       next = page_of(min(kt + 2 * kTile, k_last));
+      if constexpr (!kDirect && !W::kAhead) {
+        if (more) load_share(S, pg, page, kt + kTile);
+      }
       const bool work = w0 < nrow && kt <= wave_hi && (!a.window || kt + kTile > wave_lo - a.window + 1);
       f32x16 st[kKeys] = {};
       if (work) {
@@ -218,7 +230,7 @@ __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(At
       if constexpr (!kDirect) {
         if (more) {
           store_share(S, to);
-          load_share(S, pg, pg.there(next) ? next : 0, min(kt + 2 * kTile, k_last));
+          if constexpr (W::kAhead) load_share(S, pg, pg.there(next) ? next : 0, min(kt + 2 * kTile, k_last));
         }
       }
       if (work) {
