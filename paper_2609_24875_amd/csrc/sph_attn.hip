@@ -436,8 +436,8 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 3 : DIM * NB <= 128 ? (
     if (a.shares >= 2 * a.batch) {
       // Shares to spare: each is a stretch of one sequence, ceil(tiles / per) stretches a sequence. This many tiles always suffice:
       per = max(kWaves, (total + a.shares - a.batch - 1) / (a.shares - a.batch));
-      // Where stretches are long, the least of four smaller numbers that does, too.
-      if (total > 16 * a.shares) {
+      // Where that is a wave's step above the mean or more, the least of four smaller numbers that does, too.
+      if ((int64_t)total * a.batch > (int64_t)kWaves * a.shares * (a.shares - a.batch)) {
         constexpr int kTry[4] = {8, 9, 10, 12};              // eighths of the mean
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -590,9 +590,12 @@ Plan plan_of(const sph_kv_cache* c, int64_t batch, int q_heads, int64_t max_q, i
   if (!p.wide) {
     p.tiles = 1;
     const int64_t span = window > 0 ? std::min<int64_t>(max_len, window + max_q + kTile) : max_len;
-    // Up to 6 tiles a wave, or 16 where sequences and heads give every CU a workgroup: 517 keys of one sequence 12 us against 9 + 4
-    // for the shares and their join, 64 ragged sequences of up to 2000 keys 33 against 33 + 6; 1000 keys of one 16 against 9 + 4.
-    const int64_t rounds = batch * c->kv_heads >= kCus ? 16 : 6;
+    // Short: up to 6 tiles of 128 channels a wave, or 16 where sequences and heads give half the CUs a workgroup, since the counting
+    // of shares and their join cost about 8 us and such calls gain little from a few more workgroups. 8 kv heads, fp16, direct against
+    // shares and join: one sequence of 512 keys 9.4 and 12.2 us, 768 11.9 and 11.9, 1024 14.5 and 12.3; 16 ragged ones of up to 1024
+    // 16.0 and 17.6, 2048 24.5 and 23.5; 64 of up to 2048 52.8 and 54.4. 64 channels: one of 1536 12.2 and 11.8; 256: one of 384 14.4 and 15.4.
+    const int64_t steps = (2 * batch * c->kv_heads >= kCus ? 16 : 6) * 128;
+    const int64_t rounds = steps / c->head_dim;
     if (batch <= kEvenBatch && span > kTile * kWaves * rounds && batch * (span / kTile + 2) < (1 << 30)) {
       p.shares = (int)std::min<int64_t>(kMaxSplits - 1, std::max<int64_t>(1, kCus * workgroups_per_cu(c) / c->kv_heads));
       p.shares = (int)std::min<int64_t>(p.shares, batch * ((span + kTile * kWaves - 1) / (kTile * kWaves) + 1));

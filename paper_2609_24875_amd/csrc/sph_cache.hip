@@ -40,23 +40,20 @@ __device__ __forceinline__ void store8(_Float16* p, const float* y) {
   for (int i = 0; i < 8; ++i) o[i] = (_Float16)y[i];
   *(f16x8*)p = o;
 }
-__device__ __forceinline__ void store8(float* p, const float* y) {
-  ((f32x4*)p)[0] = f32x4{y[0], y[1], y[2], y[3]};
-  ((f32x4*)p)[1] = f32x4{y[4], y[5], y[6], y[7]};
-}
 
 // ------------------------------------------------------------------ rotation
 
-// (cos, sin) of eight consecutive pairs of one position; NaN for a position outside the table.
-struct Turn8 {
-  float c[8], s[8];
+// (cos, sin) of N consecutive pairs of one position; NaN for a position outside the table.
+template <int N>
+struct Turn {
+  float c[N], s[N];
   __device__ __forceinline__ void load(const float* table, int64_t max_pos, int half, int pos, int pair, float sign) {
     // (as a factor: stored on two branches, the angles would not stay in registers)
     const bool there = (unsigned)pos < (uint64_t)max_pos;
     const float one = there ? 1.0f : __builtin_nanf(""), turned = sign * one;
     const f32x4* t = (const f32x4*)(table + ((there ? (int64_t)pos : 0) * half + pair) * 2);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < N / 2; ++i) {
       const f32x4 w = t[i];
       c[2 * i] = one * w[0], s[2 * i] = turned * w[1], c[2 * i + 1] = one * w[2], s[2 * i + 1] = turned * w[3];
     }
@@ -86,41 +83,48 @@ struct RopeArgs {
   float sign;
 };
 
-// One thread rotates 16 channels (eight pairs) of hpt heads of a token: the angles are read once for all of
-// them. Channels behind rot_dim are copied. Four heads' loads are in flight together.
+// One thread rotates two runs of 16 bytes of hpt heads of a token (eight pairs of fp16, four of fp32: neighbouring lanes' loads and
+// stores leave no gaps): the angles are read once for all heads. Channels behind rot_dim are copied. Four heads' loads are in
+// flight together.
 template <typename T, typename O, bool INTER>
 __device__ __forceinline__ void rope_unit(const RopeArgs& a, int64_t token, int unit, int h0) {
-  const int half = a.rot / 2, units = a.rot / 16;
-  const bool turns = unit < units;
-  // first channels of the unit's two runs of eight
-  const int ca = turns && !INTER ? 8 * unit : 16 * unit;
-  const int cb = turns && !INTER ? half + 8 * unit : ca + 8;
-  Turn8 w;
-  if (turns) w.load(a.table, a.max_pos, half, a.pos[token], 8 * unit, a.sign);
+  constexpr int N = 16 / sizeof(T);
+  typedef T Run __attribute__((ext_vector_type(N)));
+  typedef O Out __attribute__((ext_vector_type(N)));
+  const int half = a.rot / 2;
+  const bool turns = unit * 2 * N < a.rot;
+  // first channels of the unit's runs
+  const int ca = turns && !INTER ? N * unit : 2 * N * unit;
+  const int cb = turns && !INTER ? half + N * unit : ca + N;
+  Turn<N> w;
+  if (turns) w.load(a.table, a.max_pos, half, a.pos[token], N * unit, a.sign);
   const int h1 = min(h0 + a.hpt, a.heads);
   const char* x = a.x + token * a.xt;
   char* y = a.y + token * a.yt;
   for (int h = h0; h < h1; h += 4) {
-    Row8<T> ra[4], rb[4];
+    Run ra[4], rb[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const char* p = x + min(h + i, h1 - 1) * a.xh;
-      ra[i].load(p + ca * sizeof(T));
-      rb[i].load(p + cb * sizeof(T));
+      ra[i] = *(const Run*)(p + ca * sizeof(T));
+      rb[i] = *(const Run*)(p + cb * sizeof(T));
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      float e[16];
+      float e[2 * N];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) e[j] = ra[i].at(j), e[8 + j] = rb[i].at(j);
+      for (int j = 0; j < N; ++j) e[j] = (float)ra[i][j], e[N + j] = (float)rb[i][j];
       if (turns) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) turn(e[INTER ? 2 * j : j], e[INTER ? 2 * j + 1 : 8 + j], w.c[j], w.s[j]);
+        for (int j = 0; j < N; ++j) turn(e[INTER ? 2 * j : j], e[INTER ? 2 * j + 1 : N + j], w.c[j], w.s[j]);
       }
       if (h + i < h1) {
         O* r = (O*)(y + (h + i) * a.yh);
-        store8(r + ca, e);
-        store8(r + cb, e + 8);
+        Out oa, ob;
+#pragma unroll
+        for (int j = 0; j < N; ++j) oa[j] = (O)e[j], ob[j] = (O)e[N + j];
+        *(Out*)(r + ca) = oa;
+        *(Out*)(r + cb) = ob;
       }
     }
   }
@@ -140,7 +144,7 @@ template <typename T, bool INTER>
 __global__ __launch_bounds__(kThreads) void k_rope(RopeArgs a) {
   int64_t token;
   uint32_t unit;
-  place(blockIdx.x, (uint32_t)a.dim / 16, token, unit);
+  place(blockIdx.x, (uint32_t)a.dim / (32 / sizeof(T)), token, unit);
   if (token >= a.tokens) return;
   rope_unit<T, T, INTER>(a, token, (int)unit, blockIdx.y * a.hpt);
 }
@@ -215,7 +219,7 @@ __device__ __forceinline__ void append_unit(const AppendArgs& a, int64_t token, 
   for (int i = 0; i < 8; ++i) x[i] = r.at(i);
   if (!is_v && a.pos && ch < a.rot) {
     const int half = a.rot / 2;
-    Turn8 w;
+    Turn<8> w;
     if (INTER) {
       // four pairs: the second half of the eight that are loaded is unused and stays inside the row of the table
       const int pair = ch / 2, first = min(pair, half - 8);
@@ -296,7 +300,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(AppendArgs a) {
     kv_block = __umulhi(blockIdx.x, a.kv_share);
     if (__umulhi(blockIdx.x + 1, a.kv_share) == kv_block) {
       const uint32_t q_block = blockIdx.x - kv_block;
-      place(q_block / a.q_head_blocks, (uint32_t)a.c.dim / 16, token, unit);
+      place(q_block / a.q_head_blocks, (uint32_t)a.c.dim / (32 / sizeof(T)), token, unit);
       if (token >= a.tokens) return;
       rope_unit<T, _Float16, INTER>(a.q, token, (int)unit, (int)(q_block % a.q_head_blocks) * a.q.hpt);
       return;
@@ -359,8 +363,8 @@ bool blocks_for(int64_t tokens, int64_t per, uint32_t* blocks) {
 
 // Heads a thread rotates: as many as leave about four waves a SIMD (2^18 threads), four at a time, so that a token's
 // angles are read once for them.
-int heads_per_thread(int64_t tokens, int heads, int dim) {
-  const int64_t threads = tokens * heads * (dim / 16);
+int heads_per_thread(int64_t tokens, int heads, int units) {
+  const int64_t threads = tokens * heads * units;
   const int64_t want = std::max<int64_t>(1, threads >> 18);
   return want < 4 ? (int)want : (int)std::min<int64_t>((want + 3) / 4 * 4, std::min(heads, 16));
 }
@@ -456,10 +460,11 @@ sph_status sph_rope(const sph_rope_desc* rope, sph_dtype dtype, int64_t tokens, 
   a.xt = x_token_stride * size, a.xh = x_head_stride * size, a.yt = y_token_stride * size, a.yh = y_head_stride * size;
   a.pos = d_pos, a.table = rope->d_table, a.max_pos = rope->max_pos;
   a.tokens = tokens, a.heads = heads, a.dim = head_dim, a.rot = rope->rot_dim;
-  a.hpt = heads_per_thread(tokens, heads, head_dim);
+  const int units = head_dim * size / 32;
+  a.hpt = heads_per_thread(tokens, heads, units);
   a.sign = rope->flags & SPH_ROPE_INVERSE ? -1.0f : 1.0f;
   uint32_t blocks;
-  if (!blocks_for(tokens, head_dim / 16, &blocks)) return SPH_ERR_SHAPE;
+  if (!blocks_for(tokens, units, &blocks)) return SPH_ERR_SHAPE;
   const dim3 grid(blocks, (unsigned)((heads + a.hpt - 1) / a.hpt));
   const bool inter = rope->flags & SPH_ROPE_INTERLEAVED;
   const void* fn = dtype == SPH_F16 ? (inter ? (const void*)k_rope<_Float16, true> : (const void*)k_rope<_Float16, false>)
@@ -510,8 +515,9 @@ sph_status sph_kv_append(const sph_kv_cache* cache, const sph_rope_desc* rope, s
     q.xt = q_token_stride * size, q.xh = q_head_stride * size, q.yt = qo_token_stride * 2, q.yh = qo_head_stride * 2;
     q.pos = d_pos, q.table = rope->d_table, q.max_pos = rope->max_pos, q.sign = a.sign;
     q.tokens = tokens, q.heads = q_heads, q.dim = cache->head_dim, q.rot = rope->rot_dim;
-    q.hpt = heads_per_thread(tokens, q_heads, cache->head_dim);
-    if (!blocks_for(tokens, cache->head_dim / 16, &unit_blocks)) return SPH_ERR_SHAPE;
+    const int units = cache->head_dim * size / 32;
+    q.hpt = heads_per_thread(tokens, q_heads, units);
+    if (!blocks_for(tokens, units, &unit_blocks)) return SPH_ERR_SHAPE;
     a.q_head_blocks = (uint32_t)((q_heads + q.hpt - 1) / q.hpt);
     q_blocks = (uint64_t)unit_blocks * a.q_head_blocks;
     if (q_blocks + kv_blocks >= (1u << 24)) return SPH_ERR_SHAPE;
