@@ -160,6 +160,8 @@ def aligned_rows(t):
     """``t`` itself where its rows suit the library (unit channel stride, 16-byte aligned, no broadcast), else a copy: what
     autograd hands a backward pass may be any view."""
     per = 16 // t.element_size()
+    if t.is_contiguous() and t.shape[-1] % per == 0:
+        return t if t.data_ptr() % 16 == 0 else t.clone()
     ok = t.stride(-1) == 1 and t.data_ptr() % 16 == 0 and all(t.stride(d) % per == 0 for d in range(t.dim() - 1) if t.shape[d] > 1)
     return t if ok else t.contiguous()
 
@@ -180,6 +182,22 @@ def rope(x, positions, table, interleaved: bool = False, inverse: bool = False, 
     _on_gpu(x)
     st = _library().sph_rope(ctypes.byref(desc), SPH_F16 if x.dtype is torch.float16 else SPH_F32, n, x.shape[1], x.shape[2],
                              px, xt, xh, pos, py, yt, yh, _stream_handle(stream))
+    _check(st, "sph_rope")
+    return out
+
+
+def rope_gradient(grad, positions, table, interleaved: bool, inverse: bool = False):
+    """The gradient of ``rope``'s rows from that of its result, whose tensors have passed ``rope``'s checks: they are not repeated, since
+    Python on autograd's thread costs several times what it does elsewhere."""
+    grad = aligned_rows(grad)
+    n, heads, dim = grad.shape
+    gt, gh, _ = grad.stride()
+    out = _new(grad)
+    desc = CRope(table.data_ptr(), table.shape[0], 2 * table.shape[1],
+                 (ROPE_INTERLEAVED if interleaved else 0) | (0 if inverse else ROPE_INVERSE))
+    st = _library().sph_rope(ctypes.byref(desc), SPH_F16 if grad.element_size() == 2 else SPH_F32, n, heads, dim, grad.data_ptr(),
+                             gt if n > 1 else 0, gh if heads > 1 else 0, positions.data_ptr(), out.data_ptr(), heads * dim, dim,
+                             _stream_handle())
     _check(st, "sph_rope")
     return out
 

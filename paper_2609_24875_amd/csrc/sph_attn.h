@@ -28,6 +28,7 @@ struct AttnArgs {
   int2* where;
   int64_t tokens;
   int batch, q_heads, group, max_q, max_len, window, tiles, splits, chunk, shares;
+  bool stream;             // k_attn reads values past the caches
   float scale;             // times log2 e
 };
 
@@ -94,17 +95,12 @@ __device__ inline void write_bad(const AttnArgs& a, const Seq& s, int kvh) {
       write_out(a, t, kvh * a.group + i / (a.c.dim / 4), i % (a.c.dim / 4) * 4, f32x4{nan, nan, nan, nan}, 0.0f, nan);
 }
 
-template <int BYTES>
+template <int BYTES, bool STREAM = false>
 __device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
-  if constexpr (BYTES == 16) {
-    const uint4 v = *(const uint4*)p;
-    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-  } else if constexpr (BYTES == 8) {
-    const uint2 v = *(const uint2*)p;
-    w[0] = v.x, w[1] = v.y;
-  } else {
-    w[0] = *(const uint32_t*)p;
-  }
+  typedef uint32_t V __attribute__((ext_vector_type(BYTES / 4)));
+  const V v = STREAM ? __builtin_nontemporal_load((const V*)p) : *(const V*)p;
+#pragma unroll
+  for (int i = 0; i < BYTES / 4; ++i) w[i] = v[i];
 }
 
 // One kv head's pages.

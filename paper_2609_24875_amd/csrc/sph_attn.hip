@@ -79,23 +79,24 @@ struct Rows {
   }
 };
 
-// Words of rows of one half of a tile: of row `row`, which is `lane_row` + a constant, from byte `byte` on.
-template <int BYTES, bool UNI>
+// Words of rows of one half of a tile: of row `row`, which is `lane_row` + a constant, from byte `byte` on. STREAM: not to be kept in caches.
+template <int BYTES, bool UNI, bool STREAM = false>
 __device__ __forceinline__ void load_row(const char* base, const int64_t* off, int token, int half, int lane_row, int row, int byte, uint32_t* w) {
   if constexpr (UNI) {
     const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(base + off[half]), 0, 16 * token, 0x00020000);
+    constexpr int kAux = STREAM ? 2 : 0;
     const int voff = lane_row * token + byte, soff = (row - lane_row) * token;
     if constexpr (BYTES == 16) {
-      const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, voff, soff, 0);
+      const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, voff, soff, kAux);
       w[0] = v[0], w[1] = v[1], w[2] = v[2], w[3] = v[3];
     } else if constexpr (BYTES == 8) {
-      const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(r, voff, soff, 0);
+      const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(r, voff, soff, kAux);
       w[0] = v[0], w[1] = v[1];
     } else {
-      w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, voff, soff, 0);
+      w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, voff, soff, kAux);
     }
   } else {
-    load_words<BYTES>(base + Rows<false>::shuffled(off[0], 16 * half + row) + byte, w);
+    load_words<BYTES, STREAM>(base + Rows<false>::shuffled(off[0], 16 * half + row) + byte, w);
   }
 }
 
@@ -113,14 +114,15 @@ __device__ __forceinline__ void load_keys(Tile<DIM, BITS>& t, const Pages& pg, c
     }
 }
 
-template <int DIM, int BITS, bool UNI>
+// A load of values takes whole lines, which nobody reads again in this call; the keys' take halves of lines.
+template <int DIM, int BITS, bool UNI, bool STREAM>
 __device__ __forceinline__ void load_values(Tile<DIM, BITS>& t, const Pages& pg, const Rows<UNI>& rows, int lane) {
   typedef Lay<DIM, BITS> L;
 #pragma unroll
   for (int i = 0; i < 2 * L::kVLoads; ++i) {
     const int half = i / L::kVLoads, row = L::v_row(lane, i % L::kVLoads), piece = L::v_piece(lane, i % L::kVLoads);
     const int lane_row = 64 % L::kVPer ? row : lane / L::kVPer;
-    load_row<L::kVPiece, UNI>(pg.v, rows.off, pg.token, half, lane_row, row, piece * L::kVPiece, t.v[i]);
+    load_row<L::kVPiece, UNI, STREAM>(pg.v, rows.off, pg.token, half, lane_row, row, piece * L::kVPiece, t.v[i]);
     if constexpr (BITS < 16)
       load_row<4, UNI>(pg.v_par, rows.par_off, pg.par_token, half, lane_row, row, piece * L::kVCh / 32 * 4, &t.v_par[i]);
   }
@@ -140,9 +142,12 @@ __device__ __forceinline__ int wave_scan(int v) {
 // Tiles c_lo .. c_hi - 1 of sequence b, as seen from the first that its rows see, under one kv head: its rows' outputs, or their part
 // `slot`.
 //
-// What bounds it: HBM reads of the pages. Each wave keeps one tile of keys and values in flight in registers while
-// it works on the one before, and a SIMD holds two to four such waves; the 16 rows that a product has cost the same
+// What bounds it: HBM reads of the pages, for short sequences the latency of the steps of a wave one after the other. Each wave keeps one
+// tile of keys and values in flight in registers while it works on the one before; the 16 rows that a product has cost the same
 // whether one query head or 16 share the kv head. The page numbers of a tile are loaded two tiles ahead.
+// 32 query heads over 8 kv heads of 128 channels: one sequence of 131072 tokens in fp16 87 us (6.2 TB/s), 64 of up to 8192 at 8 bits
+// 78 us (5.2 TB/s), 16 of 32768 under 40 query heads at 4 bits 124 us (5.4 TB/s: the vector ALU, which decodes, is 54% busy beside the reads); one
+// of 517 tokens 11.3 us (512 tokens 9.4, one 5.8).
 template <int DIM, int BITS, int NB, bool UNI>
 __device__ __forceinline__ void attend(const AttnArgs& a, char* lds, float2 (*ml_s)[16 * NB], int kvh, int b, int c_lo, int c_hi, int slot) {
   typedef Lay<DIM, BITS> L;
@@ -199,7 +204,13 @@ __device__ __forceinline__ void attend(const AttnArgs& a, char* lds, float2 (*ml
     Rows<UNI> at;
     at.set(pg, page, kt, lane, BITS < 16);
     load_keys<DIM, BITS, UNI>(T, pg, at, lane);
-    load_values<DIM, BITS, UNI>(T, pg, at, lane);
+    auto load_v = [&]() {
+      if (a.stream)
+        load_values<DIM, BITS, UNI, true>(T, pg, at, lane);
+      else
+        load_values<DIM, BITS, UNI, false>(T, pg, at, lane);
+    };
+    load_v();
     while (true) {
       const bool last = kt + kTile * kWaves >= k_hi;
       // every row sees the whole tile
@@ -247,7 +258,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, char* lds, float2 (*ml
         for (int j = 0; j < L::kVCh / 8; ++j) *(f16x8*)(vs + kk * L::kVStride + (piece * L::kVCh + 8 * j) * 2) = v[j];
       }
       __builtin_amdgcn_sched_barrier(0);
-      load_values<DIM, BITS, UNI>(T, pg, at, lane);
+      load_v();
       __builtin_amdgcn_sched_barrier(0);
       const int nnt = nt + kTile * kWaves < k_hi ? nt + kTile * kWaves : nt;
       next = page_of(nnt);
@@ -567,9 +578,13 @@ struct Plan {
 // k_attn_wide: stretches of at least four tiles where the rows alone would leave the chip idle.
 constexpr int kCus = 256;
 
-// Workgroups of k_attn on a CU: as many as keep about 64 KiB of pages on their way to it, a tile a wave. More only lengthens the queue
-// that every dependent load waits in: 64 ragged sequences of up to 8192 tokens at 8 bits take 97 us with two workgroups a CU, 113 with
-// three and 110 with one; 16 of 32768 tokens at 4 bits 200, 148 and 144 us with one, two and three.
+// Pools that the last cache before memory cannot hold are read past it (values: see load_values). One sequence of 131072 tokens in fp16 86 us
+// instead of 95, 64 of up to 8192 at 8 bits 78 instead of 82; a pool of 41 MB that stays in that cache from call to call 26 instead of 24.
+constexpr int64_t kLastCache = 256 << 20;
+
+// Workgroups of k_attn on a CU: as many as keep about 64 KiB of pages on their way to it, a tile a wave. More lengthen the queue that every
+// dependent load waits in, or wait for registers: 64 ragged sequences of up to 8192 tokens at 8 bits take 98, 78 and 95 us with one, two and three
+// workgroups a CU; 16 of 32768 tokens at 4 bits 195, 135 and 123; one of 131072 tokens in fp16 86, 88 and 90, and its join 4.7, 5.9 and 6.9.
 int workgroups_per_cu(const sph_kv_cache* c) {
   const int tile = kTile * 2 * c->head_dim * c->bits / 8;
   return std::max(1, std::min(3, (64 << 10) / (kWaves * tile)));
@@ -682,6 +697,7 @@ sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t token
   const Plan p = plan_of(cache, batch, q_heads, max_q, max_len, window);
   if (p.bytes && !d_ws) return SPH_ERR_NULL;
   if (ws_bytes < p.bytes) return SPH_ERR_BUFFER_TOO_SMALL;
+  const int bits = cache->bits, dim = cache->head_dim;
   AttnArgs a{};
   a.c = sph_cache_view(cache);
   a.q = (const char*)d_q, a.o = (char*)d_o;
@@ -691,6 +707,7 @@ sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t token
   a.max_q = (int)max_q, a.max_len = (int)max_len, a.window = p.window;
   a.tiles = p.tiles, a.splits = p.splits, a.chunk = p.chunk, a.shares = p.shares;
   a.scale = scale * kLog2e;
+  a.stream = cache->n_pages * cache->page_size * cache->kv_heads * (int64_t)dim * bits / 4 > kLastCache;
   if (p.bytes) {
     a.part = (float*)d_ws;
     a.ml = (float2*)(a.part + p.parts * cache->head_dim);
@@ -702,7 +719,6 @@ sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t token
   const bool few = p.wide ? p.splits <= kFewParts : 2 * batch > p.shares && p.shares <= kFewParts * batch;
   const int64_t joins = few ? rows : rows * (cache->head_dim / kJoinCh);
   if (grid >= (1 << 24) || (p.bytes && joins >= (1 << 26))) return SPH_ERR_SHAPE;
-  const int bits = cache->bits, dim = cache->head_dim;
   const void* fn = p.wide ? sph_attn_wide_kernel(bits, dim)
                    : cache->page_size >= 16 ? (p.nb == 1 ? kernel_for<1, true>(bits, dim) : kernel_for<2, true>(bits, dim))
                                           : (p.nb == 1 ? kernel_for<1, false>(bits, dim) : kernel_for<2, false>(bits, dim));

@@ -125,6 +125,10 @@ __device__ __forceinline__ bool clean_share(char* lds, int kt, int k_lo, int k_h
   return odd;
 }
 
+// What bounds it: matrix products and exponentials together, on two waves a SIMD (one above 128 channels). 2048 new tokens behind 14336
+// others, 32 query heads over 8 kv heads of 128 channels, fp16: 596 us, 865 TFLOP/s at a clock that the products lower to about 2.0 GHz; MFMA
+// 40%, vector ALU 42%, LDS 25% busy, no bank conflicts. Twice the rows a wave halve its LDS reads, but leave one wave a SIMD, which
+// does not overlap its products with its weights well enough: 920 us. 4096 tokens over themselves at 8 bits 226 us, 4 bits 214, fp16 197.
 template <int DIM, int BITS>
 __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(AttnArgs) {
   const AttnArgs& a = *(const AttnArgs*)__builtin_amdgcn_kernarg_segment_ptr();

@@ -83,21 +83,41 @@ struct RopeArgs {
   float sign;
 };
 
-// One thread rotates two runs of 16 bytes of hpt heads of a token (eight pairs of fp16, four of fp32: neighbouring lanes' loads and
-// stores leave no gaps): the angles are read once for all heads. Channels behind rot_dim are copied. Four heads' loads are in
-// flight together.
-template <typename T, typename O, bool INTER>
+// One thread rotates two runs of 16 bytes of hpt heads of a token (eight pairs of fp16, four of fp32), each run beside its neighbouring
+// lanes': loads and stores leave no gaps. The angles are read once for all heads. Channels behind rot_dim are copied. Four heads' loads
+// are in flight together, past the caches, since each row is read once. STREAM: stores go past them, too, which is faster beside
+// stores of the cache's pages (8192 tokens into 4 bits and back 58.5 us, otherwise 61.5; loads that stay in the caches 62) and
+// slower alone (8192 tokens 41 us, otherwise 35.5; loads that stay 45).
+template <typename T, typename O, bool INTER, bool STREAM>
 __device__ __forceinline__ void rope_unit(const RopeArgs& a, int64_t token, int unit, int h0) {
   constexpr int N = 16 / sizeof(T);
   typedef T Run __attribute__((ext_vector_type(N)));
   typedef O Out __attribute__((ext_vector_type(N)));
-  const int half = a.rot / 2;
-  const bool turns = unit * 2 * N < a.rot;
-  // first channels of the unit's runs
-  const int ca = turns && !INTER ? N * unit : 2 * N * unit;
-  const int cb = turns && !INTER ? half + N * unit : ca + N;
+  const int half = a.rot / 2, ch = N * unit;
+  // first channels of the runs: of both elements of the pairs, or of the head's halves where pairs are neighbours
+  int ca = ch, cb = a.dim / 2 + ch;
+  if (!INTER) {
+    const bool turns = ch < half;
+    ca = turns ? ch : half + ch;                             // rot + (ch - half)
+    cb = turns ? half + ch : a.dim / 2 + ch;                 // rot + (dim - rot) / 2 + (ch - half)
+  }
+  const bool turns_a = ca < a.rot, turns_b = cb < a.rot;
   Turn<N> w;
-  if (turns) w.load(a.table, a.max_pos, half, a.pos[token], N * unit, a.sign);
+  if constexpr (INTER) {
+    Turn<N / 2> u;
+    if (turns_a) {
+      u.load(a.table, a.max_pos, half, a.pos[token], ca / 2, a.sign);
+#pragma unroll
+      for (int j = 0; j < N / 2; ++j) w.c[j] = u.c[j], w.s[j] = u.s[j];
+    }
+    if (turns_b) {
+      u.load(a.table, a.max_pos, half, a.pos[token], cb / 2, a.sign);
+#pragma unroll
+      for (int j = 0; j < N / 2; ++j) w.c[N / 2 + j] = u.c[j], w.s[N / 2 + j] = u.s[j];
+    }
+  } else {
+    if (turns_a) w.load(a.table, a.max_pos, half, a.pos[token], ca, a.sign);
+  }
   const int h1 = min(h0 + a.hpt, a.heads);
   const char* x = a.x + token * a.xt;
   char* y = a.y + token * a.yt;
@@ -106,25 +126,37 @@ __device__ __forceinline__ void rope_unit(const RopeArgs& a, int64_t token, int 
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const char* p = x + min(h + i, h1 - 1) * a.xh;
-      ra[i] = *(const Run*)(p + ca * sizeof(T));
-      rb[i] = *(const Run*)(p + cb * sizeof(T));
+      ra[i] = __builtin_nontemporal_load((const Run*)(p + ca * sizeof(T)));
+      rb[i] = __builtin_nontemporal_load((const Run*)(p + cb * sizeof(T)));
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float e[2 * N];
 #pragma unroll
       for (int j = 0; j < N; ++j) e[j] = (float)ra[i][j], e[N + j] = (float)rb[i][j];
-      if (turns) {
+      if (INTER) {
+        if (turns_a)
 #pragma unroll
-        for (int j = 0; j < N; ++j) turn(e[INTER ? 2 * j : j], e[INTER ? 2 * j + 1 : N + j], w.c[j], w.s[j]);
+          for (int j = 0; j < N / 2; ++j) turn(e[2 * j], e[2 * j + 1], w.c[j], w.s[j]);
+        if (turns_b)
+#pragma unroll
+          for (int j = N / 2; j < N; ++j) turn(e[2 * j], e[2 * j + 1], w.c[j], w.s[j]);
+      } else if (turns_a) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) turn(e[j], e[N + j], w.c[j], w.s[j]);
       }
       if (h + i < h1) {
         O* r = (O*)(y + (h + i) * a.yh);
         Out oa, ob;
 #pragma unroll
         for (int j = 0; j < N; ++j) oa[j] = (O)e[j], ob[j] = (O)e[N + j];
-        *(Out*)(r + ca) = oa;
-        *(Out*)(r + cb) = ob;
+        if constexpr (STREAM) {
+          __builtin_nontemporal_store(oa, (Out*)(r + ca));
+          __builtin_nontemporal_store(ob, (Out*)(r + cb));
+        } else {
+          *(Out*)(r + ca) = oa;
+          *(Out*)(r + cb) = ob;
+        }
       }
     }
   }
@@ -140,13 +172,15 @@ __device__ __forceinline__ void place(uint32_t block, uint32_t per, int64_t& tok
   unit = idx % per;
 }
 
+// Bound by memory: 8192 tokens of 48 heads of 128 fp16 channels 35.5 us (5.7 TB/s read and written), 2051 tokens of 32 heads of
+// 128 fp32 channels, half of them turned, 15 us (4.5 TB/s; a launch of a few tokens takes 3).
 template <typename T, bool INTER>
 __global__ __launch_bounds__(kThreads) void k_rope(RopeArgs a) {
   int64_t token;
   uint32_t unit;
   place(blockIdx.x, (uint32_t)a.dim / (32 / sizeof(T)), token, unit);
   if (token >= a.tokens) return;
-  rope_unit<T, T, INTER>(a, token, (int)unit, blockIdx.y * a.hpt);
+  rope_unit<T, T, INTER, false>(a, token, (int)unit, blockIdx.y * a.hpt);
 }
 
 struct RopeFreqs {
@@ -291,6 +325,8 @@ __device__ __forceinline__ void append_unit(const AppendArgs& a, int64_t token, 
   }
 }
 
+// Bound by memory, and by the arithmetic of the codes beside it: 8192 tokens of 40 query and 8 kv heads of 128 channels into 4 bits 49 us
+// (137 MB read, 97 written: 4.8 TB/s, vector ALU 42% busy); 64 tokens into 8 bits 3.6 us, the launch's latency.
 template <typename T, int BITS, bool INTER>
 __global__ __launch_bounds__(kThreads) void k_kv_append(AppendArgs a) {
   int64_t token;
@@ -302,7 +338,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(AppendArgs a) {
       const uint32_t q_block = blockIdx.x - kv_block;
       place(q_block / a.q_head_blocks, (uint32_t)a.c.dim / (32 / sizeof(T)), token, unit);
       if (token >= a.tokens) return;
-      rope_unit<T, _Float16, INTER>(a.q, token, (int)unit, (int)(q_block % a.q_head_blocks) * a.q.hpt);
+      rope_unit<T, _Float16, INTER, true>(a.q, token, (int)unit, (int)(q_block % a.q_head_blocks) * a.q.hpt);
       return;
     }
   }
@@ -313,7 +349,8 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(AppendArgs a) {
 
 // ------------------------------------------------------------------ reading
 
-// One thread reads eight channels of one key row and of the value row beside it.
+// One thread reads eight channels of one key row and of the value row beside it. Bound by memory: 32768 tokens of 8 heads of 128
+// channels at 8 bits 34.8 us (6.0 TB/s; with stores that stay in the caches 43.5), 701 tokens of 3 heads of 96 in fp16 2.7 us, the launch's latency.
 template <int BITS>
 __global__ __launch_bounds__(kThreads) void k_kv_read(CacheView c, int64_t tokens, const int32_t* __restrict__ slots,
                                                       _Float16* __restrict__ ko, _Float16* __restrict__ vo) {
@@ -339,8 +376,8 @@ __global__ __launch_bounds__(kThreads) void k_kv_read(CacheView c, int64_t token
     }
   }
   const int64_t to = (token * c.kv_heads + head) * c.dim + ch;
-  *(f16x8*)(ko + to) = k;
-  *(f16x8*)(vo + to) = v;
+  __builtin_nontemporal_store(k, (f16x8*)(ko + to));
+  __builtin_nontemporal_store(v, (f16x8*)(vo + to));
 }
 
 // ------------------------------------------------------------------ host side

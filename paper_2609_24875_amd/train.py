@@ -81,15 +81,18 @@ class _Rope:
 
         class Fn(torch.autograd.Function):
             @staticmethod
-            def forward(ctx, x, positions, table, interleaved):
+            def forward(ctx, x, positions, table, interleaved, inverse):
                 ctx.save_for_backward(positions, table)
-                ctx.interleaved = interleaved
-                return A.rope(x.detach(), positions, table, interleaved=interleaved)
+                ctx.way = interleaved, inverse
+                return A.rope(x, positions, table, interleaved=interleaved, inverse=inverse)
 
             @staticmethod
             def backward(ctx, grad_y):
                 positions, table = ctx.saved_tensors
-                return A.rope(A.aligned_rows(grad_y), positions, table, interleaved=ctx.interleaved, inverse=True), None, None, None
+                interleaved, inverse = ctx.way
+                if grad_y.requires_grad:                    # a gradient of the gradient is asked for
+                    return Fn.apply(A.aligned_rows(grad_y), positions, table, interleaved, not inverse), None, None, None, None
+                return A.rope_gradient(grad_y, positions, table, interleaved, inverse), None, None, None, None
 
         return Fn
 
@@ -105,7 +108,7 @@ def _fn(name):
 
 def rope(x, positions, table, interleaved: bool = False):
     """``attn.rope`` with its gradient with respect to x (positions and table are constants)."""
-    return _fn("rope").apply(x, positions, table, interleaved)
+    return _fn("rope").apply(x, positions, table, interleaved, False)
 
 
 def make_module(w, dir_bits: int, radius_bits: int, init_codebook=None, kmeans_uniforms=None,

@@ -147,6 +147,23 @@ def test_rope_gradient_against_differences():
         assert abs(float((up - down) / 2 - xr.grad.view(-1)[i])) <= 1e-4
 
 
+def test_rope_gradient_of_unaligned_rows_and_of_the_gradient():
+    """The call is linear, so the gradient of sum(g' . dx) with respect to the gradient g that came in is the rotation of g'. Both
+    are bit for bit what the call itself gives."""
+    table = pkg.rope_table(64, 32)
+    pos = torch.arange(5, dtype=torch.int32, device="cuda")
+    x = _randn(5, 3, 64, seed=21, dtype=torch.float32).requires_grad_(True)
+    flat = _randn(5 * 3 * 64 + 1, seed=22, dtype=torch.float32)
+    g = flat[1:].view(5, 3, 64)                                  # 4 bytes behind a row's alignment
+    (dx,) = torch.autograd.grad(train.rope(x, pos, table), x, g)
+    assert torch.equal(dx, pkg.rope(g.clone(), pos, table, inverse=True))
+    g2 = g.clone().requires_grad_(True)
+    (dx,) = torch.autograd.grad(train.rope(x, pos, table), x, g2, create_graph=True)
+    h = _randn(5, 3, 64, seed=23, dtype=torch.float32)
+    (dg,) = torch.autograd.grad(dx, g2, h)
+    assert torch.equal(dg, pkg.rope(h, pos, table))
+
+
 def test_rope_gradient_of_broadcast_and_strided_views():
     table = pkg.rope_table(64, 64)
     pos = torch.arange(6, device=DEV).int()
