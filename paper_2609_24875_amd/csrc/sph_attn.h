@@ -97,10 +97,14 @@ __device__ inline void write_bad(const AttnArgs& a, const Seq& s, int kvh) {
 
 template <int BYTES, bool STREAM = false>
 __device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
-  typedef uint32_t V __attribute__((ext_vector_type(BYTES / 4)));
-  const V v = STREAM ? __builtin_nontemporal_load((const V*)p) : *(const V*)p;
+  if constexpr (BYTES == 4) {   // (not a vector of one: with it, k_attn_wide's 128 channels at 4 bits spill)
+    w[0] = STREAM ? __builtin_nontemporal_load((const uint32_t*)p) : *(const uint32_t*)p;
+  } else {
+    typedef uint32_t V __attribute__((ext_vector_type(BYTES / 4)));
+    const V v = STREAM ? __builtin_nontemporal_load((const V*)p) : *(const V*)p;
 #pragma unroll
-  for (int i = 0; i < BYTES / 4; ++i) w[i] = v[i];
+    for (int i = 0; i < BYTES / 4; ++i) w[i] = v[i];
+  }
 }
 
 // One kv head's pages.
