@@ -325,8 +325,8 @@ __device__ __forceinline__ void append_unit(const AppendArgs& a, int64_t token, 
   }
 }
 
-// Bound by memory, and by the arithmetic of the codes beside it: 8192 tokens of 40 query and 8 kv heads of 128 channels into 4 bits 49 us
-// (137 MB read, 97 written: 4.8 TB/s, vector ALU 42% busy); 64 tokens into 8 bits 3.6 us, the launch's latency.
+// Bound by memory, and by the arithmetic of the codes beside it: 8192 tokens of 40 query and 8 kv heads of 128 channels into 4 bits 51 us
+// (137 MB read, 97 written: 4.6 TB/s, vector ALU 42% busy); 64 tokens into 8 bits 3.6 us, the launch's latency.
 template <typename T, int BITS, bool INTER>
 __global__ __launch_bounds__(kThreads) void k_kv_append(AppendArgs a) {
   int64_t token;
