@@ -210,7 +210,7 @@ class KVCache:
     ([..][channels * bits / 8]) and ``k_par``, ``v_par`` fp16 [pages][kv heads][tokens a page][channels / 32][2]
     of (offset, step). Any strides of the first three dimensions that keep rows 16-byte aligned and are the
     same for keys and values, so both may be views of one allocation or of another order. The handle keeps the
-    attention's workspaces, one a stream."""
+    attention's workspaces, one a stream, and those that larger calls have outgrown, which captured graphs may still use."""
 
     def __init__(self, k, v, k_par=None, v_par=None, bits: int = 16):
         import torch
@@ -243,7 +243,7 @@ class KVCache:
         self.k, self.v, self.k_par, self.v_par = k, v, k_par, v_par
         self.bits, self.n_pages, self.kv_heads, self.page_size, self.head_dim = bits, pages, heads, page, dim
         self.device = k.device
-        self.workspaces = {}
+        self.workspaces, self.outgrown = {}, []
         self.desc = CKVCache(bits, heads, dim, page, pages, k.data_ptr(), v.data_ptr(), *strides,
                              k_par.data_ptr() if bits < 16 else None, v_par.data_ptr() if bits < 16 else None, *par)
         self._ref = ctypes.byref(self.desc)
@@ -342,15 +342,19 @@ def attention_workspace_bytes(cache: KVCache, batch: int, tokens: int, q_heads: 
 
 def _attention_workspace(cache: KVCache, need: int, handle: int, stream):
     """A workspace of at least ``need`` bytes for calls on the stream ``handle``, kept with the cache; streams do not share
-    one, since their calls may run together."""
+    one, since their calls may run together. A captured graph holds the address of the one that its call used, so one that a larger call
+    outgrows is kept, and its successor is twice its size or more: all of them together take less than twice the last."""
     import torch
     if torch.cuda.is_current_stream_capturing():
         # memory of the graph's own pool must not serve later calls outside it
         raise RuntimeError("no workspace of this size on this stream yet: make one call on the capture stream before "
                            "capturing a graph")
-    # allocated on the stream that uses it, so that the one it replaces is freed behind that stream's calls
+    old = cache.workspaces.get(handle)
+    # allocated on the stream that uses it, so that it is freed behind that stream's calls
     with torch.cuda.stream(stream):
-        ws = torch.empty(need, dtype=torch.uint8, device=cache.device)
+        ws = torch.empty(need if old is None else max(need, 2 * old.numel()), dtype=torch.uint8, device=cache.device)
+    if old is not None:
+        cache.outgrown.append(old)
     cache.workspaces[handle] = ws
     return ws
 

@@ -663,3 +663,42 @@ def test_a_decode_step_replays_from_a_graph():
     with pytest.raises(RuntimeError, match="capture"):
         with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=side):
             pkg.attention(rows[:, :8], fresh, pages, lens, max_len=1920)
+
+
+def test_a_graph_keeps_the_workspace_that_a_larger_call_outgrew():
+    """The stream of a captured call is used again by a call that needs more: the graph's workspace stays the cache's, and
+    replays give what they gave, whatever memory later tensors take."""
+    c = _cache(16, 128, 64, 400, 2)
+    _fill(c, 160)
+    lens = [5000, 3000, 4000, 4000]
+    pages, _ = _tables(c, lens, 161)
+    q, ln = _randn(4, 8, 128, seed=162), _i32(lens)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def one():
+        return pkg.attention(q[:1], c, pages[:1], ln[:1], max_len=5000)
+
+    with torch.cuda.stream(side):
+        want = one()
+    torch.cuda.synchronize()
+    held = c.workspaces[side.cuda_stream]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        got = one()
+    many = q.repeat_interleave(16, dim=0).contiguous()           # 16 tokens of each sequence
+    start = _i32([0, 16, 32, 48, 64])
+    with torch.cuda.stream(side):
+        pkg.attention(many, c, pages, ln, q_start=start, max_q=16, max_len=5000)
+    torch.cuda.synchronize()
+    grown = c.workspaces[side.cuda_stream]
+    assert grown.numel() >= 2 * held.numel() and any(x is held for x in c.outgrown)
+    with torch.cuda.stream(side):
+        later = [torch.full_like(held, 7) for _ in range(4)]     # what an allocator would give a freed block to
+    for _ in range(3):
+        got.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+        assert all(bool((x == 7).all()) for x in later)
