@@ -702,3 +702,26 @@ def test_a_graph_keeps_the_workspace_that_a_larger_call_outgrew():
         torch.cuda.synchronize()
         assert torch.equal(got, want)
         assert all(bool((x == 7).all()) for x in later)
+
+
+@pytest.mark.parametrize("new", [1, 12])
+@pytest.mark.parametrize("bits,dim,page", [(16, 96, 8), (16, 128, 64), (8, 96, 4), (8, 128, 16), (8, 64, 8), (4, 96, 8), (4, 128, 1), (4, 256, 32)])
+def test_pools_larger_than_the_caches_give_the_same(bits, dim, page, new):
+    """The same pages among many unused ones, where values are read past the caches: bit for bit what the small pool gives."""
+    lens = [333, 1900, new]
+    count = 3 * -(-1900 // page)
+    small = _cache(bits, dim, page, count, 2)
+    pages, _ = _tables(small, lens, 170)
+    _fill(small, 171)
+    large = pkg.KVCache.empty((300 << 20) // (page * 2 * dim * bits // 4) + 1, 2, dim, page_size=page, bits=bits, device=DEV)
+    step = large.n_pages // count
+    for a, b in ((small.k, large.k), (small.v, large.v), (small.k_par, large.k_par), (small.v_par, large.v_par)):
+        if a is not None:
+            b[::step][:count] = a
+    q = _randn(3 * new, 4, dim, seed=172)
+    start = _i32([0, new, 2 * new, 3 * new])
+    for x in (0, 200):
+        got = [pkg.attention(q, c, t, _i32(lens), q_start=start, max_q=new, max_len=1900, window=x, return_lse=True)
+               for c, t in ((small, pages), (large, (pages * step).contiguous()))]
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+        assert bool(torch.isfinite(got[0][0]).all())
