@@ -70,7 +70,12 @@ __device__ __forceinline__ void write_out(const AttnArgs& a, int64_t token, int 
   const float inv = 1.0f / l;
   f16x4 y;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) y[i] = (_Float16)(l == 0.0f ? 0.0f : acc[i] * inv);
+  for (int i = 0; i < 4; ++i) {
+    float x = l == 0.0f ? 0.0f : acc[i] * inv;
+    // a mean of finite values lies between them: above fp16's largest only what the weights' rounding adds
+    if (__builtin_isfinite(x)) x = fminf(fmaxf(x, -65504.0f), 65504.0f);
+    y[i] = (_Float16)x;
+  }
   *(f16x4*)(a.o + token * a.ot + head * a.oh + 2 * ch) = y;
   if (ch == 0 && a.lse) a.lse[token * a.q_heads + head] = l == 0.0f ? -INFINITY : (m + __builtin_log2f(l)) * kLn2;
 }

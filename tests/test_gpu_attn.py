@@ -725,3 +725,38 @@ def test_pools_larger_than_the_caches_give_the_same(bits, dim, page, new):
                for c, t in ((small, pages), (large, (pages * step).contiguous()))]
         assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
         assert bool(torch.isfinite(got[0][0]).all())
+
+
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("new,group,keys", [(1, 4, 300), (1, 4, 9000), (5, 4, 300), (60, 4, 300), (60, 4, 5000)])
+def test_a_mean_of_the_largest_values_stays_finite(new, group, keys, bits, sign):
+    """Every value is fp16's largest, so every output is: weights that round up must not carry it to infinity. The bound of o is
+    one rounding of the weights and the output's, 2^-10 relative."""
+    c = _cache(bits, 128, 16, -(-keys // 16), 2)
+    n = c.n_pages * c.page_size
+    pkg.kv_append(c, _randn(n, 2, 128, seed=180), torch.full((n, 2, 128), sign * 65504.0, dtype=torch.float16, device=DEV),
+                  torch.arange(n, device=DEV).int())
+    pages, _ = _tables(c, [keys], 181)
+    o = pkg.attention(_randn(new, 2 * group, 128, seed=182), c, pages, _i32([keys]), q_start=_i32([0, new]), max_q=new, max_len=keys)
+    assert bool(torch.isfinite(o).all())
+    assert float((o.double() - sign * 65504.0).abs().max()) <= 65504.0 * 2.0 ** -10
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("group", [1, 40])
+def test_a_weight_rounded_up_does_not_carry_its_value_to_infinity(group, bits):
+    """A key some tiles behind the first has a weight of 128 to 256 beside the first's 1, in steps of an eighth in fp16: rounded up it adds up
+    to 4.9e-4 of itself, twice what fp16's largest number is from infinity."""
+    assert any((float(np.float16(w)) - w) / (1 + w) > 2.0 ** -12 for w in np.exp(np.float16(4.9) * np.linspace(1, 1.12, 200)))
+    c = _cache(bits, 64, 64, 3, 1)
+    k = torch.zeros(192, 1, 64, dtype=torch.float16, device=DEV)
+    k[:, :, 0] = -60.0                                           # e^-60: nothing in fp16
+    k[0, :, 0], k[128, :, 0] = 0.0, 4.9
+    pkg.kv_append(c, k, torch.full_like(k, 65504.0), torch.arange(192, device=DEV).int())
+    q = torch.zeros(200, group, 64, dtype=torch.float16, device=DEV)
+    q[:, :, 0] = torch.linspace(1, 1.12, 200, device=DEV)[:, None]
+    pages = torch.arange(3, device=DEV).int().expand(200, 3).contiguous()
+    o = pkg.attention(q, c, pages, torch.full((200,), 192, dtype=torch.int32, device=DEV), max_len=192, scale=1.0)
+    assert bool(torch.isfinite(o).all())
+    assert float((o.double() - 65504.0).abs().max()) <= 65504.0 * 2.0 ** -10
