@@ -27,7 +27,8 @@ struct AttnArgs {
   float2* ml;
   int2* where;
   int64_t tokens;
-  int batch, q_heads, group, max_q, max_len, window, tiles, splits, chunk, shares;
+  int batch, q_heads, group, max_q, max_len, window, tiles, splits, chunk, shares, fold;
+  // (fold: tiles of rows between k_attn_wide's workgroups that share a CU, 0 for the longest first)
   bool stream;             // k_attn reads values past the caches
   float scale;             // times log2 e
 };

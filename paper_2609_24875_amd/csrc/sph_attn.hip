@@ -568,7 +568,7 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(AttnArgs a) {
 // ------------------------------------------------------------------ host side
 
 struct Plan {
-  int wide, nb, tiles, splits, chunk, shares, window;
+  int wide, nb, tiles, splits, chunk, shares, fold, window;
   size_t parts;                            // rows of partial sums
   size_t bytes;
 };
@@ -628,6 +628,12 @@ Plan plan_of(const sph_kv_cache* c, int64_t batch, int q_heads, int64_t max_q, i
     p.chunk = (int)std::max<int64_t>(step, ((span + want - 1) / want + step - 1) / step * step);
     p.splits = (int)std::max<int64_t>(1, (span + p.chunk - 1) / p.chunk);
     if (p.splits > 1) slots = p.splits * batch;
+    // All workgroups resident at once, two on some CUs (the i-th and the (i + 256)-th; of 64 channels a CU takes more, of 192 one): long
+    // rows share theirs with short ones. 8 kv heads of 128 channels, so and with the longest first, fp16: prompts of 2048 tokens 63.2 and 66.3 us,
+    // 1536 48.0 and 50.1, four of 512 26.7 and 30.3, 1300 behind 6700 others 233 and 241; four of 500 at 8 bits 30.4 and 35.1; 2048 of 96
+    // channels 50.4 and 51.4, of 64 42.6 and 42.1.
+    if (c->head_dim > 64 && c->head_dim <= 128 && p.splits == 1 && kCus % c->kv_heads == 0 && units > kCus && units <= 2 * kCus)
+      p.fold = kCus / c->kv_heads;
   }
   p.parts = (size_t)slots * c->kv_heads * rows;
   if (slots) p.bytes = p.parts * (c->head_dim + 2) * sizeof(float) + (size_t)batch * sizeof(int2);
@@ -705,7 +711,7 @@ sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t token
   a.q_start = d_q_start, a.pages = d_pages, a.pages_stride = pages_stride, a.lens = d_seq_lens, a.lse = d_lse;
   a.tokens = tokens, a.batch = (int)batch, a.q_heads = q_heads, a.group = q_heads / cache->kv_heads;
   a.max_q = (int)max_q, a.max_len = (int)max_len, a.window = p.window;
-  a.tiles = p.tiles, a.splits = p.splits, a.chunk = p.chunk, a.shares = p.shares;
+  a.tiles = p.tiles, a.splits = p.splits, a.chunk = p.chunk, a.shares = p.shares, a.fold = p.fold;
   a.scale = scale * kLog2e;
   a.stream = cache->n_pages * cache->page_size * cache->kv_heads * (int64_t)dim * bits / 4 > kLastCache;
   if (p.bytes) {

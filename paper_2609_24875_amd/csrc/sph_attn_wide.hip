@@ -126,7 +126,7 @@ __device__ __forceinline__ bool clean_share(char* lds, int kt, int k_lo, int k_h
 }
 
 // What bounds it: matrix products and exponentials together, on two waves a SIMD (one above 128 channels). 2048 new tokens behind 14336
-// others, 32 query heads over 8 kv heads of 128 channels, fp16: 596 us, 865 TFLOP/s at a clock that the products lower to about 2.0 GHz; MFMA
+// others, 32 query heads over 8 kv heads of 128 channels, fp16: 579 us, 890 TFLOP/s at a clock that the products lower to about 2.0 GHz; MFMA
 // 40%, vector ALU 42%, LDS 25% busy, no bank conflicts. Twice the rows a wave halve its LDS reads, but leave one wave a SIMD, which
 // does not overlap its products with its weights well enough: 920 us. 4096 tokens over themselves at 8 bits 226 us, 4 bits 214, fp16 197.
 template <int DIM, int BITS>
@@ -141,9 +141,18 @@ __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(At
   uint32_t id = blockIdx.x;
   const int kvh = id % a.c.kv_heads;
   id /= a.c.kv_heads;
-  const int tile = a.tiles - 1 - (int)(id % a.tiles);        // the last rows see most
+  const int place = id % a.tiles;
   id /= a.tiles;
   const int b = id % a.batch, split = id / a.batch;
+  // The last rows see most, so they come first. Where all workgroups are resident at once, two on some CUs (see plan_of), the ones that
+  // share a CU, a.fold places apart, are a long and a short one, and the longest have theirs alone.
+  int tile = a.tiles - 1 - place;
+  if (a.fold && a.batch > 1) {
+    if (b * a.tiles >= a.fold) tile = place;
+  } else if (a.fold) {
+    const int shared = a.tiles - a.fold;
+    tile = place < shared ? 2 * shared - 1 - place : place < a.fold ? a.tiles - 1 - (place - shared) : place - a.fold;
+  }
   Seq s;
   s.load(a, b);
   if (s.bad) {

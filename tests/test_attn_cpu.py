@@ -314,3 +314,31 @@ def test_spare_shares_cut_each_sequence_evenly():
         for b in range(batch):
             edges = [0] + [hi for _, hi in got[b]]
             assert edges[-1] == tiles[b] and [lo for lo, _ in got[b]] == edges[:-1]
+
+
+@pytest.mark.parametrize("kv_heads", [1, 2, 4, 8, 16, 64, 256])
+def test_folded_rows_are_taken_once_and_balanced(kv_heads):
+    """Where workgroups of many rows share CUs in pairs, every sequence's tiles are each some workgroup's, and a single sequence's pairs
+    have equal sums (the kernel's arithmetic, in Python)."""
+    fold = 256 // kv_heads
+    for batch in (1, 2, 3, 4, 7, 16):
+        for tiles in range(1, 2 * fold // batch + 1):
+            if not fold < tiles * batch <= 2 * fold:
+                continue
+            at = []
+            for b in range(batch):
+                row = []
+                for place in range(tiles):
+                    tile = tiles - 1 - place
+                    if batch > 1:
+                        if b * tiles >= fold:
+                            tile = place
+                    else:
+                        shared = tiles - fold
+                        tile = 2 * shared - 1 - place if place < shared else tiles - 1 - (place - shared) if place < fold else place - fold
+                    row.append(tile)
+                assert sorted(row) == list(range(tiles))
+                at += row
+            if batch == 1:
+                pairs = {at[i] + at[i + fold] for i in range(tiles - fold)}
+                assert pairs == {2 * (tiles - fold) - 1}

@@ -760,3 +760,10 @@ def test_a_weight_rounded_up_does_not_carry_its_value_to_infinity(group, bits):
     o = pkg.attention(q, c, pages, torch.full((200,), 192, dtype=torch.int32, device=DEV), max_len=192, scale=1.0)
     assert bool(torch.isfinite(o).all())
     assert float((o.double() - 65504.0).abs().max()) <= 65504.0 * 2.0 ** -10
+
+
+@pytest.mark.parametrize("bits,dim,window", [(16, 128, 0), (8, 128, 40), (4, 96, 0), (16, 96, 100)])
+@pytest.mark.parametrize("lens,new", [([170], [170]), ([300], [250]), ([50, 64, 100], [50, 64, 33]), ([64, 3, 0, 70], [64, 1, 0, 60])])
+def test_attention_of_prompts_that_fill_the_chip_once_or_twice(lens, new, bits, dim, window):
+    """Workgroups that share a compute unit take long and short rows: every row is some workgroup's."""
+    _run(bits, dim, 16, heads=64, group=4, lens=lens, new=new, window=window, seed=190)
