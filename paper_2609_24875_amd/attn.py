@@ -86,7 +86,8 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none",
         # the pair that makes `turns` turns over the original context
         def pair(turns):
             return rot_dim * math.log(original_max_pos / (turns * 2.0 * math.pi)) / (2.0 * math.log(base))
-        lo, hi = max(math.floor(pair(beta_fast)), 0), min(math.ceil(pair(beta_slow)), rot_dim // 2 - 1)
+        # (the slow end may lie behind the last pair, which then stops short of the whole factor)
+        lo, hi = max(math.floor(pair(beta_fast)), 0), min(math.ceil(pair(beta_slow)), rot_dim - 1)
         keep = 1.0 - np.clip((i - lo) / max(hi - lo, 1e-3), 0.0, 1.0)
         return f * keep + f / factor * (1.0 - keep), 0.1 * math.log(factor) + 1.0
     raise ValueError(f"scaling must be none, linear, ntk or yarn, not {scaling!r}")

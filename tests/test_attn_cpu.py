@@ -234,6 +234,25 @@ def test_rope_frequencies():
             pkg.rope_frequencies(rot)
 
 
+@pytest.mark.parametrize("base,rot,original", [(10000.0, 128, 4096), (10000.0, 128, 65536), (10000.0, 128, 131072), (10000.0, 128, 1 << 20),
+                                               (10000.0, 64, 262144), (500000.0, 128, 8192), (500000.0, 128, 1 << 23), (1e6, 128, 32768)])
+def test_yarn_divides_by_the_whole_factor_only_behind_the_slow_pair(base, rot, original):
+    """The pair index at which a pair makes `turns` turns over the original context solves original base^(-2i/rot) = 2 pi turns; the ramp goes from
+    the index of 32 turns, rounded down, to that of one, rounded up, which for long contexts lies behind the last pair. In exact steps of one
+    pair, so that a pair between has its own share."""
+    factor = 4.0
+    f, _ = pkg.rope_frequencies(rot, base=base)
+    y, m = pkg.rope_frequencies(rot, base=base, scaling="yarn", factor=factor, original_max_pos=original)
+    fast, slow = (math.log(original / (2 * math.pi * turns), base) * rot / 2 for turns in (32, 1))
+    lo, hi = max(math.floor(fast), 0), math.ceil(slow)
+    assert lo < hi < rot
+    for i in range(rot // 2):
+        stretched = 0.0 if i <= lo else 1.0 if i >= hi else (i - lo) / (hi - lo)
+        assert math.isclose(y[i], f[i] * (1 - stretched) + f[i] / factor * stretched, rel_tol=1e-12)
+    turns = original * f / (2 * math.pi)
+    assert np.all(y[turns > 1] > f[turns > 1] / factor * (1 + 1e-3)) and np.all(np.diff(y) < 0)
+
+
 # ------------------------------------------------------------------ launch arithmetic
 
 def test_cache_blocks_are_spread_evenly_and_each_runs_once():
