@@ -381,7 +381,8 @@ sph_status sph_kv_read(const sph_kv_cache* cache, int64_t tokens, const int32_t*
  * position p sees the tokens j <= p, and with window > 0 only j > p - window; o = sum_j softmax_j(scale
  * q.k_j) v_j, with query head h reading kv head h / (q_heads / kv_heads). A query that sees nothing
  * gets zeros. Scores, the softmax's maximum and sum and the output are held in fp32; the weights
- * exp(s - max) are rounded to fp16 for the matrix cores.
+ * exp(s - max) are rounded to fp16 for the matrix cores, lifted so that those down to 2^-25 of the largest keep 11 bits and none
+ * is off by more than 2^-36 of it.
  *
  * d_q, d_o: device fp16 rows [tokens][q_heads]. d_q_start: device int32[batch + 1], ascending from 0 to
  * `tokens`: sequence b's queries are tokens d_q_start[b]..d_q_start[b+1]-1, at most max_q of them; or NULL with

@@ -44,6 +44,11 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 
+// Weights are exp2(score - m + kLift), m a maximum that is raised, and o and l scaled down, only when a score passes it by kRise: up to 2^15,
+// inside fp16's range, and at full precision down to 2^-25 of m's, since those that fp16 loses would be missing from o and not from l.
+// Rises of 2, 4 and 8 (lifts to match): 2048 tokens over themselves 63.7, 62.3 and 62.0 us, 4096 of 192 channels 365, 348 and 335, single tokens alike.
+constexpr float kRise = 4.0f, kLift = 11.0f;
+
 // The queries of one sequence: tokens start .. end - 1.
 struct Seq {
   int start, end, n, len;

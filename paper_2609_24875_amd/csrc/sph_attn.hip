@@ -262,8 +262,6 @@ __device__ __forceinline__ void attend(const AttnArgs& a, char* lds, float2 (*ml
       __builtin_amdgcn_sched_barrier(0);
       const int nnt = nt + kTile * kWaves < k_hi ? nt + kTile * kWaves : nt;
       next = page_of(nnt);
-      // weights; the reference m is raised, and o and l scaled down, only when a score passes it by 2^8: weights up to
-      // 256 lose nothing in fp16 or fp32
       f16x8 p[NB];
       bool rise = false;
       float x[NB][8], top[NB];
@@ -285,7 +283,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, char* lds, float2 (*ml
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) top[n] = fmaxf(top[n], x[n][i]);
-        rise |= top[n] > m[n] + 8.0f;
+        rise |= top[n] > m[n] + kRise;
       }
       if (__any(rise)) {
 #pragma unroll
@@ -293,8 +291,9 @@ __device__ __forceinline__ void attend(const AttnArgs& a, char* lds, float2 (*ml
           float mn = fmaxf(m[n], top[n]);
           mn = fmaxf(mn, __shfl_xor(mn, 16));
           mn = fmaxf(mn, __shfl_xor(mn, 32));
-          base[n] = mn == -INFINITY ? 0.0f : mn;
-          const float keep = __builtin_amdgcn_exp2f(m[n] - base[n]);
+          const float ref = mn == -INFINITY ? 0.0f : mn;
+          const float keep = __builtin_amdgcn_exp2f(m[n] - ref);
+          base[n] = ref - kLift;
           m[n] = mn;
           l[n] *= keep;
 #pragma unroll
@@ -355,7 +354,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, char* lds, float2 (*ml
   float* os = (float*)lds + wave * kRows * kOStride;
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
-    if (g4 == 0) ml_s[wave][16 * n + col] = make_float2(m[n], l[n]);
+    if (g4 == 0) ml_s[wave][16 * n + col] = make_float2(m[n] - kLift, l[n]);
 #pragma unroll
     for (int i = 0; i < DIM / 16; ++i) *(f32x4*)(os + (16 * n + col) * kOStride + 16 * i + 4 * g4) = o[n][i];
   }

@@ -269,11 +269,12 @@ __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(At
 #pragma unroll
           for (int i = 0; i < 16; i += 2) top = fmaxf(top, fmaxf(st[u][i], st[u][i + 1]));
         // -inf times a scale of 0 is NaN, which raises nothing: with nothing seen m stays -inf
-        if (__any(top * scale > m + 8.0f)) {
+        if (__any(top * scale > m + kRise)) {
           float mn = fmaxf(m, top * scale);
           mn = fmaxf(mn, __shfl_xor(mn, 32));
-          base = mn == -INFINITY ? 0.0f : mn;
-          const float keep = __builtin_amdgcn_exp2f(m - base);
+          const float ref = mn == -INFINITY ? 0.0f : mn;
+          const float keep = __builtin_amdgcn_exp2f(m - ref);
+          base = ref - kLift;
           m = mn;
           l *= keep;
 #pragma unroll
@@ -324,6 +325,7 @@ __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(At
       tile_at(kt + kTile, lds_b, lds_a);
     }
     l += __shfl_xor(l, 32);
+    m -= kLift;
   }
   const bool any_odd = __syncthreads_or(odd);
   if (w0 + col >= nrow) return;

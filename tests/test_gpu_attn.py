@@ -767,3 +767,42 @@ def test_a_weight_rounded_up_does_not_carry_its_value_to_infinity(group, bits):
 def test_attention_of_prompts_that_fill_the_chip_once_or_twice(lens, new, bits, dim, window):
     """Workgroups that share a compute unit take long and short rows: every row is some workgroup's."""
     _run(bits, dim, 16, heads=64, group=4, lens=lens, new=new, window=window, seed=190)
+
+
+@pytest.mark.parametrize("below", [17.0, 18.0, 20.0])
+@pytest.mark.parametrize("new,group,lens,bits,dim,window", [
+    (1, 4, [700, 90], 16, 128, 0), (1, 4, [20000, 3000], 16, 64, 0), (1, 5, [20000], 8, 128, 0), (1, 20, [3000, 9], 4, 96, 0),
+    (5, 4, [16000, 40], 8, 192, 0), (60, 4, [400], 16, 128, 0), (60, 4, [16000], 16, 64, 0), (70, 2, [5000, 3000], 4, 256, 0),
+    (40, 8, [16000, 300, 200, 100], 8, 128, 0), (60, 4, [16000], 8, 96, 15990)])
+def test_small_weights_beside_a_large_one_are_kept(new, group, lens, bits, dim, window, below):
+    """The first key that is seen outweighs every other one by e^below and has a value of zero, so the output is what the others' weights
+    leave of theirs. Weights reach the values' product in fp16, lifted by 2^11: half an ulp, 2^-11 of each, or 2^-25 below the normal range, 2^-36 of
+    the largest. The rest of the bound as in ``_reference``, whose 2^-25 of the largest for each key is what this leaves out."""
+    cols = -(-max(lens) // 64)
+    c = _cache(bits, dim, 64, len(lens) * cols, 2)
+    pages, slots = _tables(c, lens, 200)
+    first = [max(0, ln - new + 1 - window) if window else 0 for ln in lens]
+    for b, ln in enumerate(lens):
+        k = torch.zeros(ln, 2, dim, dtype=torch.float16, device=DEV)
+        k[:, :, 1:] = _randn(ln, 2, dim - 1, seed=201 + b)
+        v = 1000.0 + 300.0 * _randn(ln, 2, dim, seed=205 + b)
+        k[:first[b] + new, :, 0] = 1.0 if window else 0.0             # with a window, the first that each query sees
+        k[first[b], :, 0] = 1.0
+        v[:first[b] + (new if window else 1)] = 0.0
+        pkg.kv_append(c, k, v, slots[b].int())
+    keys, values = pkg.kv_read(c, torch.arange(c.n_pages * 64, device=DEV).int())
+    q = torch.zeros(new * len(lens), 2 * group, dim, dtype=torch.float16, device=DEV)
+    q[:, :, 0] = below
+    start = _i32([new * i for i in range(len(lens) + 1)])
+    o, lse = pkg.attention(q, c, pages, _i32(lens), q_start=start, max_q=new, max_len=max(lens), window=window, scale=1.0, return_lse=True)
+    ro, rl, ob, lb = _reference(q, keys, values, slots, lens, [new] * len(lens), window, 1.0)
+    t = 0
+    for b, ln in enumerate(lens):
+        for i in range(new):
+            p = ln - new + i
+            lo = max(0, p - window + 1) if window else 0
+            seen = slots[b][lo:p + 1]
+            top = values[seen].double().abs().amax(0).repeat_interleave(group, 0)
+            ob[t] += len(seen) * (2.0 ** -36 - 2.0 ** -25) * top
+            t += 1
+    _close((o, lse), (ro, rl, ob, lb))
