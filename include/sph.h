@@ -388,7 +388,8 @@ sph_status sph_kv_read(const sph_kv_cache* cache, int64_t tokens, const int32_t*
  * `tokens`: sequence b's queries are tokens d_q_start[b]..d_q_start[b+1]-1, at most max_q of them; or NULL with
  * max_q = 1 and tokens = batch: one each. d_seq_lens: device int32[batch]; d_pages: device int32[batch][pages_stride], at least
  * ceil(max_len / page_size) entries each, of which only those below the sequence's length are read. max_len (0..2^30): the
- * host's bound of the lengths; the launch is planned for it. d_lse: device fp32[tokens][q_heads], natural
+ * host's bound of the lengths; the launch is planned for it. batch is 0..65536 and max_q 1..2^24; SPH_ERR_SHAPE, from the workspace
+ * query too, where batch * kv_heads * ceil(max_q * group / 128) passes a launch's 2^24 workgroups. d_lse: device fp32[tokens][q_heads], natural
  * logarithm of sum_j exp(scale q.k_j) (-inf where nothing is seen), or NULL. scale must be finite. d_ws: at
  * least sph_attention_workspace_bytes, 256-byte aligned, no initial contents; concurrent calls must not share one.
  * Keys and values that no query sees are never used, whatever they hold. Queries of a sequence whose length is outside 0..max_len, whose start and count are

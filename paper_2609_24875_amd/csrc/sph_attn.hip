@@ -567,7 +567,10 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(AttnArgs a) {
 // ------------------------------------------------------------------ host side
 
 struct Plan {
-  int wide, nb, tiles, splits, chunk, shares, fold, window;
+  int wide, nb, splits, chunk, shares, fold, window;
+  int64_t tiles;                           // (up to 2^33 before the launch is refused)
+  int64_t grid, joins;                     // workgroups; waves of the join
+  bool few;                                // k_attn_join's form
   size_t parts;                            // rows of partial sums
   size_t bytes;
 };
@@ -616,7 +619,7 @@ Plan plan_of(const sph_kv_cache* c, int64_t batch, int q_heads, int64_t max_q, i
       slots = p.shares + batch;
     }
   } else {
-    p.tiles = (int)((rows + kWideRows - 1) / kWideRows);
+    p.tiles = (rows + kWideRows - 1) / kWideRows;
     const int64_t tile = sph_attn_wide_tile(c->head_dim), step = 4 * tile;
     const int64_t span = window > 0 ? std::min<int64_t>(max_len, window + kWideRows / group + 1 + tile) : max_len;
     // None where the rows alone give half the CUs a workgroup: two parts save less than their join costs (900 rows of one prompt 35 us,
@@ -636,8 +639,16 @@ Plan plan_of(const sph_kv_cache* c, int64_t batch, int q_heads, int64_t max_q, i
   }
   p.parts = (size_t)slots * c->kv_heads * rows;
   if (slots) p.bytes = p.parts * (c->head_dim + 2) * sizeof(float) + (size_t)batch * sizeof(int2);
+  const int64_t heads = c->kv_heads, all = heads * batch * rows;
+  p.grid = p.wide ? heads * batch * p.tiles * p.splits : heads * (p.shares ? p.shares : batch);
+  // k_attn_wide's parts are few, and k_attn's where sequences share a workgroup rather than the other way round
+  p.few = p.wide ? p.splits <= kFewParts : 2 * batch > p.shares && p.shares <= kFewParts * batch;
+  p.joins = p.few ? all : all * (c->head_dim / kJoinCh);
   return p;
 }
+
+// Whether launches take it (and rows of a sequence fit 32 bits).
+bool launchable(const Plan& p) { return p.grid < (1 << 24) && (!p.bytes || p.joins < (1 << 26)); }
 
 sph_status check_sizes(const sph_kv_cache* c, int64_t batch, int64_t tokens, int32_t q_heads, int64_t max_q, int64_t max_len,
                        int64_t window) {
@@ -676,7 +687,11 @@ sph_status sph_attention_workspace_bytes(const sph_kv_cache* cache, int64_t batc
                                          int64_t max_q, int64_t max_len, int64_t window, size_t* bytes) {
   if (!bytes) return SPH_ERR_NULL;
   if (const sph_status st = check_sizes(cache, batch, tokens, q_heads, max_q, max_len, window)) return st;
-  *bytes = batch && tokens ? plan_of(cache, batch, q_heads, max_q, max_len, window).bytes : 0;
+  *bytes = 0;
+  if (!batch || !tokens) return SPH_OK;
+  const Plan p = plan_of(cache, batch, q_heads, max_q, max_len, window);
+  if (!launchable(p)) return SPH_ERR_SHAPE;
+  *bytes = p.bytes;
   return SPH_OK;
 }
 
@@ -700,6 +715,7 @@ sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t token
     return SPH_ERR_SHAPE;
   if ((tokens > 1 && o_token_stride == 0) || (q_heads > 1 && o_head_stride == 0)) return SPH_ERR_SHAPE;  // rows written twice
   const Plan p = plan_of(cache, batch, q_heads, max_q, max_len, window);
+  if (!launchable(p)) return SPH_ERR_SHAPE;
   if (p.bytes && !d_ws) return SPH_ERR_NULL;
   if (ws_bytes < p.bytes) return SPH_ERR_BUFFER_TOO_SMALL;
   const int bits = cache->bits, dim = cache->head_dim;
@@ -710,7 +726,7 @@ sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t token
   a.q_start = d_q_start, a.pages = d_pages, a.pages_stride = pages_stride, a.lens = d_seq_lens, a.lse = d_lse;
   a.tokens = tokens, a.batch = (int)batch, a.q_heads = q_heads, a.group = q_heads / cache->kv_heads;
   a.max_q = (int)max_q, a.max_len = (int)max_len, a.window = p.window;
-  a.tiles = p.tiles, a.splits = p.splits, a.chunk = p.chunk, a.shares = p.shares, a.fold = p.fold;
+  a.tiles = (int)p.tiles, a.splits = p.splits, a.chunk = p.chunk, a.shares = p.shares, a.fold = p.fold;
   a.scale = scale * kLog2e;
   a.stream = cache->n_pages * cache->page_size * cache->kv_heads * (int64_t)dim * bits / 4 > kLastCache;
   if (p.bytes) {
@@ -718,17 +734,11 @@ sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t token
     a.ml = (float2*)(a.part + p.parts * cache->head_dim);
     a.where = (int2*)(a.ml + p.parts);
   }
-  const int64_t heads = cache->kv_heads;
-  const int64_t grid = p.wide ? heads * batch * p.tiles * p.splits : heads * (p.shares ? p.shares : batch), rows = heads * batch * max_q * a.group;
-  // k_attn_wide's parts are few, and k_attn's where sequences share a workgroup rather than the other way round
-  const bool few = p.wide ? p.splits <= kFewParts : 2 * batch > p.shares && p.shares <= kFewParts * batch;
-  const int64_t joins = few ? rows : rows * (cache->head_dim / kJoinCh);
-  if (grid >= (1 << 24) || (p.bytes && joins >= (1 << 26))) return SPH_ERR_SHAPE;
   const void* fn = p.wide ? sph_attn_wide_kernel(bits, dim)
                    : cache->page_size >= 16 ? (p.nb == 1 ? kernel_for<1, true>(bits, dim) : kernel_for<2, true>(bits, dim))
                                           : (p.nb == 1 ? kernel_for<1, false>(bits, dim) : kernel_for<2, false>(bits, dim));
-  if (!launch_ok(fn, dim3((unsigned)grid), (hipStream_t)stream, a)) return SPH_ERR_HIP;
-  if (p.bytes && !launch_ok(few ? (const void*)k_attn_join<true> : (const void*)k_attn_join<false>, dim3((unsigned)((joins + kWaves - 1) / kWaves)),
+  if (!launch_ok(fn, dim3((unsigned)p.grid), (hipStream_t)stream, a)) return SPH_ERR_HIP;
+  if (p.bytes && !launch_ok(p.few ? (const void*)k_attn_join<true> : (const void*)k_attn_join<false>, dim3((unsigned)((p.joins + kWaves - 1) / kWaves)),
                             (hipStream_t)stream, a))
     return SPH_ERR_HIP;
   return SPH_OK;

@@ -145,6 +145,18 @@ def test_attention_workspace():
     assert A._library().sph_attention_workspace_bytes(ctypes.byref(_cache()), 1, 1, 8, 1, 64, 0, None) == NULL
 
 
+@needs_lib
+@pytest.mark.parametrize("kv_heads,heads,batch,max_q", [(1, 65535, 1, 1 << 24), (1, 32768, 1, 1 << 24), (1, 49152, 3, 1 << 24), (2, 65534, 65536, 1 << 24),
+                                                        (1024, 64512, 65536, 1 << 20), (8, 32, 65536, 1 << 13), (8, 32, 4096, 65536)])
+def test_rows_beyond_a_launch_are_refused(kv_heads, heads, batch, max_q):
+    """Tiles of rows that pass 32 bits, or a launch's 2^24 workgroups, on the way to a plan: a status from both entries."""
+    lib, r, n = A._library(), ctypes.byref(_cache(kv_heads=kv_heads)), ctypes.c_size_t(7)
+    for max_len in (64, 4096, 1 << 30):
+        assert lib.sph_attention_workspace_bytes(r, batch, 1 << 26, heads, max_q, max_len, 0, ctypes.byref(n)) == SHAPE
+        assert lib.sph_attention(r, batch, 1 << 26, heads, P, heads * 128, 128, P, max_q, P, 1 << 26, P, max_len, 0, 1.0, P, heads * 128, 128,
+                                 None, P, 1 << 40, None) == SHAPE
+
+
 # ------------------------------------------------------------------ the binding
 
 def _cpu_cache(bits=8, **kw):
