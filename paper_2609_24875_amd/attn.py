@@ -211,7 +211,8 @@ class KVCache:
     ([..][channels * bits / 8]) and ``k_par``, ``v_par`` fp16 [pages][kv heads][tokens a page][channels / 32][2]
     of (offset, step). Any strides of the first three dimensions that keep rows 16-byte aligned and are the
     same for keys and values, so both may be views of one allocation or of another order. The handle keeps the
-    attention's workspaces, one a stream, and those that larger calls have outgrown, which captured graphs may still use."""
+    attention's workspaces, one a stream, and those that larger calls have outgrown; calls that a graph captures (``torch.cuda.graph``)
+    have theirs in the graph's memory pool, so that its replays need no order with other calls' or other graphs'."""
 
     def __init__(self, k, v, k_par=None, v_par=None, bits: int = 16):
         import torch
@@ -343,10 +344,10 @@ def attention_workspace_bytes(cache: KVCache, batch: int, tokens: int, q_heads: 
 
 def _attention_workspace(cache: KVCache, need: int, handle: int, stream):
     """A workspace of at least ``need`` bytes for calls on the stream ``handle``, kept with the cache; streams do not share
-    one, since their calls may run together. A captured graph holds the address of the one that its call used, so one that a larger call
-    outgrows is kept, and its successor is twice its size or more: all of them together take less than twice the last."""
+    one, since their calls may run together. One that a larger call outgrows is kept, and its successor is twice its size or more: all of
+    them together take less than twice the last."""
     import torch
-    if torch.cuda.is_current_stream_capturing():
+    if _capturing(stream):
         # memory of the graph's own pool must not serve later calls outside it
         raise RuntimeError("no workspace of this size on this stream yet: make one call on the capture stream before "
                            "capturing a graph")
@@ -358,6 +359,22 @@ def _attention_workspace(cache: KVCache, need: int, handle: int, stream):
         cache.outgrown.append(old)
     cache.workspaces[handle] = ws
     return ws
+
+
+def _capturing(stream) -> bool:
+    import torch
+    if stream is None:
+        return torch.cuda.is_current_stream_capturing()
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
+def _graph_workspace(cache: KVCache, need: int, stream):
+    """A captured call's workspace: from the pool of its graph, whose replays may run beside calls on any stream and beside
+    other graphs. Given back when the call is captured, since only this graph's later calls on the stream get it again."""
+    import torch
+    with torch.cuda.stream(stream):
+        return torch.empty(need, dtype=torch.uint8, device=cache.device)
 
 
 def attention(q, cache: KVCache, pages, seq_lens, q_start=None, max_q: int = 1, max_len: int | None = None, window: int = 0,
@@ -407,6 +424,10 @@ def attention(q, cache: KVCache, pages, seq_lens, q_start=None, max_q: int = 1, 
                                         None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(),
                                         0 if ws is None else ws.numel(), handle)
 
+    if ws is not None and _capturing(stream):
+        need = attention_workspace_bytes(cache, batch, n, heads, max_q, max_len, window)
+        if need <= ws.numel():
+            ws = _graph_workspace(cache, need, stream)
     st = call(ws)
     if st in (SPH_ERR_NULL, SPH_ERR_BUFFER_TOO_SMALL):
         # the library found, before it launched anything, that it needs a workspace or a larger one
