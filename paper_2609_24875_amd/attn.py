@@ -98,6 +98,7 @@ def rope_table(rot_dim: int, max_pos: int, device="cuda", stream=None, **scaling
     import torch
     f, magnitude = rope_frequencies(rot_dim, **scaling)
     out = torch.empty((max_pos, rot_dim // 2, 2), dtype=torch.float32, device=device)
+    _on_gpu(out)
     arr = (ctypes.c_double * len(f))(*f)
     _check(_library().sph_rope_table(rot_dim, max_pos, arr, magnitude, out.data_ptr(), _stream_handle(stream)), "sph_rope_table")
     return out

@@ -224,6 +224,12 @@ def test_binding_refusals():
             f()
 
 
+@needs_lib
+def test_a_table_is_made_on_a_gpu_only():
+    with pytest.raises(ValueError, match="GPU"):
+        pkg.rope_table(64, 10, device="cpu")
+
+
 # ------------------------------------------------------------------ rotary frequencies
 
 def test_rope_frequencies():
