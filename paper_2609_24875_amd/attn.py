@@ -1,5 +1,6 @@
 """Rotary positions, the paged key-value cache and its attention (include/sph.h): argument
-marshalling only, as in ``sph``.
+marshalling only, as in ``sph``. ``stream``: the call runs as it would under ``torch.cuda.stream(stream)``, to which the
+tensors that it returns then belong.
 
 A decoder block runs ``gemm`` (fused q/k/v), ``kv_append`` (rotates keys and queries and writes the
 cache), ``attention`` and ``gemm`` (o); ``block.AttentionBlock`` does so. The cache's pages are plain
@@ -96,11 +97,14 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none",
 def rope_table(rot_dim: int, max_pos: int, device="cuda", stream=None, **scaling):
     """fp32 [max_pos][rot_dim/2][2] of (cos, sin) (sph_rope_table); keywords as ``rope_frequencies``."""
     import torch
+    if stream is not None:                      # what is made for the call belongs to its stream
+        with torch.cuda.stream(stream):
+            return rope_table(rot_dim, max_pos, device, **scaling)
     f, magnitude = rope_frequencies(rot_dim, **scaling)
     out = torch.empty((max_pos, rot_dim // 2, 2), dtype=torch.float32, device=device)
     _on_gpu(out)
     arr = (ctypes.c_double * len(f))(*f)
-    _check(_library().sph_rope_table(rot_dim, max_pos, arr, magnitude, out.data_ptr(), _stream_handle(stream)), "sph_rope_table")
+    _check(_library().sph_rope_table(rot_dim, max_pos, arr, magnitude, out.data_ptr(), _stream_handle()), "sph_rope_table")
     return out
 
 
@@ -174,6 +178,9 @@ def rope(x, positions, table, interleaved: bool = False, inverse: bool = False, 
     copied. ``inverse`` turns back and is the gradient (``train.rope`` is the differentiable form).
     ``out`` may be x."""
     import torch
+    if stream is not None:                      # what is made for the call belongs to its stream
+        with torch.cuda.stream(stream):
+            return rope(x, positions, table, interleaved, inverse, out)
     half = (torch.float16, torch.float32)
     px, xt, xh = _rows(x, "x", None, half)
     dev, n = x.device, x.shape[0]
@@ -183,7 +190,7 @@ def rope(x, positions, table, interleaved: bool = False, inverse: bool = False, 
     py, yt, yh = _rows(out, "out", dev, (x.dtype,), x.shape)
     _on_gpu(x)
     st = _library().sph_rope(ctypes.byref(desc), SPH_F16 if x.dtype is torch.float16 else SPH_F32, n, x.shape[1], x.shape[2],
-                             px, xt, xh, pos, py, yt, yh, _stream_handle(stream))
+                             px, xt, xh, pos, py, yt, yh, _stream_handle())
     _check(st, "sph_rope")
     return out
 
@@ -285,6 +292,9 @@ def kv_append(cache: KVCache, k, v, slots, positions=None, table=None, interleav
     ``table`` and ``positions`` the keys are rotated on the way, and so are the queries q [tokens][q heads][channels] in
     the same launch. Returns the rotated queries in fp16 (``q_out`` or a new tensor; None without q)."""
     import torch
+    if stream is not None:                      # what is made for the call belongs to its stream
+        with torch.cuda.stream(stream):
+            return kv_append(cache, k, v, slots, positions, table, interleaved, q, q_out)
     dev = cache.device
     dt = (k.dtype,) if isinstance(k, torch.Tensor) and k.dtype is torch.float16 else (torch.float32,)
     n = k.shape[0] if isinstance(k, torch.Tensor) and k.dim() else 0
@@ -309,7 +319,7 @@ def kv_append(cache: KVCache, k, v, slots, positions=None, table=None, interleav
         po, ot, oh = _rows(q_out, "q_out", dev, (torch.float16,), shape)
     _on_gpu(k)
     st = _library().sph_kv_append(cache._ref, desc, SPH_F16 if dt[0] is torch.float16 else SPH_F32, n, pk, kt, kh, pv, vt, vh, ps,
-                                  heads, pq, qt, qh, po, ot, oh, pos, _stream_handle(stream))
+                                  heads, pq, qt, qh, po, ot, oh, pos, _stream_handle())
     _check(st, "sph_kv_append")
     return q_out if q is not None else None
 
@@ -318,6 +328,9 @@ def kv_read(cache: KVCache, slots, out=None, stream=None):
     """The keys and values of int32 ``slots`` as two fp16 tensors [tokens][kv heads][channels]
     (sph_kv_read); rows of slots outside the pool are zero. ``out``: a pair of contiguous tensors."""
     import torch
+    if stream is not None:                      # what is made for the call belongs to its stream
+        with torch.cuda.stream(stream):
+            return kv_read(cache, slots, out)
     dev = cache.device
     ps = _ints(slots, "slots", dev)
     shape = (slots.shape[0], cache.kv_heads, cache.head_dim)
@@ -330,7 +343,7 @@ def kv_read(cache: KVCache, slots, out=None, stream=None):
             if t.dtype != torch.float16 or t.device != dev or t.shape != shape or not t.is_contiguous():
                 raise ValueError(f"out must be two contiguous fp16 tensors of shape {shape} on {dev}")
     _on_gpu(slots)
-    _check(_library().sph_kv_read(cache._ref, shape[0], ps, k.data_ptr(), v.data_ptr(), _stream_handle(stream)), "sph_kv_read")
+    _check(_library().sph_kv_read(cache._ref, shape[0], ps, k.data_ptr(), v.data_ptr(), _stream_handle()), "sph_kv_read")
     return k, v
 
 
@@ -343,39 +356,21 @@ def attention_workspace_bytes(cache: KVCache, batch: int, tokens: int, q_heads: 
     return out.value
 
 
-def _attention_workspace(cache: KVCache, need: int, handle: int, stream):
-    """A workspace of at least ``need`` bytes for calls on the stream ``handle``, kept with the cache; streams do not share
+def _attention_workspace(cache: KVCache, need: int, handle: int):
+    """A workspace of at least ``need`` bytes for calls on the current stream, ``handle``, kept with the cache; streams do not share
     one, since their calls may run together. One that a larger call outgrows is kept, and its successor is twice its size or more: all of
     them together take less than twice the last."""
     import torch
-    if _capturing(stream):
+    if torch.cuda.is_current_stream_capturing():
         # memory of the graph's own pool must not serve later calls outside it
         raise RuntimeError("no workspace of this size on this stream yet: make one call on the capture stream before "
                            "capturing a graph")
     old = cache.workspaces.get(handle)
-    # allocated on the stream that uses it, so that it is freed behind that stream's calls
-    with torch.cuda.stream(stream):
-        ws = torch.empty(need if old is None else max(need, 2 * old.numel()), dtype=torch.uint8, device=cache.device)
+    ws = torch.empty(need if old is None else max(need, 2 * old.numel()), dtype=torch.uint8, device=cache.device)
     if old is not None:
         cache.outgrown.append(old)
     cache.workspaces[handle] = ws
     return ws
-
-
-def _capturing(stream) -> bool:
-    import torch
-    if stream is None:
-        return torch.cuda.is_current_stream_capturing()
-    with torch.cuda.stream(stream):
-        return torch.cuda.is_current_stream_capturing()
-
-
-def _graph_workspace(cache: KVCache, need: int, stream):
-    """A captured call's workspace: from the pool of its graph, whose replays may run beside calls on any stream and beside
-    other graphs. Given back when the call is captured, since only this graph's later calls on the stream get it again."""
-    import torch
-    with torch.cuda.stream(stream):
-        return torch.empty(need, dtype=torch.uint8, device=cache.device)
 
 
 def attention(q, cache: KVCache, pages, seq_lens, q_start=None, max_q: int = 1, max_len: int | None = None, window: int = 0,
@@ -389,6 +384,9 @@ def attention(q, cache: KVCache, pages, seq_lens, q_start=None, max_q: int = 1, 
     (default: what the pages' columns hold). scale: default channels^-0.5. Returns fp16 o like q, with ``return_lse`` also fp32
     [tokens][q heads], the logarithm of each softmax's sum."""
     import torch
+    if stream is not None:                      # what is made for the call belongs to its stream
+        with torch.cuda.stream(stream):
+            return attention(q, cache, pages, seq_lens, q_start, max_q, max_len, window, scale, out, return_lse)
     dev, half = cache.device, (torch.float16,)
     pq, qt, qh = _rows(q, "q", dev, half)
     n, heads, dim = q.shape
@@ -416,7 +414,7 @@ def attention(q, cache: KVCache, pages, seq_lens, q_start=None, max_q: int = 1, 
         po, ot, oh = _rows(out, "out", dev, half, (n, heads, dim))
     lse = torch.empty((n, heads), dtype=torch.float32, device=dev) if return_lse else None
     _on_gpu(q)
-    handle = _stream_handle(stream)
+    handle = _stream_handle()
     ws = cache.workspaces.get(handle)
 
     def call(ws):
@@ -425,15 +423,17 @@ def attention(q, cache: KVCache, pages, seq_lens, q_start=None, max_q: int = 1, 
                                         None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(),
                                         0 if ws is None else ws.numel(), handle)
 
-    if ws is not None and _capturing(stream):
+    if ws is not None and torch.cuda.is_current_stream_capturing():
         need = attention_workspace_bytes(cache, batch, n, heads, max_q, max_len, window)
         if need <= ws.numel():
-            ws = _graph_workspace(cache, need, stream)
+            # in the pool of its graph, whose replays may run beside any call and any other graph: let go when the call is captured, it
+            # serves only later calls of the graph
+            ws = torch.empty(need, dtype=torch.uint8, device=dev)
     st = call(ws)
     if st in (SPH_ERR_NULL, SPH_ERR_BUFFER_TOO_SMALL):
         # the library found, before it launched anything, that it needs a workspace or a larger one
         need = attention_workspace_bytes(cache, batch, n, heads, max_q, max_len, window)
         if need > (0 if ws is None else ws.numel()):
-            st = call(_attention_workspace(cache, need, handle, stream))
+            st = call(_attention_workspace(cache, need, handle))
     _check(st, "sph_attention")
     return (out, lse) if return_lse else out

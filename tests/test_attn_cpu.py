@@ -3,6 +3,7 @@ binding (before any HIP call), the rotary frequencies, and models of the launche
 ragged sequences, and cache blocks spread among query blocks."""
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -228,6 +229,59 @@ def test_binding_refusals():
 def test_a_table_is_made_on_a_gpu_only():
     with pytest.raises(ValueError, match="GPU"):
         pkg.rope_table(64, 10, device="cpu")
+
+
+class _Streams:
+    """Stands for torch.cuda.stream: which stream is current, and on which one each tensor was made."""
+
+    def __init__(self, monkeypatch):
+        self.now, self.made = [None], []
+        monkeypatch.setattr(torch.cuda, "stream", self.stream)
+        monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+        for name in ("empty", "empty_like", "zeros"):
+            monkeypatch.setattr(torch, name, self.recorded(getattr(torch, name)))
+
+    def recorded(self, f):
+        def make(*a, **kw):
+            self.made.append(self.now[-1])
+            return f(*a, **kw)
+        return make
+
+    @contextlib.contextmanager
+    def stream(self, s):
+        self.now.append(self.now[-1] if s is None else s)
+        yield
+        self.now.pop()
+
+
+class _Stream:
+    cuda_stream = 77
+
+
+def test_tensors_made_for_a_stream_are_made_on_it(monkeypatch):
+    """A tensor belongs to the stream that it was made on: the allocator hands its memory to that stream's later work as soon as it is let go, and
+    takes it from that stream's earlier work. So results of a call on another stream than the current one are made on that stream."""
+    class Lib:
+        def __getattr__(self, name):
+            return lambda *a: 0
+    c = _cpu_cache(16)
+    h, kv, pos, tab = torch.zeros(3, 4, 64).half(), torch.zeros(3, 2, 64).half(), torch.zeros(3, dtype=torch.int32), torch.zeros(10, 32, 2)
+    pages = torch.zeros(3, 4, dtype=torch.int32)
+    monkeypatch.setattr(A, "_library", Lib)
+    monkeypatch.setattr(A, "_on_gpu", lambda *t: None)
+    monkeypatch.setattr(A, "_stream_handle", lambda s=None: 77)
+    st, on = _Streams(monkeypatch), _Stream()
+    calls = (lambda **kw: pkg.rope(h, pos, tab, **kw), lambda **kw: pkg.rope(h[:, :2], pos, tab, **kw), lambda **kw: pkg.rope_table(64, 10, device="cpu", **kw),
+             lambda **kw: pkg.kv_append(c, kv, kv, pos, positions=pos, table=tab, q=h, **kw), lambda **kw: pkg.kv_read(c, pos, **kw),
+             lambda **kw: pkg.attention(h, c, pages, pos, return_lse=True, **kw), lambda **kw: pkg.attention(h[:, :2], c, pages, pos, **kw))
+    for f in calls:
+        st.made.clear()
+        f(stream=on)
+        assert st.made and all(s is on for s in st.made)
+    with torch.cuda.stream(on):
+        st.made.clear()
+        A.rope_gradient(h, pos, tab, False)
+        assert st.made == [on]
 
 
 # ------------------------------------------------------------------ rotary frequencies
