@@ -24,14 +24,17 @@ class AttentionBlock:
 
     def __call__(self, x, positions, slots, pages, seq_lens, q_start=None, max_q: int = 1, max_len: int | None = None, stream=None):
         """y fp16 [tokens][hidden] of x fp16 [tokens][hidden], the new tokens of all sequences one after the other. positions, slots:
-        int32 [tokens], where each stands and is kept; pages, seq_lens, q_start, max_q, max_len: as ``attention``."""
+        int32 [tokens], where each stands and is kept; pages, seq_lens, q_start, max_q, max_len, stream: as ``attention``."""
         import torch
+        if stream is not None:                  # so that the rows between the calls, let go at the end, are that stream's
+            with torch.cuda.stream(stream):
+                return self(x, positions, slots, pages, seq_lens, q_start, max_q, max_len)
         h, kv, n = self.q_heads, self.cache.kv_heads, x.shape[0]
-        rows = B.gemm(self.w_qkv, x, out_dtype=torch.float16, stream=stream).view(n, h + 2 * kv, self.cache.head_dim)
+        rows = B.gemm(self.w_qkv, x, out_dtype=torch.float16).view(n, h + 2 * kv, self.cache.head_dim)
         # the queries turn where they are
         q = A.kv_append(self.cache, rows[:, h:h + kv], rows[:, h + kv:], slots, positions=positions, table=self.table,
-                        interleaved=self.interleaved, q=rows[:, :h], q_out=rows[:, :h], stream=stream)
+                        interleaved=self.interleaved, q=rows[:, :h], q_out=rows[:, :h])
         o = torch.empty((n, h, self.cache.head_dim), dtype=torch.float16, device=x.device)
         A.attention(q, self.cache, pages, seq_lens, q_start=q_start, max_q=max_q, max_len=max_len, window=self.window, scale=self.scale,
-                    out=o, stream=stream)
-        return B.gemm(self.w_o, o.view(n, -1), out_dtype=torch.float16, stream=stream)
+                    out=o)
+        return B.gemm(self.w_o, o.view(n, -1), out_dtype=torch.float16)

@@ -284,6 +284,35 @@ def test_tensors_made_for_a_stream_are_made_on_it(monkeypatch):
         assert st.made == [on]
 
 
+def test_a_block_on_a_given_stream_runs_on_it_whole(monkeypatch):
+    """The rows and the outputs between a block's four calls are let go when it returns, before the stream has read them: they have to be
+    that stream's, as its result."""
+    from paper_2609_24875_amd import block as K
+
+    class Weights:
+        def __init__(self, n, k):
+            self.n, self.k = n, k
+
+    st, on, seen = _Streams(monkeypatch), _Stream(), []
+
+    def gemm(w, x, out_dtype=None, stream=None):
+        seen.append((st.now[-1], stream))
+        return torch.empty(x.shape[0], w.n, dtype=out_dtype)
+
+    monkeypatch.setattr(K.B, "gemm", gemm)
+    monkeypatch.setattr(K.A, "kv_append", lambda *a, q=None, stream=None, **kw: seen.append((st.now[-1], stream)) or q)
+    monkeypatch.setattr(K.A, "attention", lambda *a, stream=None, **kw: seen.append((st.now[-1], stream)))
+    block = K.AttentionBlock(Weights(8 * 64, 256), Weights(256, 4 * 64), _cpu_cache(16), None, 4)
+    x = torch.zeros(3, 256).half()
+    st.made.clear()
+    assert block(x, None, None, None, None, stream=on).shape == (3, 256)
+    assert len(seen) == 4 and all(now is on and s in (None, on) for now, s in seen)
+    assert len(st.made) == 3 and all(s is on for s in st.made)
+    seen.clear()
+    block(x, None, None, None, None)
+    assert all(s == (None, None) for s in seen)
+
+
 # ------------------------------------------------------------------ rotary frequencies
 
 def test_rope_frequencies():

@@ -111,6 +111,25 @@ def test_prompts_in_parts_and_token_by_token_give_the_same(bits):
     assert float((steps - whole).square().mean().sqrt()) <= bar
 
 
+def test_block_on_a_stream_of_its_own():
+    """Calls queued on another stream, while tensors of the current one come and go in memory that was let go."""
+    block, _, _ = _block(8)
+    lens = [150, 33]
+    pages = torch.randperm(64, device=DEV)[:2 * 10].reshape(2, 10).int()
+    pos, slots, start = _place(pages, lens, lens)
+    ln = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    xs = [torch.randn(sum(lens), HIDDEN, generator=torch.Generator(DEV).manual_seed(20 + i), device=DEV).half() for i in range(4)]
+    want = [block(x, pos, slots, pages, ln, q_start=start, max_q=150) for x in xs]
+    torch.cuda.synchronize()
+    side, got = torch.cuda.Stream(), []
+    for x in xs:
+        got.append(block(x, pos, slots, pages, ln, q_start=start, max_q=150, stream=side))
+        for n in (HEADS + 2 * KV, HEADS):
+            torch.full((sum(lens), n, DIM), 1e4, dtype=torch.float16, device=DEV)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_block_checks_its_parts():
     block, _, _ = _block()
     for args in ((block.w_o, block.w_o), (block.w_qkv, block.w_qkv)):
