@@ -205,11 +205,14 @@ def workspace_bytes(w: SphWeights, m: int) -> int:
     return out.value
 
 
-def _workspace(w: SphWeights, m: int, device, handle: int):
+def _workspace(w: SphWeights, m: int, device, handle: int, stream=None):
     """Zero-filled workspace for (w, m) on the stream ``handle``, allocated once and kept with the
     weights (the library leaves it zero-filled after every call). Calls on different streams may run
-    concurrently, so each stream gets its own."""
+    concurrently, so each stream gets its own, filled in its own order."""
     import torch
+    if stream is not None and torch.device(device).type != "cpu":
+        with torch.cuda.stream(stream):
+            return _workspace(w, m, device, handle)
     nb = workspace_bytes(w, m)
     if nb == 0:
         return None, 0
@@ -244,7 +247,7 @@ def _launch(fn, what: str, w: SphWeights, m: int, x, args: tuple, stream):
             return
         if st == SPH_ERR_HIP:
             raise SphError(st, what)
-    ws, nb = _workspace(w, m, x.device, handle)
+    ws, nb = _workspace(w, m, x.device, handle, stream)
     _check(fn(desc, *args, ws.data_ptr() if ws is not None else None, nb, handle), what)
 
 

@@ -1,5 +1,6 @@
 """The binding's order of attempts for a decode call: a held workspace (or none, up to batch 32) goes
 to the library at once, everything else asks for the size, allocates and raises as stated."""
+from contextlib import contextmanager
 from types import SimpleNamespace
 
 import pytest
@@ -64,6 +65,27 @@ def test_launch_errors(monkeypatch):
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
     with pytest.raises(RuntimeError, match="capturing a graph"):
         B._launch(_library(512, []), "call", _weights(), 1, SimpleNamespace(device="cpu"), (), STREAM)
+
+
+@pytest.mark.parametrize("stream", [STREAM, None])
+def test_a_workspace_is_cleared_on_the_stream_that_uses_it(monkeypatch, stream):
+    """The clearing is queued where the call is: on another stream nothing would order the two."""
+    now, made = [None], []
+
+    @contextmanager
+    def on(s):
+        now.append(s)
+        yield
+        now.pop()
+
+    zeros = torch.zeros
+    monkeypatch.setattr(B, "workspace_bytes", lambda w, m: 512)
+    monkeypatch.setattr(B, "_stream_handle", lambda s=None: 77)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch, "zeros", lambda *a, device=None, **kw: made.append((now[-1], device)) or zeros(*a, **kw))
+    B._launch(_library(512, []), "call", _weights(), 1, SimpleNamespace(device="cuda:0"), (), stream)
+    assert made == [(stream, "cuda:0")]
 
 
 @pytest.mark.parametrize("missing", [None, "_cuda_getCurrentRawStream", "_cuda_getDevice"])
