@@ -152,8 +152,11 @@ def _rope_desc(table, device, interleaved: bool, inverse: bool) -> CRope:
 
 
 def _on_gpu(t):
+    import torch
     if not t.is_cuda:
         raise ValueError(f"tensors must be on a GPU, not on {t.device}")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
 
 
 def _new(x):

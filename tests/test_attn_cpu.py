@@ -231,6 +231,22 @@ def test_a_table_is_made_on_a_gpu_only():
         pkg.rope_table(64, 10, device="cpu")
 
 
+def test_calls_on_another_gpu_than_the_current_one_are_refused(monkeypatch):
+    """The launch goes to the current device, where another device's addresses mean nothing."""
+    class Tensor:
+        is_cuda, device = True, "cuda:1"
+
+        def get_device(self):
+            return 1
+    for now in (1, 0):
+        monkeypatch.setattr(torch.cuda, "current_device", lambda: now)
+        if now:
+            A._on_gpu(Tensor())
+        else:
+            with pytest.raises(ValueError, match="cuda:1"):
+                A._on_gpu(Tensor())
+
+
 class _Streams:
     """Stands for torch.cuda.stream: which stream is current, and on which one each tensor was made."""
 
