@@ -46,8 +46,27 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves;
 
 // Weights are exp2(score - m + kLift), m a maximum that is raised, and o and l scaled down, only when a score passes it by kRise: up to 2^15,
 // inside fp16's range, and at full precision down to 2^-25 of m's, since those that fp16 loses would be missing from o and not from l.
-// Rises of 2, 4 and 8 (lifts to match): 2048 tokens over themselves 63.7, 62.3 and 62.0 us, 4096 of 192 channels 365, 348 and 335, single tokens alike.
+// Rises of 4 and 8 (lifts to match): 2048 tokens over themselves 62.3 and 62.0 us, 4096 of 192 channels 354 and 343, single tokens alike.
 constexpr float kRise = 4.0f, kLift = 11.0f;
+// Scores from here on are so far apart in fp32 (2^-3 and more) that a weight could end up above fp16's range: they are compared without a rise
+// or a lift, and rounded before the maximum is subtracted.
+constexpr float kFar = 1 << 20;
+
+// A row's reference: weights are exp2(score - base), base 0 at first. It has to be raised where a score passes `top` (at first -inf).
+struct Ref {
+  float top, base;
+  // To the score mn, where that raises it (so that what the sums are scaled by, `keep`, never grows them).
+  __device__ __forceinline__ bool raise(float mn, float& keep) {
+    const bool near = fabsf(mn) < kFar;
+    const float to = near ? mn - kLift : mn, from = log();
+    if (!(to > from)) return false;
+    keep = __builtin_amdgcn_exp2f(from - to);
+    top = near ? mn + kRise : mn, base = to;
+    return true;
+  }
+  // what the sum of the weights is relative to: -inf with no score yet
+  __device__ __forceinline__ float log() const { return top == -INFINITY ? -INFINITY : base; }
+};
 
 // The queries of one sequence: tokens start .. end - 1.
 struct Seq {

@@ -174,9 +174,10 @@ __device__ __forceinline__ void attend(const AttnArgs& a, char* lds, float2 (*ml
   int pos[NB];
   bool odd = false;
   f32x4 o[NB][DIM / 16] = {};
-  float m[NB], base[NB], l[NB];
+  Ref ref[NB];
+  float l[NB];
 #pragma unroll
-  for (int n = 0; n < NB; ++n) m[n] = -INFINITY, base[n] = 0.0f, l[n] = 0.0f;
+  for (int n = 0; n < NB; ++n) ref[n] = {-INFINITY, 0.0f}, l[n] = 0.0f;
   const int t0 = (k_lo & ~(kTile - 1)) + kTile * wave;
   if (t0 < k_hi) {
     f16x8 q[NB][L::kSteps];
@@ -283,18 +284,16 @@ __device__ __forceinline__ void attend(const AttnArgs& a, char* lds, float2 (*ml
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) top[n] = fmaxf(top[n], x[n][i]);
-        rise |= top[n] > m[n] + kRise;
+        rise |= top[n] > ref[n].top;
       }
       if (__any(rise)) {
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
-          float mn = fmaxf(m[n], top[n]);
+          float mn = top[n];
           mn = fmaxf(mn, __shfl_xor(mn, 16));
           mn = fmaxf(mn, __shfl_xor(mn, 32));
-          const float ref = mn == -INFINITY ? 0.0f : mn;
-          const float keep = __builtin_amdgcn_exp2f(m[n] - ref);
-          base[n] = ref - kLift;
-          m[n] = mn;
+          float keep;
+          if (!ref[n].raise(mn, keep)) continue;
           l[n] *= keep;
 #pragma unroll
           for (int i = 0; i < DIM / 16; ++i) o[n][i] *= keep;
@@ -304,7 +303,9 @@ __device__ __forceinline__ void attend(const AttnArgs& a, char* lds, float2 (*ml
       for (int n = 0; n < NB; ++n)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          x[n][i] = __builtin_amdgcn_exp2f(x[n][i] - base[n]);
+          // of the rounded score, as the reference was: not fused with its product
+#pragma clang fp contract(off)
+          x[n][i] = __builtin_amdgcn_exp2f(x[n][i] - ref[n].base);
           l[n] += x[n][i];
           p[n][i] = (_Float16)x[n][i];
         }
@@ -354,7 +355,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, char* lds, float2 (*ml
   float* os = (float*)lds + wave * kRows * kOStride;
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
-    if (g4 == 0) ml_s[wave][16 * n + col] = make_float2(m[n] - kLift, l[n]);
+    if (g4 == 0) ml_s[wave][16 * n + col] = make_float2(ref[n].log(), l[n]);
 #pragma unroll
     for (int i = 0; i < DIM / 16; ++i) *(f32x4*)(os + (16 * n + col) * kOStride + 16 * i + 4 * g4) = o[n][i];
   }

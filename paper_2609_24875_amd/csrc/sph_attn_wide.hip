@@ -174,8 +174,9 @@ __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(At
   const int r = r0 + min(w0 + col, nrow - 1), t = r / a.group, head = kvh * a.group + r % a.group, pos = first + t;
   const int wave_lo = first + (r0 + min(w0, nrow - 1)) / a.group, wave_hi = first + (r0 + min(w0 + 31, nrow - 1)) / a.group;
   f32x16 o[kBlocks] = {};
-  float m = -INFINITY, base = 0.0f, l = 0.0f;
-  bool odd = false;
+  Ref ref = {-INFINITY, 0.0f};
+  float l = 0.0f;
+  bool odd = false, far = false;
   if (k_lo < k_hi) {
     // |scale| is applied to the scores, its sign to the queries
     // (a scale of 0 as one that rounds every score to 0, since 0 times the -inf of an unseen key would be NaN)
@@ -268,17 +269,23 @@ __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(At
         for (int u = 0; u < kKeys; ++u)
 #pragma unroll
           for (int i = 0; i < 16; i += 2) top = fmaxf(top, fmaxf(st[u][i], st[u][i + 1]));
-        // -inf times a scale of 0 is NaN, which raises nothing: with nothing seen m stays -inf
-        if (__any(top * scale > m + kRise)) {
-          float mn = fmaxf(m, top * scale);
+        if (__any(top * scale > ref.top)) {
+          float mn = top * scale;
           mn = fmaxf(mn, __shfl_xor(mn, 32));
-          const float ref = mn == -INFINITY ? 0.0f : mn;
-          const float keep = __builtin_amdgcn_exp2f(m - ref);
-          base = ref - kLift;
-          m = mn;
-          l *= keep;
+          float keep;
+          if (ref.raise(mn, keep)) {
+            l *= keep;
 #pragma unroll
-          for (int i = 0; i < kBlocks; ++i) o[i] *= keep;
+            for (int i = 0; i < kBlocks; ++i) o[i] *= keep;
+          }
+          far = __any(fabsf(ref.base) >= kFar);
+        }
+        float by = scale;
+        if (far) {
+          // (a score that is not rounded before the subtraction may lie above a reference that is, by more than fp16 holds)
+#pragma unroll
+          for (int u = 0; u < kKeys; ++u) st[u] *= scale;
+          by = 1.0f;
         }
         // In steps of 16 keys: while a step's products run, the values of the next are read and its weights computed.
         constexpr int kGroups = 2 * kKeys;
@@ -299,7 +306,7 @@ __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(At
         auto weights = [&](int g) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const float x = __builtin_amdgcn_exp2f(fmaf(st[g >> 1][8 * (g & 1) + i], scale, -base));
+            const float x = __builtin_amdgcn_exp2f(fmaf(st[g >> 1][8 * (g & 1) + i], by, -ref.base));
             l += x;
             p[g][i] = (_Float16)x;
           }
@@ -325,7 +332,6 @@ __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(At
       tile_at(kt + kTile, lds_b, lds_a);
     }
     l += __shfl_xor(l, 32);
-    m -= kLift;
   }
   const bool any_odd = __syncthreads_or(odd);
   if (w0 + col >= nrow) return;
@@ -337,9 +343,9 @@ __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(At
       f32x4 acc = {o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]};
       if (any_odd) acc += odd_values<DIM, BITS>(span, pg, pages, pos, ch);
       if (a.splits > 1)
-        write_part(a, split * a.batch + b, kvh, r, ch, acc, m, l);
+        write_part(a, split * a.batch + b, kvh, r, ch, acc, ref.log(), l);
       else
-        write_out(a, s.start + t, head, ch, acc, m, l);
+        write_out(a, s.start + t, head, ch, acc, ref.log(), l);
     }
 }
 

@@ -888,3 +888,63 @@ def test_graphs_captured_on_one_stream_replay_beside_each_other(new):
             eager = call(2)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out + [eager], want))
+
+
+@pytest.mark.parametrize("order", ["rising", "falling", "pairs"])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("size", [1e5, 3e6, 4e7, 1.5e9, 4e12, 1e18])
+@pytest.mark.parametrize("new,group,keys,bits,dim", [(1, 4, 900, 16, 128), (1, 3, 9000, 8, 64), (6, 5, 700, 4, 128), (60, 4, 900, 16, 128),
+                                                     (60, 4, 9000, 8, 64), (200, 2, 900, 16, 192), (70, 4, 900, 4, 96), (130, 2, 700, 16, 256)])
+def test_huge_scores_pick_their_largest(new, group, keys, bits, dim, size, sign, order):
+    """Scores up to `size` that differ by 2^-11 of themselves or not at all: the output is the mean of the largest one's values. A score is one exact
+    product, scaled with a rounding or two of 2^-24, so a gap stays one of at least 40 and other weights are nothing."""
+    c = _cache(bits, dim, 64, -(-keys // 64), 2)
+    step = (torch.arange(keys, device=DEV) * 1023 // (keys - 1) if order != "falling" else 1023 - torch.arange(keys, device=DEV) * 1023 // (keys - 1))
+    if order == "pairs":
+        step = step // 2 * 2
+    k = torch.zeros(keys, 2, dim, dtype=torch.float16, device=DEV)
+    k[:, :, 0] = (1024.0 + step)[:, None].half()
+    v = _randn(keys, 2, dim, seed=230)
+    slots = torch.arange(keys, device=DEV).int()
+    pkg.kv_append(c, k, v, slots)
+    keys_, values = pkg.kv_read(c, slots)
+    pages = torch.arange(c.n_pages, device=DEV).int()[None]
+    q = torch.zeros(new, 2 * group, dim, dtype=torch.float16, device=DEV)
+    q[:, :, 0] = sign * 1024.0
+    scale = size / 2.0 ** 21
+    o, lse = pkg.attention(q, c, pages, _i32([keys]), q_start=_i32([0, new]), max_q=new, max_len=keys, scale=scale, return_lse=True)
+    s = keys_[:, :, 0].double() * sign * 1024.0 * float(np.float32(scale))    # [keys][kv heads]
+    for t in range(new):
+        p = keys - new + t + 1
+        top = s[:p].amax(0)
+        w = (s[:p] == top).double()
+        ref = (w[..., None] * values[:p].double()).sum(0) / w.sum(0)[:, None]
+        mag = (w[..., None] * values[:p].double().abs()).sum(0) / w.sum(0)[:, None]
+        ref, mag, top = (x.repeat_interleave(group, 0) for x in (ref, mag, top))
+        assert ((o[t].double() - ref).abs() <= 2.0 ** -11 * ref.abs() + 2.0 ** -25 + mag * (2.0 ** -11 + 2.0 ** -18)).all()
+        assert ((lse[t].double() - top).abs() <= 2.0 ** -21 * top.abs() + 12.0).all()
+
+
+@pytest.mark.parametrize("falling", [False, True])
+@pytest.mark.parametrize("new,group,keys,bits,dim", [(1, 4, 500, 16, 128), (8, 4, 500, 8, 64), (1, 4, 20000, 16, 64), (60, 4, 500, 16, 128), (60, 4, 500, 4, 96),
+                                                     (150, 2, 500, 8, 192), (60, 8, 9000, 16, 64)])
+def test_huge_scores_that_hardly_differ(new, group, keys, bits, dim, falling):
+    """Scores of 2^20 to 2^37 that rise or fall by a few of their own roundings from key to key: whatever weights that leaves, they are finite and the mean of
+    equal values is that value, to the weights' and the output's rounding."""
+    pages = torch.arange(-(-keys // 64), device=DEV).int()[None]
+    c = _cache(bits, dim, 64, pages.shape[1], 2)
+    k = torch.zeros(keys, 2, dim, dtype=torch.float16, device=DEV)
+    at = torch.arange(keys, device=DEV)
+    k[:, :, 0] = 4096.0
+    k[:, :, 32] = ((keys - at if falling else at) * 500 // keys // 4)[:, None]
+    pkg.kv_append(c, k, torch.full_like(k, 1.5), torch.arange(keys, device=DEV).int())
+    q = torch.zeros(new, 2 * group, dim, dtype=torch.float16, device=DEV)
+    for log in range(8, 26):
+        for sign in (1.0, -1.0):
+            for small in (0.5, 2.0, 8.0):
+                q[:, :, 0], q[:, :, 32] = sign * 2.0 ** min(log, 15), small
+                o, lse = pkg.attention(q, c, pages, _i32([keys]), q_start=_i32([0, new]), max_q=new, max_len=keys, scale=2.0 ** (log - min(log, 15)),
+                                       return_lse=True)
+                assert bool(((o.double() - 1.5).abs() <= 1.5 * 2.0 ** -10).all()), (log, sign, small)
+                top = sign * 2.0 ** (log + 12)
+                assert bool(((lse - top).abs() <= 2.0 ** -20 * abs(top) + 1100 * 2.0 ** (log - min(log, 15))).all())
