@@ -44,13 +44,15 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 
-// Weights are exp2(score - m + kLift), m a maximum that is raised, and o and l scaled down, only when a score passes it by kRise: up to 2^15,
+// Weights are exp2(score - m + kLift), m a maximum that is raised, and o and l scaled down, only when a score passes it by kRise: below 2^16,
 // inside fp16's range, and at full precision down to 2^-25 of m's, since those that fp16 loses would be missing from o and not from l.
-// Rises of 4 and 8 (lifts to match): 2048 tokens over themselves 62.3 and 62.0 us, 4096 of 192 channels 354 and 343, single tokens alike.
-constexpr float kRise = 4.0f, kLift = 11.0f;
-// Scores from here on are so far apart in fp32 (2^-3 and more) that a weight could end up above fp16's range: they are compared without a rise
+// Against a rise of 8 with a lift of 7: 2048 tokens over themselves 61.9 and 62.1 us, 4096 of 192 channels 351 and 346, of 256 531 and 518, single tokens
+// alike.
+constexpr float kRise = 4.75f, kLift = 11.0f;
+static_assert(kRise + kLift < 15.9f, "fp16's range, and room for three roundings of scores below kFar");
+// Scores from here on are so far apart in fp32 (2^-6 and more) that a weight could end up above fp16's range: they are compared without a rise
 // or a lift, and rounded before the maximum is subtracted.
-constexpr float kFar = 1 << 20;
+constexpr float kFar = 1 << 17;
 
 // A row's reference: weights are exp2(score - base), base 0 at first. It has to be raised where a score passes `top` (at first -inf).
 struct Ref {

@@ -447,7 +447,8 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 64 ? 3 : DIM * NB <= 128 ? (
     if (a.shares >= 2 * a.batch) {
       // Shares to spare: each is a stretch of one sequence, ceil(tiles / per) stretches a sequence. This many tiles always suffice:
       per = max(kWaves, (total + a.shares - a.batch - 1) / (a.shares - a.batch));
-      // Where that is a wave's step above the mean or more, the least of four smaller numbers that does, too.
+      // Where that is a wave's step above the mean or more, the least of four smaller numbers that does, too (16 sequences of 32768 tokens at 4 bits
+      // under 40 query heads 130 us, without 139; one, two or three long sequences within 1%).
       if ((int64_t)total * a.batch > (int64_t)kWaves * a.shares * (a.shares - a.batch)) {
         constexpr int kTry[4] = {8, 9, 10, 12};              // eighths of the mean
 #pragma unroll
@@ -632,9 +633,9 @@ Plan plan_of(const sph_kv_cache* c, int64_t batch, int q_heads, int64_t max_q, i
     p.splits = (int)std::max<int64_t>(1, (span + p.chunk - 1) / p.chunk);
     if (p.splits > 1) slots = p.splits * batch;
     // All workgroups resident at once, two on some CUs (the i-th and the (i + 256)-th; of 64 channels a CU takes more, of 192 one): long
-    // rows share theirs with short ones. 8 kv heads of 128 channels, so and with the longest first, fp16: prompts of 2048 tokens 63.2 and 66.3 us,
-    // 1536 48.0 and 50.1, four of 512 26.7 and 30.3, 1300 behind 6700 others 233 and 241; four of 500 at 8 bits 30.4 and 35.1; 2048 of 96
-    // channels 50.4 and 51.4, of 64 42.6 and 42.1.
+    // rows share theirs with short ones. 8 kv heads of 128 channels, so and with the longest first, fp16: prompts of 2048 tokens 62.0 and 65.0 us,
+    // 1536 46.3 and 47.9, four of 512 26.8 and 30.1, 1300 behind 6700 others 236 and 243; four of 500 at 8 bits 30.7 and 35.6; 2048 of 96
+    // channels 51.1 and 52.6, of 64 43.2 and 43.3.
     if (c->head_dim > 64 && c->head_dim <= 128 && p.splits == 1 && kCus % c->kv_heads == 0 && units > kCus && units <= 2 * kCus)
       p.fold = kCus / c->kv_heads;
   }

@@ -11,12 +11,12 @@ namespace {
 
 template <int DIM, int BITS>
 struct Wide {
-  // Keys of a tile: 64 where the scores of so many leave room for the output's registers (4096 tokens of 32 heads of 192 channels: 374 us,
-  // with 32 434).
+  // Keys of a tile: 64 where the scores of so many leave room for the output's registers (4096 tokens of 32 heads of 192 channels: 351 us,
+  // with 32 425).
   static constexpr int kTile = DIM <= 192 ? 64 : 32;
   // Codes are loaded a whole tile ahead where they fit the registers, else when the tile before begins: held through the weights'
   // products, 8-bit codes of 128 and 256 channels spill, and at 64 channels cost the third wave a SIMD (4096 tokens of 32 heads with either:
-  // 4 bits, 64 channels 144 and 131 us, 128 212 and 222, 256 599 and 632; 8 bits, 128 228 and 224).
+  // 4 bits, 64 channels 144 and 130 us, 128 211 and 220, 192 430 and 444, 256 648 and 666; 8 bits, 128 226 and 224, 192 434 and 432, 256 660 and 653).
   static constexpr bool kAhead = BITS == 4 && DIM > 64;
   static constexpr int kPer = DIM / 8;                       // pieces of eight channels in a row
   static constexpr int kPieces = kTile * kPer / kThreads;    // a thread's share of a tile's keys, and of its values
@@ -126,9 +126,10 @@ __device__ __forceinline__ bool clean_share(char* lds, int kt, int k_lo, int k_h
 }
 
 // What bounds it: matrix products and exponentials together, on two waves a SIMD (one above 128 channels). 2048 new tokens behind 14336
-// others, 32 query heads over 8 kv heads of 128 channels, fp16: 579 us, 890 TFLOP/s at a clock that the products lower to about 2.0 GHz; MFMA
+// others, 32 query heads over 8 kv heads of 128 channels, fp16: 577 to 602 us from card to card, 890 to 855 TFLOP/s at a clock
+// that the products lower to about 2.0 GHz; MFMA
 // 40%, vector ALU 42%, LDS 25% busy, no bank conflicts. Twice the rows a wave halve its LDS reads, but leave one wave a SIMD, which
-// does not overlap its products with its weights well enough: 920 us. 4096 tokens over themselves at 8 bits 226 us, 4 bits 214, fp16 197.
+// does not overlap its products with its weights well enough: 920 us. 4096 tokens over themselves at 8 bits 224 us, 4 bits 211, fp16 185.
 template <int DIM, int BITS>
 __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(AttnArgs) {
   const AttnArgs& a = *(const AttnArgs*)__builtin_amdgcn_kernarg_segment_ptr();
@@ -269,7 +270,9 @@ __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(At
         for (int u = 0; u < kKeys; ++u)
 #pragma unroll
           for (int i = 0; i < 16; i += 2) top = fmaxf(top, fmaxf(st[u][i], st[u][i + 1]));
-        if (__any(top * scale > ref.top)) {
+        // (far scores are rounded here: one that is not before the subtraction may lie above a reference that is, by more than fp16 holds)
+        float by = scale;
+        if (far | __any(top * scale > ref.top)) {
           float mn = top * scale;
           mn = fmaxf(mn, __shfl_xor(mn, 32));
           float keep;
@@ -279,13 +282,11 @@ __global__ __launch_bounds__(kThreads, (DIM <= 128 ? 2 : 1)) void k_attn_wide(At
             for (int i = 0; i < kBlocks; ++i) o[i] *= keep;
           }
           far = __any(fabsf(ref.base) >= kFar);
-        }
-        float by = scale;
-        if (far) {
-          // (a score that is not rounded before the subtraction may lie above a reference that is, by more than fp16 holds)
+          if (far) {
 #pragma unroll
-          for (int u = 0; u < kKeys; ++u) st[u] *= scale;
-          by = 1.0f;
+            for (int u = 0; u < kKeys; ++u) st[u] *= scale;
+            by = 1.0f;
+          }
         }
         // In steps of 16 keys: while a step's products run, the values of the next are read and its weights computed.
         constexpr int kGroups = 2 * kKeys;
