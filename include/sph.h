@@ -379,8 +379,8 @@ sph_status sph_kv_read(const sph_kv_cache* cache, int64_t tokens, const int32_t*
  * first): sequence b has d_seq_lens[b] tokens (0..max_len), of which the last n_b are new and ask. Token j of the
  * sequence is slot d_pages[b * pages_stride + j / page_size] * page_size + j % page_size. The query at
  * position p sees the tokens j <= p, and with window > 0 only j > p - window; o = sum_j softmax_j(scale
- * q.k_j) v_j, with query head h reading kv head h / (q_heads / kv_heads). A query that sees nothing
- * gets zeros. Scores, the softmax's maximum and sum and the output are held in fp32; the weights
+ * q.k_j) v_j, with query head h reading kv head h / (q_heads / kv_heads). A query that sees nothing,
+ * or whose every score is -inf, gets zeros. Scores, the softmax's maximum and sum and the output are held in fp32; the weights
  * exp(s - max) are rounded to fp16 for the matrix cores, lifted so that those down to 2^-25 of the largest keep 11 bits and none
  * is off by more than 2^-36 of it.
  *
@@ -389,7 +389,9 @@ sph_status sph_kv_read(const sph_kv_cache* cache, int64_t tokens, const int32_t*
  * max_q = 1 and tokens = batch: one each. d_seq_lens: device int32[batch]; d_pages: device int32[batch][pages_stride], at least
  * ceil(max_len / page_size) entries each, of which only those below the sequence's length are read. max_len (0..2^30): the
  * host's bound of the lengths; the launch is planned for it. batch is 0..65536 and max_q 1..2^24; SPH_ERR_SHAPE, from the workspace
- * query too, where batch * kv_heads * ceil(max_q * group / 128) passes a launch's 2^24 workgroups. d_lse: device fp32[tokens][q_heads], natural
+ * query too, where batch * kv_heads * ceil(max_q * group / 128) passes a launch's 2^24 workgroups. With up to 32 rows (max_q * group; 16 above 128
+ * channels) a kv head and up to 512 sequences, keys are shared out by the lengths that the device holds; more sequences are a workgroup each
+ * and kv head, however long, and more rows are shared out by max_q and max_len, which are therefore better close to the truth. d_lse: device fp32[tokens][q_heads], natural
  * logarithm of sum_j exp(scale q.k_j) (-inf where nothing is seen), or NULL. scale must be finite. d_ws: at
  * least sph_attention_workspace_bytes, 256-byte aligned, no initial contents; concurrent calls must not share one.
  * Keys and values that no query sees are never used, whatever they hold. Queries of a sequence whose length is outside 0..max_len, whose start and count are

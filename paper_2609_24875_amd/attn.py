@@ -222,7 +222,8 @@ class KVCache:
     ([..][channels * bits / 8]) and ``k_par``, ``v_par`` fp16 [pages][kv heads][tokens a page][channels / 32][2]
     of (offset, step). Any strides of the first three dimensions that keep rows 16-byte aligned and are the
     same for keys and values, so both may be views of one allocation or of another order. The handle keeps the
-    attention's workspaces, one a stream, and those that larger calls have outgrown; calls that a graph captures (``torch.cuda.graph``)
+    attention's workspaces (``attention_workspace_bytes``: a few MB for decode steps, tens for drafts behind long caches), one a stream,
+    and those that larger calls have outgrown; calls that a graph captures (``torch.cuda.graph``)
     have theirs in the graph's memory pool, so that its replays need no order with other calls' or other graphs'."""
 
     def __init__(self, k, v, k_par=None, v_par=None, bits: int = 16):

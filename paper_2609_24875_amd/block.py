@@ -10,7 +10,8 @@ from . import sph as B
 class AttentionBlock:
     """``w_qkv``: packed [(q heads + 2 kv heads) * channels][hidden], the rows of q, k and v one under the
     other; ``w_o``: packed [hidden][q heads * channels]; ``cache``: this layer's pages; ``table``: rotary positions
-    (``rope_table``), shared by all layers."""
+    (``rope_table``), shared by all layers. Graphs of a block use the products' workspaces of the stream that captured them, as graphs of
+    ``gemm`` do, so their replays are ordered with each other and with the block's calls on that stream."""
 
     def __init__(self, w_qkv: B.SphWeights, w_o: B.SphWeights, cache: A.KVCache, table, q_heads: int, interleaved: bool = False,
                  window: int = 0, scale: float | None = None):

@@ -208,7 +208,8 @@ def workspace_bytes(w: SphWeights, m: int) -> int:
 def _workspace(w: SphWeights, m: int, device, handle: int, stream=None):
     """Zero-filled workspace for (w, m) on the stream ``handle``, allocated once and kept with the
     weights (the library leaves it zero-filled after every call). Calls on different streams may run
-    concurrently, so each stream gets its own, filled in its own order."""
+    concurrently, so each stream gets its own, filled in its own order. A captured call keeps that of
+    its capture stream wherever it is replayed: replays are ordered with that stream's calls."""
     import torch
     if stream is not None and torch.device(device).type != "cpu":
         with torch.cuda.stream(stream):
