@@ -948,3 +948,34 @@ def test_huge_scores_that_hardly_differ(new, group, keys, bits, dim, falling):
                 assert bool(((o.double() - 1.5).abs() <= 1.5 * 2.0 ** -10).all()), (log, sign, small)
                 top = sign * 2.0 ** (log + 12)
                 assert bool(((lse - top).abs() <= 2.0 ** -20 * abs(top) + 1100 * 2.0 ** (log - min(log, 15))).all())
+
+
+@pytest.mark.parametrize("new,group,bits", FORMS)
+def test_rows_whose_every_score_is_minus_infinity(new, group, bits):
+    """An infinite query over keys of the other sign: exp(-inf) is 0 and so are the sum and the output; one key of its own sign is +inf
+    and makes NaN of the rows that see it; the rows beside them keep theirs."""
+    lens = [new + 300, new + 20]
+    c = _cache(bits, 64, 16, 2 * 32, 1)
+    keys, values = _fill(c, 240)
+    n = c.n_pages * 16
+    k = keys.clone()
+    k[:, :, 0] = -1.0 - k[:, :, 0].abs()
+    pkg.kv_append(c, k, values, torch.arange(n, device=DEV).int())
+    pages, slots = _tables(c, lens, 241, 32)
+    q = _randn(2 * new, group, 64, seed=242)
+    start = _i32([0, new, 2 * new])
+    kw = dict(q_start=start, max_q=new, max_len=512, return_lse=True)
+    o, lse = pkg.attention(q, c, pages, _i32(lens), **kw)
+    hot = torch.arange(2 * new, device=DEV) % 3 == 0
+    q2 = q.clone()
+    q2[hot, :, 0] = INF
+    x, y = pkg.attention(q2, c, pages, _i32(lens), **kw)
+    assert not x[hot].any() and torch.isneginf(y[hot]).all()
+    assert torch.equal(x[~hot], o[~hot]) and torch.equal(y[~hot], lse[~hot])
+    own = k.clone()
+    own[slots[0][5], :, 0] = 1.0                                 # an early key of the first sequence
+    pkg.kv_append(c, own, values, torch.arange(n, device=DEV).int())
+    x, y = pkg.attention(q2, c, pages, _i32(lens), **kw)
+    first = torch.arange(2 * new, device=DEV) < new
+    assert torch.isnan(x[hot & first]).all() and torch.isnan(y[hot & first]).all()
+    assert not x[hot & ~first].any() and torch.isfinite(x[~hot]).all()
