@@ -335,6 +335,15 @@ sph_status sph_rope(const sph_rope_desc* rope, sph_dtype dtype, int64_t tokens, 
                     const void* d_x, int64_t x_token_stride, int64_t x_head_stride, const int32_t* d_pos, void* d_y,
                     int64_t y_token_stride, int64_t y_head_stride, void* stream);
 
+/* sph_rope with positions along several axes, as images and videos have them: pair i of a row turns by the angles that the table has for
+ * the token's position along axis d_axes[i] (device uint8[rot_dim/2], 8-byte aligned). n_axes: 1..16; d_pos: device int32[n_axes], each
+ * axis's `tokens` positions pos_stride (0 and more) elements behind the last one's. The table's frequencies are per pair, so axes may share
+ * one spectrum or have one each. A pair whose position is outside the table, or whose axis is n_axes or more, gets NaN. With one
+ * axis, or positions that agree along all of them, results are sph_rope's, bit for bit. */
+sph_status sph_rope_axes(const sph_rope_desc* rope, const uint8_t* d_axes, int32_t n_axes, int64_t pos_stride, sph_dtype dtype,
+                         int64_t tokens, int32_t heads, int32_t head_dim, const void* d_x, int64_t x_token_stride, int64_t x_head_stride,
+                         const int32_t* d_pos, void* d_y, int64_t y_token_stride, int64_t y_head_stride, void* stream);
+
 /* A key-value cache in pages of page_size tokens: a plain host-side value that describes caller-owned
  * device arrays. Slot s is token s % page_size of page s / page_size. With 16 bits a row of d_k / d_v is
  * head_dim fp16 numbers. With 8 or 4 bits it is head_dim codes (bytes; at 4 bits the 32-bit word w of a row
@@ -369,6 +378,13 @@ sph_status sph_kv_append(const sph_kv_cache* cache, const sph_rope_desc* rope, s
                          int64_t v_token_stride, int64_t v_head_stride, const int32_t* d_slots, int32_t q_heads,
                          const void* d_q, int64_t q_token_stride, int64_t q_head_stride, void* d_q_out,
                          int64_t qo_token_stride, int64_t qo_head_stride, const int32_t* d_pos, void* stream);
+
+/* sph_kv_append with positions along several axes: d_axes, n_axes, pos_stride and d_pos as in sph_rope_axes; rope must not be NULL. */
+sph_status sph_kv_append_axes(const sph_kv_cache* cache, const sph_rope_desc* rope, const uint8_t* d_axes, int32_t n_axes,
+                              int64_t pos_stride, sph_dtype dtype, int64_t tokens, const void* d_k, int64_t k_token_stride,
+                              int64_t k_head_stride, const void* d_v, int64_t v_token_stride, int64_t v_head_stride,
+                              const int32_t* d_slots, int32_t q_heads, const void* d_q, int64_t q_token_stride, int64_t q_head_stride,
+                              void* d_q_out, int64_t qo_token_stride, int64_t qo_head_stride, const int32_t* d_pos, void* stream);
 
 /* Read tokens back: d_k_out and d_v_out (device fp16[tokens][kv_heads][head_dim], contiguous) receive the
  * rows of the slots d_slots (device int32[tokens], any order, repeats allowed). A slot outside the pool reads as zeros. Asynchronous. */

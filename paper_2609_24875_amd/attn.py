@@ -20,6 +20,7 @@ KV_BITS = (16, 8, 4)
 KV_HEAD_DIMS = (64, 96, 128, 192, 256)
 SPH_ERR_NULL, SPH_ERR_BUFFER_TOO_SMALL = 1, 6
 KV_GROUP = 32                       # channels that share an offset and a step
+MAX_AXES = 16                       # of a rotation's positions
 
 
 class CRope(ctypes.Structure):
@@ -47,13 +48,15 @@ def _library():
         pr, pc = ctypes.POINTER(CRope), ctypes.POINTER(CKVCache)
         lib.sph_rope_table.argtypes = [I32, I64, ctypes.POINTER(ctypes.c_double), ctypes.c_double, P, P]
         lib.sph_rope.argtypes = [pr, I32, I64, I32, I32, P, I64, I64, P, P, I64, I64, P]
+        lib.sph_rope_axes.argtypes = [pr, P, I32, I64, *lib.sph_rope.argtypes[1:]]
         lib.sph_kv_append.argtypes = [pc, pr, I32, I64, P, I64, I64, P, I64, I64, P, I32, P, I64, I64, P, I64, I64, P, P]
+        lib.sph_kv_append_axes.argtypes = [pc, pr, P, I32, I64, *lib.sph_kv_append.argtypes[2:]]
         lib.sph_kv_read.argtypes = [pc, I64, P, P, P, P]
         lib.sph_attention.argtypes = [pc, I64, I64, I32, P, I64, I64, P, I64, P, I64, P, I64, I64, ctypes.c_float,
                                       P, I64, I64, P, P, SZ, P]
         lib.sph_attention_workspace_bytes.argtypes = [pc, I64, I64, I32, I64, I64, I64, ctypes.POINTER(SZ)]
-        for name in ("sph_rope_table", "sph_rope", "sph_kv_append", "sph_kv_read", "sph_attention",
-                     "sph_attention_workspace_bytes"):
+        for name in ("sph_rope_table", "sph_rope", "sph_rope_axes", "sph_kv_append", "sph_kv_append_axes", "sph_kv_read",
+                     "sph_attention", "sph_attention_workspace_bytes"):
             getattr(lib, name).restype = ctypes.c_int
         _declared = lib
     return _declared
@@ -94,18 +97,69 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none",
     raise ValueError(f"scaling must be none, linear, ntk or yarn, not {scaling!r}")
 
 
-def rope_table(rot_dim: int, max_pos: int, device="cuda", stream=None, **scaling):
-    """fp32 [max_pos][rot_dim/2][2] of (cos, sin) (sph_rope_table); keywords as ``rope_frequencies``."""
+def rope_table(rot_dim: int, max_pos: int, device="cuda", stream=None, frequencies=None, **scaling):
+    """fp32 [max_pos][rot_dim/2][2] of (cos, sin) (sph_rope_table); keywords as ``rope_frequencies``, or ``frequencies``: the angle
+    a position of every pair, for instance of axes with a spectrum each."""
     import torch
     if stream is not None:                      # what is made for the call belongs to its stream
         with torch.cuda.stream(stream):
-            return rope_table(rot_dim, max_pos, device, **scaling)
-    f, magnitude = rope_frequencies(rot_dim, **scaling)
+            return rope_table(rot_dim, max_pos, device, frequencies=frequencies, **scaling)
+    if frequencies is None:
+        f, magnitude = rope_frequencies(rot_dim, **scaling)
+    else:
+        if scaling:
+            raise ValueError("frequencies are given: no scaling")
+        f, magnitude = [float(x) for x in frequencies], 1.0
+        if len(f) != rot_dim // 2:
+            raise ValueError(f"{len(f)} frequencies for {rot_dim // 2} pairs")
     out = torch.empty((max_pos, rot_dim // 2, 2), dtype=torch.float32, device=device)
     _on_gpu(out)
     arr = (ctypes.c_double * len(f))(*f)
     _check(_library().sph_rope_table(rot_dim, max_pos, arr, magnitude, out.data_ptr(), _stream_handle()), "sph_rope_table")
     return out
+
+
+def rope_axes(sections, cycled: bool = False, device="cuda", stream=None):
+    """The axis of every pair, as ``rope`` takes it: uint8 [pairs]. ``sections``: how many pairs each axis turns (1 to 16 axes, a
+    multiple of 8 pairs in all). Axis 0 has the first pairs, axis 1 the next ones and so on, or with ``cycled`` the axes take the pairs in
+    turn, each until its share is used up. For axes with a spectrum each, give ``rope_table`` the frequencies (``frequencies=``) in this order."""
+    import torch
+    left = [int(n) for n in sections]
+    if not 1 <= len(left) <= MAX_AXES or any(n != m or n < 0 for n, m in zip(left, sections)) or sum(left) < 8 or sum(left) % 8:
+        raise ValueError(f"sections must be the pairs of 1 to {MAX_AXES} axes, a multiple of 8 in all, not {sections!r}")
+    axis = []
+    if cycled:
+        while any(left):
+            for a, n in enumerate(left):
+                if n:
+                    left[a] -= 1
+                    axis.append(a)
+    else:
+        axis = [a for a, n in enumerate(left) for _ in range(n)]
+    if stream is not None:                      # what is made for the call belongs to its stream
+        with torch.cuda.stream(stream):
+            return torch.tensor(axis, dtype=torch.uint8, device=device)
+    return torch.tensor(axis, dtype=torch.uint8, device=device)
+
+
+def _axes(axes, positions, table, device, tokens: int):
+    """(axes' pointer, number of axes, elements between their positions, positions' pointer)."""
+    import torch
+    if not isinstance(axes, torch.Tensor) or axes.dtype is not torch.uint8:
+        raise TypeError("axes must be a torch.uint8 tensor")
+    if axes.device != device:
+        raise ValueError(f"axes is on {axes.device}, the rows on {device}")
+    if axes.shape != table.shape[1:2] or not axes.is_contiguous() or axes.data_ptr() % 8:
+        raise ValueError(f"axes must be contiguous [{table.shape[1]}], 8-byte aligned, got shape {tuple(axes.shape)}")
+    if not isinstance(positions, torch.Tensor) or positions.dtype is not torch.int32:
+        raise TypeError("positions must be a torch.int32 tensor")
+    if positions.device != device:
+        raise ValueError(f"positions is on {positions.device}, the rows on {device}")
+    if positions.dim() != 2 or not 1 <= positions.shape[0] <= MAX_AXES or positions.shape[1] != tokens or (tokens > 1 and positions.stride(1) != 1):
+        raise ValueError(f"positions must be [axes][{tokens}] with unit stride along the tokens, got shape {tuple(positions.shape)} and "
+                         f"strides {tuple(positions.stride())}")
+    count = positions.shape[0]
+    return axes.data_ptr(), count, positions.stride(0) if count > 1 else 0, positions.data_ptr()
 
 
 def _ints(t, name: str, device, count: int | None = None):
@@ -175,30 +229,36 @@ def aligned_rows(t):
     return t if ok else t.contiguous()
 
 
-def rope(x, positions, table, interleaved: bool = False, inverse: bool = False, out=None, stream=None):
+def rope(x, positions, table, interleaved: bool = False, inverse: bool = False, out=None, stream=None, axes=None):
     """Rotary positions of device rows x[tokens][heads][channels], fp16 or fp32 (sph_rope): the first
     2 * table.shape[1] channels of each row turn by the angles of its token's position, the others are
     copied. ``inverse`` turns back and is the gradient (``train.rope`` is the differentiable form).
-    ``out`` may be x."""
+    ``out`` may be x. With ``axes`` (``rope_axes``: uint8, the axis of every pair) positions is int32 [axes][tokens], and each pair turns by
+    its own axis's position, as in images and videos (sph_rope_axes)."""
     import torch
     if stream is not None:                      # what is made for the call belongs to its stream
         with torch.cuda.stream(stream):
-            return rope(x, positions, table, interleaved, inverse, out)
+            return rope(x, positions, table, interleaved, inverse, out, axes=axes)
     half = (torch.float16, torch.float32)
     px, xt, xh = _rows(x, "x", None, half)
     dev, n = x.device, x.shape[0]
     desc = _rope_desc(table, dev, interleaved, inverse)
-    pos = _ints(positions, "positions", dev, n)
+    if axes is None:
+        pos = _ints(positions, "positions", dev, n)
+    else:
+        *more, pos = _axes(axes, positions, table, dev, n)
     out = _new(x) if out is None else out
     py, yt, yh = _rows(out, "out", dev, (x.dtype,), x.shape)
     _on_gpu(x)
-    st = _library().sph_rope(ctypes.byref(desc), SPH_F16 if x.dtype is torch.float16 else SPH_F32, n, x.shape[1], x.shape[2],
-                             px, xt, xh, pos, py, yt, yh, _stream_handle())
-    _check(st, "sph_rope")
+    args = (SPH_F16 if x.dtype is torch.float16 else SPH_F32, n, x.shape[1], x.shape[2], px, xt, xh, pos, py, yt, yh, _stream_handle())
+    if axes is None:
+        _check(_library().sph_rope(ctypes.byref(desc), *args), "sph_rope")
+    else:
+        _check(_library().sph_rope_axes(ctypes.byref(desc), *more, *args), "sph_rope_axes")
     return out
 
 
-def rope_gradient(grad, positions, table, interleaved: bool, inverse: bool = False):
+def rope_gradient(grad, positions, table, interleaved: bool, inverse: bool = False, axes=None):
     """The gradient of ``rope``'s rows from that of its result, whose tensors have passed ``rope``'s checks: they are not repeated, since
     Python on autograd's thread costs several times what it does elsewhere."""
     grad = aligned_rows(grad)
@@ -207,10 +267,14 @@ def rope_gradient(grad, positions, table, interleaved: bool, inverse: bool = Fal
     out = _new(grad)
     desc = CRope(table.data_ptr(), table.shape[0], 2 * table.shape[1],
                  (ROPE_INTERLEAVED if interleaved else 0) | (0 if inverse else ROPE_INVERSE))
-    st = _library().sph_rope(ctypes.byref(desc), SPH_F16 if grad.element_size() == 2 else SPH_F32, n, heads, dim, grad.data_ptr(),
-                             gt if n > 1 else 0, gh if heads > 1 else 0, positions.data_ptr(), out.data_ptr(), heads * dim, dim,
-                             _stream_handle())
-    _check(st, "sph_rope")
+    args = (SPH_F16 if grad.element_size() == 2 else SPH_F32, n, heads, dim, grad.data_ptr(), gt if n > 1 else 0, gh if heads > 1 else 0,
+            positions.data_ptr(), out.data_ptr(), heads * dim, dim, _stream_handle())
+    if axes is None:
+        _check(_library().sph_rope(ctypes.byref(desc), *args), "sph_rope")
+    else:
+        count = positions.shape[0]
+        _check(_library().sph_rope_axes(ctypes.byref(desc), axes.data_ptr(), count, positions.stride(0) if count > 1 else 0, *args),
+               "sph_rope_axes")
     return out
 
 
@@ -290,15 +354,16 @@ class KVCache:
         return sum(t.numel() * t.element_size() for t in (self.k, self.v, self.k_par, self.v_par) if t is not None)
 
 
-def kv_append(cache: KVCache, k, v, slots, positions=None, table=None, interleaved: bool = False, q=None, q_out=None, stream=None):
+def kv_append(cache: KVCache, k, v, slots, positions=None, table=None, interleaved: bool = False, q=None, q_out=None, stream=None,
+              axes=None):
     """Write a key and a value row per token and head, k and v [tokens][kv heads][channels] (fp16 or fp32,
     any row strides), to the int32 ``slots`` (sph_kv_append; page * page_size + place in the page, -1 for a padding token). With
     ``table`` and ``positions`` the keys are rotated on the way, and so are the queries q [tokens][q heads][channels] in
-    the same launch. Returns the rotated queries in fp16 (``q_out`` or a new tensor; None without q)."""
+    the same launch. Returns the rotated queries in fp16 (``q_out`` or a new tensor; None without q). ``axes``: as in ``rope``."""
     import torch
     if stream is not None:                      # what is made for the call belongs to its stream
         with torch.cuda.stream(stream):
-            return kv_append(cache, k, v, slots, positions, table, interleaved, q, q_out)
+            return kv_append(cache, k, v, slots, positions, table, interleaved, q, q_out, axes=axes)
     dev = cache.device
     dt = (k.dtype,) if isinstance(k, torch.Tensor) and k.dtype is torch.float16 else (torch.float32,)
     n = k.shape[0] if isinstance(k, torch.Tensor) and k.dim() else 0
@@ -309,9 +374,12 @@ def kv_append(cache: KVCache, k, v, slots, positions=None, table=None, interleav
     desc = pos = None
     if table is not None:
         desc = ctypes.byref(_rope_desc(table, dev, interleaved, False))
-        pos = _ints(positions, "positions", dev, n)
-    elif positions is not None or q is not None:
-        raise ValueError("positions and q need a table")
+        if axes is None:
+            pos = _ints(positions, "positions", dev, n)
+        else:
+            *more, pos = _axes(axes, positions, table, dev, n)
+    elif positions is not None or q is not None or axes is not None:
+        raise ValueError("positions, axes and q need a table")
     pq = po = None
     heads = qt = qh = ot = oh = 0
     if q is not None:
@@ -322,9 +390,12 @@ def kv_append(cache: KVCache, k, v, slots, positions=None, table=None, interleav
             q_out = torch.empty(shape, dtype=torch.float16, device=dev)
         po, ot, oh = _rows(q_out, "q_out", dev, (torch.float16,), shape)
     _on_gpu(k)
-    st = _library().sph_kv_append(cache._ref, desc, SPH_F16 if dt[0] is torch.float16 else SPH_F32, n, pk, kt, kh, pv, vt, vh, ps,
-                                  heads, pq, qt, qh, po, ot, oh, pos, _stream_handle())
-    _check(st, "sph_kv_append")
+    args = (SPH_F16 if dt[0] is torch.float16 else SPH_F32, n, pk, kt, kh, pv, vt, vh, ps, heads, pq, qt, qh, po, ot, oh, pos,
+            _stream_handle())
+    if axes is None:
+        _check(_library().sph_kv_append(cache._ref, desc, *args), "sph_kv_append")
+    else:
+        _check(_library().sph_kv_append_axes(cache._ref, desc, *more, *args), "sph_kv_append_axes")
     return q_out if q is not None else None
 
 

@@ -60,6 +60,33 @@ struct Turn {
   }
 };
 
+// Which axis each pair turns along: a byte a pair, and the axes' positions, `stride` tokens apart. `of` is NULL where all pairs have one.
+struct Axes {
+  const uint8_t* of;
+  int64_t stride;
+  int count;
+};
+
+// As Turn, with each pair at the position along its own axis; NaN too for an axis that there is not. A row's runs mostly lie in one
+// axis's share of the pairs, so that lanes read whole lines of the table; where axes alternate, its pairs come from as many rows.
+template <int N>
+struct TurnAxes : Turn<N> {
+  __device__ __forceinline__ void load(const float* table, int64_t max_pos, int half, const int32_t* pos, const Axes& x, int pair, float sign) {
+    // (pair is a multiple of N)
+    typedef uint8_t Bytes __attribute__((ext_vector_type(N)));
+    const Bytes axis = *(const Bytes*)(x.of + pair);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bool known = axis[i] < x.count;
+      const int p = pos[known ? axis[i] * x.stride : 0];
+      const bool there = known && (unsigned)p < (uint64_t)max_pos;
+      const float one = there ? 1.0f : __builtin_nanf("");
+      const float2 w = ((const float2*)table)[(there ? (int64_t)p : 0) * half + pair + i];
+      this->c[i] = one * w.x, this->s[i] = sign * one * w.y;
+    }
+  }
+};
+
 // One pair turned. Each product is rounded before the sum, so that every path that rotates, whatever the
 // compiler would fuse in it, gives the same bits: keys rotated on their way into the cache get the codes that they
 // would get if they were rotated in fp32 first.
@@ -81,6 +108,7 @@ struct RopeArgs {
   int heads, dim, rot;
   int hpt;                 // heads a thread takes
   float sign;
+  Axes axes;
 };
 
 // One thread rotates two runs of 16 bytes of hpt heads of a token (eight pairs of fp16, four of fp32), each run beside its neighbouring
@@ -88,7 +116,7 @@ struct RopeArgs {
 // are in flight together, past the caches, since each row is read once. STREAM: stores go past them, too, which is faster beside
 // stores of the cache's pages (8192 tokens into 4 bits and back 58.5 us, otherwise 61.5; loads that stay in the caches 62) and
 // slower alone (8192 tokens 41 us, otherwise 35.5; loads that stay 45).
-template <typename T, typename O, bool INTER, bool STREAM>
+template <typename T, typename O, bool INTER, bool STREAM, bool AXES>
 __device__ __forceinline__ void rope_unit(const RopeArgs& a, int64_t token, int unit, int h0) {
   constexpr int N = 16 / sizeof(T);
   typedef T Run __attribute__((ext_vector_type(N)));
@@ -103,7 +131,25 @@ __device__ __forceinline__ void rope_unit(const RopeArgs& a, int64_t token, int 
   }
   const bool turns_a = ca < a.rot, turns_b = cb < a.rot;
   Turn<N> w;
-  if constexpr (INTER) {
+  if constexpr (AXES && INTER) {
+    TurnAxes<N / 2> u;
+    if (turns_a) {
+      u.load(a.table, a.max_pos, half, a.pos + token, a.axes, ca / 2, a.sign);
+#pragma unroll
+      for (int j = 0; j < N / 2; ++j) w.c[j] = u.c[j], w.s[j] = u.s[j];
+    }
+    if (turns_b) {
+      u.load(a.table, a.max_pos, half, a.pos + token, a.axes, cb / 2, a.sign);
+#pragma unroll
+      for (int j = 0; j < N / 2; ++j) w.c[N / 2 + j] = u.c[j], w.s[N / 2 + j] = u.s[j];
+    }
+  } else if constexpr (AXES) {
+    TurnAxes<N> u;
+    if (turns_a) {
+      u.load(a.table, a.max_pos, half, a.pos + token, a.axes, ca, a.sign);
+      w = u;
+    }
+  } else if constexpr (INTER) {
     Turn<N / 2> u;
     if (turns_a) {
       u.load(a.table, a.max_pos, half, a.pos[token], ca / 2, a.sign);
@@ -174,13 +220,13 @@ __device__ __forceinline__ void place(uint32_t block, uint32_t per, int64_t& tok
 
 // Bound by memory: 8192 tokens of 48 heads of 128 fp16 channels 35.5 us (5.7 TB/s read and written), 2051 tokens of 32 heads of
 // 128 fp32 channels, half of them turned, 15 us (4.5 TB/s; a launch of a few tokens takes 3).
-template <typename T, bool INTER>
+template <typename T, bool INTER, bool AXES>
 __global__ __launch_bounds__(kThreads) void k_rope(RopeArgs a) {
   int64_t token;
   uint32_t unit;
   place(blockIdx.x, (uint32_t)a.dim / (32 / sizeof(T)), token, unit);
   if (token >= a.tokens) return;
-  rope_unit<T, T, INTER, false>(a, token, (int)unit, blockIdx.y * a.hpt);
+  rope_unit<T, T, INTER, false, AXES>(a, token, (int)unit, blockIdx.y * a.hpt);
 }
 
 struct RopeFreqs {
@@ -217,7 +263,7 @@ struct AppendArgs {
   // are bound by memory: block i is the (i kv_share / 2^32)-th of them if that number changes behind it.
   uint32_t kv_share;       // 0: all blocks write the cache
   uint32_t q_head_blocks;
-  RopeArgs q;
+  RopeArgs q;              // (its axes are the keys', too)
 };
 
 template <int CTRL>
@@ -236,7 +282,7 @@ __device__ __forceinline__ float quad_max(float v) {
 
 // One thread writes eight channels of one key or value row; four neighbouring lanes share an offset and a step.
 // A rotated key's partner channels are read beside its own.
-template <typename T, int BITS, bool INTER>
+template <typename T, int BITS, bool INTER, bool AXES>
 __device__ __forceinline__ void append_unit(const AppendArgs& a, int64_t token, uint32_t unit) {
   const CacheView& c = a.c;
   const uint32_t per_row = (uint32_t)c.dim / 8, per_kind = per_row * c.kv_heads;
@@ -254,7 +300,12 @@ __device__ __forceinline__ void append_unit(const AppendArgs& a, int64_t token, 
   if (!is_v && a.pos && ch < a.rot) {
     const int half = a.rot / 2;
     Turn<8> w;
-    if (INTER) {
+    if constexpr (AXES && INTER) {
+      TurnAxes<4> u;
+      u.load(a.table, a.max_pos, half, a.pos + token, a.q.axes, ch / 2, a.sign);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) turn(x[2 * j], x[2 * j + 1], u.c[j], u.s[j]);
+    } else if (INTER) {
       // four pairs: the second half of the eight that are loaded is unused and stays inside the row of the table
       const int pair = ch / 2, first = min(pair, half - 8);
       w.load(a.table, a.max_pos, half, a.pos[token], first, a.sign);
@@ -266,7 +317,13 @@ __device__ __forceinline__ void append_unit(const AppendArgs& a, int64_t token, 
       }
     } else {
       const bool low = ch < half;
-      w.load(a.table, a.max_pos, half, a.pos[token], low ? ch : ch - half, a.sign);
+      if constexpr (AXES) {
+        TurnAxes<8> u;
+        u.load(a.table, a.max_pos, half, a.pos + token, a.q.axes, low ? ch : ch - half, a.sign);
+        w = u;
+      } else {
+        w.load(a.table, a.max_pos, half, a.pos[token], low ? ch : ch - half, a.sign);
+      }
       Row8<T> o;
       o.load(row + (low ? ch + half : ch - half) * sizeof(T));
 #pragma unroll
@@ -327,7 +384,7 @@ __device__ __forceinline__ void append_unit(const AppendArgs& a, int64_t token, 
 
 // Bound by memory, and by the arithmetic of the codes beside it: 8192 tokens of 40 query and 8 kv heads of 128 channels into 4 bits 51 us
 // (137 MB read, 97 written: 4.6 TB/s, vector ALU 42% busy); 64 tokens into 8 bits 3.6 us, the launch's latency.
-template <typename T, int BITS, bool INTER>
+template <typename T, int BITS, bool INTER, bool AXES>
 __global__ __launch_bounds__(kThreads) void k_kv_append(AppendArgs a) {
   int64_t token;
   uint32_t unit;
@@ -338,13 +395,13 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(AppendArgs a) {
       const uint32_t q_block = blockIdx.x - kv_block;
       place(q_block / a.q_head_blocks, (uint32_t)a.c.dim / (32 / sizeof(T)), token, unit);
       if (token >= a.tokens) return;
-      rope_unit<T, _Float16, INTER, true>(a.q, token, (int)unit, (int)(q_block % a.q_head_blocks) * a.q.hpt);
+      rope_unit<T, _Float16, INTER, true, AXES>(a.q, token, (int)unit, (int)(q_block % a.q_head_blocks) * a.q.hpt);
       return;
     }
   }
   place(kv_block, (uint32_t)(a.c.dim / 8) * 2 * a.c.kv_heads, token, unit);
   if (token >= a.tokens) return;
-  append_unit<T, BITS, INTER>(a, token, unit);
+  append_unit<T, BITS, INTER, AXES>(a, token, unit);
 }
 
 // ------------------------------------------------------------------ reading
@@ -414,6 +471,31 @@ sph_status check_rope(const sph_rope_desc* r, int head_dim) {
   return SPH_OK;
 }
 
+// The kernel for a type, a way of pairing, and one axis or several.
+template <typename T>
+const void* rope_kernel(bool inter, bool axes) {
+  return inter ? (axes ? (const void*)k_rope<T, true, true> : (const void*)k_rope<T, true, false>)
+               : (axes ? (const void*)k_rope<T, false, true> : (const void*)k_rope<T, false, false>);
+}
+
+template <typename T, int BITS>
+const void* append_kernel(bool inter, bool axes) {
+  return inter ? (axes ? (const void*)k_kv_append<T, BITS, true, true> : (const void*)k_kv_append<T, BITS, true, false>)
+               : (axes ? (const void*)k_kv_append<T, BITS, false, true> : (const void*)k_kv_append<T, BITS, false, false>);
+}
+
+template <typename T>
+const void* append_kernel(int bits, bool inter, bool axes) {
+  return bits == 16 ? append_kernel<T, 16>(inter, axes) : bits == 8 ? append_kernel<T, 8>(inter, axes) : append_kernel<T, 4>(inter, axes);
+}
+
+constexpr int kMaxAxes = 16;
+
+sph_status check_axes(const uint8_t* d_axes, int32_t n_axes, int64_t stride) {
+  if (n_axes < 1 || n_axes > kMaxAxes || (uintptr_t)d_axes % 8 || stride < 0 || stride >= (int64_t(1) << 40)) return SPH_ERR_SHAPE;
+  return d_axes ? SPH_OK : SPH_ERR_NULL;
+}
+
 // 16-byte rows of elements of `size` bytes. Strides are only used by calls with more than one token or head, but have to be aligned always.
 bool rows_ok(const void* p, int64_t ts, int64_t hs, int size) {
   const int64_t lim = int64_t(1) << 40;
@@ -461,24 +543,9 @@ CacheView sph_cache_view(const sph_kv_cache* c) {
   return v;
 }
 
-extern "C" {
+namespace {
 
-sph_status sph_rope_table(int32_t rot_dim, int64_t max_pos, const double* inv_freq, double magnitude, float* d_table,
-                          void* stream) {
-  if (!inv_freq || !d_table) return SPH_ERR_NULL;
-  if (rot_dim < 16 || rot_dim % 16 || rot_dim > 512 || max_pos < 1 || max_pos > INT32_MAX || (uintptr_t)d_table % 16) return SPH_ERR_SHAPE;
-  RopeFreqs f{};
-  for (int i = 0; i < rot_dim / 2; ++i) {
-    if (!std::isfinite(inv_freq[i])) return SPH_ERR_BAD_VALUE;
-    f.f[i] = inv_freq[i];
-  }
-  if (!std::isfinite(magnitude)) return SPH_ERR_BAD_VALUE;
-  uint32_t blocks;
-  if (!blocks_for(max_pos, rot_dim / 2, &blocks)) return SPH_ERR_SHAPE;
-  return launch((const void*)k_rope_table, dim3(blocks), (hipStream_t)stream, f, (int)(rot_dim / 2), max_pos, magnitude, d_table);
-}
-
-sph_status sph_rope(const sph_rope_desc* rope, sph_dtype dtype, int64_t tokens, int32_t heads, int32_t head_dim,
+sph_status rope_call(const sph_rope_desc* rope, const Axes* axes, sph_dtype dtype, int64_t tokens, int32_t heads, int32_t head_dim,
                     const void* d_x, int64_t x_token_stride, int64_t x_head_stride, const int32_t* d_pos, void* d_y,
                     int64_t y_token_stride, int64_t y_head_stride, void* stream) {
   if (!rope) return SPH_ERR_NULL;
@@ -486,6 +553,8 @@ sph_status sph_rope(const sph_rope_desc* rope, sph_dtype dtype, int64_t tokens, 
       head_dim % 16 || head_dim > 512)
     return SPH_ERR_SHAPE;
   if (const sph_status st = check_rope(rope, head_dim)) return st;
+  if (axes)
+    if (const sph_status st = check_axes(axes->of, axes->count, axes->stride)) return st;
   if (tokens == 0) return SPH_OK;
   if (!d_x || !d_y || !d_pos) return SPH_ERR_NULL;
   const int size = dtype == SPH_F16 ? 2 : 4;
@@ -503,13 +572,13 @@ sph_status sph_rope(const sph_rope_desc* rope, sph_dtype dtype, int64_t tokens, 
   uint32_t blocks;
   if (!blocks_for(tokens, units, &blocks)) return SPH_ERR_SHAPE;
   const dim3 grid(blocks, (unsigned)((heads + a.hpt - 1) / a.hpt));
+  if (axes) a.axes = *axes;
   const bool inter = rope->flags & SPH_ROPE_INTERLEAVED;
-  const void* fn = dtype == SPH_F16 ? (inter ? (const void*)k_rope<_Float16, true> : (const void*)k_rope<_Float16, false>)
-                                    : (inter ? (const void*)k_rope<float, true> : (const void*)k_rope<float, false>);
+  const void* fn = dtype == SPH_F16 ? rope_kernel<_Float16>(inter, axes) : rope_kernel<float>(inter, axes);
   return launch(fn, grid, (hipStream_t)stream, a);
 }
 
-sph_status sph_kv_append(const sph_kv_cache* cache, const sph_rope_desc* rope, sph_dtype dtype, int64_t tokens,
+sph_status append_call(const sph_kv_cache* cache, const sph_rope_desc* rope, const Axes* axes, sph_dtype dtype, int64_t tokens,
                          const void* d_k, int64_t k_token_stride, int64_t k_head_stride, const void* d_v,
                          int64_t v_token_stride, int64_t v_head_stride, const int32_t* d_slots, int32_t q_heads,
                          const void* d_q, int64_t q_token_stride, int64_t q_head_stride, void* d_q_out,
@@ -519,6 +588,8 @@ sph_status sph_kv_append(const sph_kv_cache* cache, const sph_rope_desc* rope, s
   if ((dtype != SPH_F16 && dtype != SPH_F32) || !tokens_ok(tokens) || q_heads < 0 || q_heads > 65535) return SPH_ERR_SHAPE;
   if (rope) {
     if (const sph_status st = check_rope(rope, cache->head_dim)) return st;
+    if (axes)
+      if (const sph_status st = check_axes(axes->of, axes->count, axes->stride)) return st;
   } else if (q_heads) {
     return SPH_ERR_NULL;
   }
@@ -561,15 +632,63 @@ sph_status sph_kv_append(const sph_kv_cache* cache, const sph_rope_desc* rope, s
     // rounded up: floor(total * share / 2^32) is kv_blocks, since total < 2^32
     a.kv_share = (uint32_t)((((uint64_t)kv_blocks << 32) + q_blocks + kv_blocks - 1) / (q_blocks + kv_blocks));
   }
-  const void* fn = nullptr;
-#define SPH_PICK(B)                                                                                                    \
-  fn = dtype == SPH_F16 ? (inter ? (const void*)k_kv_append<_Float16, B, true> : (const void*)k_kv_append<_Float16, B, false>) \
-                        : (inter ? (const void*)k_kv_append<float, B, true> : (const void*)k_kv_append<float, B, false>)
-  if (cache->bits == 16) SPH_PICK(16);
-  if (cache->bits == 8) SPH_PICK(8);
-  if (cache->bits == 4) SPH_PICK(4);
-#undef SPH_PICK
+  if (axes) a.q.axes = *axes;
+  const void* fn = dtype == SPH_F16 ? append_kernel<_Float16>(cache->bits, inter, axes) : append_kernel<float>(cache->bits, inter, axes);
   return launch(fn, dim3((uint32_t)q_blocks + kv_blocks), (hipStream_t)stream, a);
+}
+
+}  // namespace
+
+extern "C" {
+
+sph_status sph_rope_table(int32_t rot_dim, int64_t max_pos, const double* inv_freq, double magnitude, float* d_table,
+                          void* stream) {
+  if (!inv_freq || !d_table) return SPH_ERR_NULL;
+  if (rot_dim < 16 || rot_dim % 16 || rot_dim > 512 || max_pos < 1 || max_pos > INT32_MAX || (uintptr_t)d_table % 16) return SPH_ERR_SHAPE;
+  RopeFreqs f{};
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    if (!std::isfinite(inv_freq[i])) return SPH_ERR_BAD_VALUE;
+    f.f[i] = inv_freq[i];
+  }
+  if (!std::isfinite(magnitude)) return SPH_ERR_BAD_VALUE;
+  uint32_t blocks;
+  if (!blocks_for(max_pos, rot_dim / 2, &blocks)) return SPH_ERR_SHAPE;
+  return launch((const void*)k_rope_table, dim3(blocks), (hipStream_t)stream, f, (int)(rot_dim / 2), max_pos, magnitude, d_table);
+}
+
+sph_status sph_rope(const sph_rope_desc* rope, sph_dtype dtype, int64_t tokens, int32_t heads, int32_t head_dim,
+                    const void* d_x, int64_t x_token_stride, int64_t x_head_stride, const int32_t* d_pos, void* d_y,
+                    int64_t y_token_stride, int64_t y_head_stride, void* stream) {
+  return rope_call(rope, nullptr, dtype, tokens, heads, head_dim, d_x, x_token_stride, x_head_stride, d_pos, d_y, y_token_stride,
+                   y_head_stride, stream);
+}
+
+sph_status sph_rope_axes(const sph_rope_desc* rope, const uint8_t* d_axes, int32_t n_axes, int64_t pos_stride, sph_dtype dtype,
+                         int64_t tokens, int32_t heads, int32_t head_dim, const void* d_x, int64_t x_token_stride, int64_t x_head_stride,
+                         const int32_t* d_pos, void* d_y, int64_t y_token_stride, int64_t y_head_stride, void* stream) {
+  const Axes axes = {d_axes, pos_stride, n_axes};
+  return rope_call(rope, &axes, dtype, tokens, heads, head_dim, d_x, x_token_stride, x_head_stride, d_pos, d_y, y_token_stride,
+                   y_head_stride, stream);
+}
+
+sph_status sph_kv_append(const sph_kv_cache* cache, const sph_rope_desc* rope, sph_dtype dtype, int64_t tokens,
+                         const void* d_k, int64_t k_token_stride, int64_t k_head_stride, const void* d_v,
+                         int64_t v_token_stride, int64_t v_head_stride, const int32_t* d_slots, int32_t q_heads,
+                         const void* d_q, int64_t q_token_stride, int64_t q_head_stride, void* d_q_out,
+                         int64_t qo_token_stride, int64_t qo_head_stride, const int32_t* d_pos, void* stream) {
+  return append_call(cache, rope, nullptr, dtype, tokens, d_k, k_token_stride, k_head_stride, d_v, v_token_stride, v_head_stride, d_slots,
+                     q_heads, d_q, q_token_stride, q_head_stride, d_q_out, qo_token_stride, qo_head_stride, d_pos, stream);
+}
+
+sph_status sph_kv_append_axes(const sph_kv_cache* cache, const sph_rope_desc* rope, const uint8_t* d_axes, int32_t n_axes,
+                              int64_t pos_stride, sph_dtype dtype, int64_t tokens, const void* d_k, int64_t k_token_stride,
+                              int64_t k_head_stride, const void* d_v, int64_t v_token_stride, int64_t v_head_stride,
+                              const int32_t* d_slots, int32_t q_heads, const void* d_q, int64_t q_token_stride, int64_t q_head_stride,
+                              void* d_q_out, int64_t qo_token_stride, int64_t qo_head_stride, const int32_t* d_pos, void* stream) {
+  if (!rope) return SPH_ERR_NULL;
+  const Axes axes = {d_axes, pos_stride, n_axes};
+  return append_call(cache, rope, &axes, dtype, tokens, d_k, k_token_stride, k_head_stride, d_v, v_token_stride, v_head_stride, d_slots,
+                     q_heads, d_q, q_token_stride, q_head_stride, d_q_out, qo_token_stride, qo_head_stride, d_pos, stream);
 }
 
 sph_status sph_kv_read(const sph_kv_cache* cache, int64_t tokens, const int32_t* d_slots, void* d_k_out, void* d_v_out,

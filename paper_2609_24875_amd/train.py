@@ -81,18 +81,18 @@ class _Rope:
 
         class Fn(torch.autograd.Function):
             @staticmethod
-            def forward(ctx, x, positions, table, interleaved, inverse):
-                ctx.save_for_backward(positions, table)
+            def forward(ctx, x, positions, table, interleaved, inverse, axes):
+                ctx.save_for_backward(positions, table, axes)
                 ctx.way = interleaved, inverse
-                return A.rope(x, positions, table, interleaved=interleaved, inverse=inverse)
+                return A.rope(x, positions, table, interleaved=interleaved, inverse=inverse, axes=axes)
 
             @staticmethod
             def backward(ctx, grad_y):
-                positions, table = ctx.saved_tensors
+                positions, table, axes = ctx.saved_tensors
                 interleaved, inverse = ctx.way
                 if grad_y.requires_grad:                    # a gradient of the gradient is asked for
-                    return Fn.apply(A.aligned_rows(grad_y), positions, table, interleaved, not inverse), None, None, None, None
-                return A.rope_gradient(grad_y, positions, table, interleaved, inverse), None, None, None, None
+                    return Fn.apply(A.aligned_rows(grad_y), positions, table, interleaved, not inverse, axes), None, None, None, None, None
+                return A.rope_gradient(grad_y, positions, table, interleaved, inverse, axes), None, None, None, None, None
 
         return Fn
 
@@ -106,9 +106,9 @@ def _fn(name):
     return _FNS[name]
 
 
-def rope(x, positions, table, interleaved: bool = False):
-    """``attn.rope`` with its gradient with respect to x (positions and table are constants)."""
-    return _fn("rope").apply(x, positions, table, interleaved, False)
+def rope(x, positions, table, interleaved: bool = False, axes=None):
+    """``attn.rope`` with its gradient with respect to x (positions, table and axes are constants)."""
+    return _fn("rope").apply(x, positions, table, interleaved, False, axes)
 
 
 def make_module(w, dir_bits: int, radius_bits: int, init_codebook=None, kmeans_uniforms=None,
