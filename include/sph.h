@@ -424,6 +424,28 @@ sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t token
 sph_status sph_attention_workspace_bytes(const sph_kv_cache* cache, int64_t batch, int64_t tokens, int32_t q_heads,
                                          int64_t max_q, int64_t max_len, int64_t window, size_t* bytes);
 
+/* Shrink sequences to `keep` tokens (1..2^30): the first `first` and the last `recent` of them (together at most keep) and, of the
+ * others, those with the largest sums, equal ones by the lower index, NaN above all numbers. Kept tokens stay in order: the i-th becomes token
+ * i. Sequences of `keep` tokens or fewer keep all. d_sums: device fp32, a sum for every token of a sequence (rows of at least max_len;
+ * strides in elements), for each kv head (heads = kv_heads), whose tokens are then chosen and moved by themselves, or one for
+ * all (heads = 1). Such sums are sph_attention_weights' results.
+ *
+ * d_pages, pages_stride, d_seq_lens, max_len: as in sph_attention (batch 0..65536). d_to_pages: device int32[batch][to_stride], the
+ * pages that receive the tokens, at least ceil(min(keep, max_len) / page_size) of each row. Either d_pages itself (and to_stride equal to
+ * pages_stride): tokens move within their pages, which no other sequence may hold from the first evicted token on; or other pages, none of
+ * them in d_pages or twice among the first that receive tokens, and then d_pages' are only read (they may be shared). Keys stay rotated as they were.
+ *
+ * d_new_lens: device int32[batch], min(length, keep); may be d_seq_lens. d_new_sums: device fp32 rows of new_width (min(keep, max_len)..2^30), apart from each
+ * other: the kept tokens' sums, then zeros; may be d_sums with the same strides, otherwise must not overlap it. d_kept: device int32[batch][heads][keep],
+ * which tokens were kept, in order, then -1. A sequence whose length is outside 0..max_len stays as it is, with NaN for its
+ * new sums and -1 for kept. A token of a page outside the pool is NaN in its new place; nothing is written to such a page.
+ * Results do not depend on the launch. SPH_ERR_SHAPE also where batch * heads passes 2^22 - 1, or a launch 2^32 threads. Asynchronous. */
+sph_status sph_kv_evict(const sph_kv_cache* cache, int64_t batch, const int32_t* d_pages, int64_t pages_stride, const int32_t* d_seq_lens,
+                        int64_t max_len, const float* d_sums, int32_t heads, int64_t sums_seq_stride, int64_t sums_head_stride,
+                        int64_t keep, int64_t recent, int64_t first, const int32_t* d_to_pages, int64_t to_stride, int32_t* d_new_lens,
+                        float* d_new_sums, int64_t new_width, int64_t new_seq_stride, int64_t new_head_stride, int32_t* d_kept,
+                        void* stream);
+
 /* Whether (dir_bits, radius_bits) is one of the built-in formats: 1 yes, 0 no. */
 int sph_format_supported(const sph_format* fmt);
 

@@ -55,8 +55,9 @@ def _library():
         lib.sph_attention.argtypes = [pc, I64, I64, I32, P, I64, I64, P, I64, P, I64, P, I64, I64, ctypes.c_float,
                                       P, I64, I64, P, P, SZ, P]
         lib.sph_attention_workspace_bytes.argtypes = [pc, I64, I64, I32, I64, I64, I64, ctypes.POINTER(SZ)]
+        lib.sph_kv_evict.argtypes = [pc, I64, P, I64, P, I64, P, I32, I64, I64, I64, I64, I64, P, I64, P, P, I64, I64, I64, P, P]
         for name in ("sph_rope_table", "sph_rope", "sph_rope_axes", "sph_kv_append", "sph_kv_append_axes", "sph_kv_read",
-                     "sph_attention", "sph_attention_workspace_bytes"):
+                     "sph_attention", "sph_attention_workspace_bytes", "sph_kv_evict"):
             getattr(lib, name).restype = ctypes.c_int
         _declared = lib
     return _declared
@@ -512,3 +513,80 @@ def attention(q, cache: KVCache, pages, seq_lens, q_start=None, max_q: int = 1, 
             st = call(_attention_workspace(cache, need, handle))
     _check(st, "sph_attention")
     return (out, lse) if return_lse else out
+
+
+# ------------------------------------------------------------------ eviction
+
+def _sums(t, name: str, device, batch: int, heads, width: int):
+    """Checks fp32 [batch][heads][width or more] sums with unit stride along the tokens; (pointer, sequence stride, head stride)."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32:
+        raise TypeError(f"{name} must be a torch.float32 tensor")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.dim() != 3 or t.shape[0] != batch or t.shape[1] not in heads or t.shape[2] < width or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name} must be [{batch}][{' or '.join(str(h) for h in heads)}][{width} or more] with unit stride along the tokens, "
+                         f"got shape {tuple(t.shape)} and strides {tuple(t.stride())}")
+    # (the stride of a dimension of one element is never used and may hold anything)
+    return t.data_ptr(), t.stride(0) if batch > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
+
+
+def _page_table(pages, name: str, device, batch: int):
+    """Checks int32 [batch][columns]; (pointer, row stride, columns)."""
+    import torch
+    if not isinstance(pages, torch.Tensor) or pages.dtype is not torch.int32:
+        raise TypeError(f"{name} must be a torch.int32 tensor")
+    rows, cols = pages.shape if pages.dim() == 2 else (-1, 0)
+    if rows != batch or pages.device != device or (cols > 1 and rows > 0 and pages.stride(1) != 1):
+        raise ValueError(f"{name} must be [{batch}][columns] on {device} with unit stride along the columns")
+    row = pages.stride(0) if batch > 1 else cols
+    if row < cols:
+        raise ValueError(f"rows of {name} must not overlap")
+    return pages.data_ptr(), row, cols
+
+
+def kv_evict(cache: KVCache, pages, seq_lens, sums, keep: int, recent: int = 0, first: int = 0, to_pages=None, max_len: int | None = None,
+             lens_out=None, sums_out=None, stream=None):
+    """Shrink sequences to ``keep`` tokens (sph_kv_evict): the ``first`` ones, the last ``recent``, and of the others those with the largest
+    ``sums`` (fp32 [batch][kv heads][tokens], as ``attention_weights`` gives them: each kv head chooses its own; or [batch][1][tokens]: one choice
+    for all), in order. pages, seq_lens, max_len: as in ``attention`` (max_len default: what pages and sums hold). Without
+    ``to_pages`` tokens move within their pages, which other sequences must not share from the first evicted token on; with int32 [batch][columns] ``to_pages``
+    (pages of no sequence here) they are copied there, and pages may be shared. Returns (lens int32 [batch]: the new lengths, ``lens_out`` or a
+    new tensor; sums: the kept tokens' and zeros behind them, ``sums_out``, which may be sums, or new fp32 [batch][heads][max_len]; kept int32
+    [batch][heads][keep]: which tokens were kept, then -1)."""
+    import torch
+    if stream is not None:                      # what is made for the call belongs to its stream
+        with torch.cuda.stream(stream):
+            return kv_evict(cache, pages, seq_lens, sums, keep, recent, first, to_pages, max_len, lens_out, sums_out)
+    dev = cache.device
+    batch = seq_lens.shape[0] if isinstance(seq_lens, torch.Tensor) and seq_lens.dim() else 0
+    lens = _ints(seq_lens, "seq_lens", dev, batch)
+    pp, row, cols = _page_table(pages, "pages", dev, batch)
+    held = cols * cache.page_size
+    if max_len is None:
+        max_len = min(held, sums.shape[2] if isinstance(sums, torch.Tensor) and sums.dim() == 3 else held)
+    elif max_len > held:
+        raise ValueError(f"max_len {max_len} is more than the {cols} columns of pages hold")
+    ps, ss, sh = _sums(sums, "sums", dev, batch, (cache.kv_heads, 1) if cache.kv_heads > 1 else (1,), max_len)
+    if keep < 1 or recent < 0 or first < 0 or recent + first > keep:
+        raise ValueError(f"keep {keep} must be positive and hold recent {recent} and first {first}")
+    most = min(keep, max_len)
+    if to_pages is None:
+        pt, to_row = pp, row
+    else:
+        pt, to_row, to_cols = _page_table(to_pages, "to_pages", dev, batch)
+        if to_cols * cache.page_size < most:
+            raise ValueError(f"the {to_cols} columns of to_pages do not hold {most} tokens")
+    heads = sums.shape[1]
+    if sums_out is None:
+        sums_out = torch.empty((batch, heads, max_len), dtype=torch.float32, device=dev)
+    pn, ns, nh = _sums(sums_out, "sums_out", dev, batch, (heads,), most)
+    if lens_out is None:
+        lens_out = torch.empty_like(seq_lens)
+    pl = _ints(lens_out, "lens_out", dev, batch)
+    _on_gpu(seq_lens)
+    kept = torch.empty((batch, heads, keep), dtype=torch.int32, device=dev)
+    st = _library().sph_kv_evict(cache._ref, batch, pp, row, lens, max_len, ps, heads, ss, sh, keep, recent, first, pt, to_row, pl, pn,
+                                 sums_out.shape[2], ns, nh, kept.data_ptr(), _stream_handle())
+    _check(st, "sph_kv_evict")
+    return lens_out, sums_out, kept
