@@ -424,6 +424,27 @@ sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t token
 sph_status sph_attention_workspace_bytes(const sph_kv_cache* cache, int64_t batch, int64_t tokens, int32_t q_heads,
                                          int64_t max_q, int64_t max_len, int64_t window, size_t* bytes);
 
+/* How much attention every cached token got: for each token j of a sequence, the sum over the new tokens and query heads that see it of
+ * exp(scale q.k_j - lse), their softmax's weight for it, added to what it got before (d_before). Arguments as in sph_attention (whose d_q, d_q_start, d_pages,
+ * d_seq_lens, window and scale give the same weights); d_lse: device fp32[tokens][q_heads] as sph_attention writes it, -inf for rows that
+ * see nothing. d_sums, d_before: device fp32 rows of max_len numbers and more for each sequence and kv head (heads = kv_heads), over its group
+ * of query heads, or one row for each sequence (heads = 1), over all; strides in elements. d_before: NULL for zeros, or d_sums with the same strides, or rows
+ * that do not overlap it. Entries from a sequence's length on, up to max_len, become 0 whatever they were, so that tokens added later start there.
+ * Keys that no row sees are never used, whatever they hold. A sequence whose length, start or count is outside its range gets NaN, a token of a page outside
+ * the pool that some row sees, too. Sums are held in fp32, in an order fixed by the arguments: repeated calls give bitwise
+ * identical results. d_ws: at least sph_attention_weights_workspace_bytes, 256-byte aligned, no initial contents; concurrent calls must not share one.
+ * SPH_ERR_SHAPE also where a launch would pass 2^24 workgroups, of 128 (above 128 channels a head) or 256 tokens of max_len each and more. Asynchronous. */
+sph_status sph_attention_weights(const sph_kv_cache* cache, int64_t batch, int64_t tokens, int32_t q_heads, const void* d_q,
+                                 int64_t q_token_stride, int64_t q_head_stride, const int32_t* d_q_start, int64_t max_q,
+                                 const int32_t* d_pages, int64_t pages_stride, const int32_t* d_seq_lens, int64_t max_len, int64_t window,
+                                 float scale, const float* d_lse, int32_t heads, const float* d_before, int64_t before_seq_stride,
+                                 int64_t before_head_stride, float* d_sums, int64_t sums_seq_stride, int64_t sums_head_stride, void* d_ws,
+                                 size_t ws_bytes, void* stream);
+
+/* Device workspace of sph_attention_weights with these arguments (0 when it needs none): sums of several heads, or of some of the rows, where they are joined. */
+sph_status sph_attention_weights_workspace_bytes(const sph_kv_cache* cache, int64_t batch, int64_t tokens, int32_t q_heads, int32_t heads,
+                                                 int64_t max_q, int64_t max_len, int64_t window, size_t* bytes);
+
 /* Shrink sequences to `keep` tokens (1..2^30): the first `first` and the last `recent` of them (together at most keep) and, of the
  * others, those with the largest sums, equal ones by the lower index, NaN above all numbers. Kept tokens stay in order: the i-th becomes token
  * i. Sequences of `keep` tokens or fewer keep all. d_sums: device fp32, a sum for every token of a sequence (rows of at least max_len;

@@ -55,9 +55,13 @@ def _library():
         lib.sph_attention.argtypes = [pc, I64, I64, I32, P, I64, I64, P, I64, P, I64, P, I64, I64, ctypes.c_float,
                                       P, I64, I64, P, P, SZ, P]
         lib.sph_attention_workspace_bytes.argtypes = [pc, I64, I64, I32, I64, I64, I64, ctypes.POINTER(SZ)]
+        lib.sph_attention_weights.argtypes = [pc, I64, I64, I32, P, I64, I64, P, I64, P, I64, P, I64, I64, ctypes.c_float, P, I32,
+                                              P, I64, I64, P, I64, I64, P, SZ, P]
+        lib.sph_attention_weights_workspace_bytes.argtypes = [pc, I64, I64, I32, I32, I64, I64, I64, ctypes.POINTER(SZ)]
         lib.sph_kv_evict.argtypes = [pc, I64, P, I64, P, I64, P, I32, I64, I64, I64, I64, I64, P, I64, P, P, I64, I64, I64, P, P]
         for name in ("sph_rope_table", "sph_rope", "sph_rope_axes", "sph_kv_append", "sph_kv_append_axes", "sph_kv_read",
-                     "sph_attention", "sph_attention_workspace_bytes", "sph_kv_evict"):
+                     "sph_attention", "sph_attention_workspace_bytes", "sph_attention_weights", "sph_attention_weights_workspace_bytes",
+                     "sph_kv_evict"):
             getattr(lib, name).restype = ctypes.c_int
         _declared = lib
     return _declared
@@ -449,6 +453,26 @@ def _attention_workspace(cache: KVCache, need: int, handle: int):
     return ws
 
 
+def _with_workspace(cache: KVCache, handle: int, call, need):
+    """``call(workspace)`` on the current stream, ``handle``, and its status. ``need()``: the bytes that the call wants, asked for only
+    where the one at hand may not do."""
+    import torch
+    ws = cache.workspaces.get(handle)
+    if ws is not None and torch.cuda.is_current_stream_capturing():
+        least = need()
+        if least <= ws.numel():
+            # in the pool of its graph, whose replays may run beside any call and any other graph: let go when the call is captured, it
+            # serves only later calls of the graph
+            ws = torch.empty(least, dtype=torch.uint8, device=cache.device)
+    st = call(ws)
+    if st in (SPH_ERR_NULL, SPH_ERR_BUFFER_TOO_SMALL):
+        # the library found, before it launched anything, that it needs a workspace or a larger one
+        least = need()
+        if least > (0 if ws is None else ws.numel()):
+            st = call(_attention_workspace(cache, least, handle))
+    return st
+
+
 def attention(q, cache: KVCache, pages, seq_lens, q_start=None, max_q: int = 1, max_len: int | None = None, window: int = 0,
               scale: float | None = None, out=None, return_lse: bool = False, stream=None):
     """Attention of new tokens over a cache that already holds their keys and values (sph_attention).
@@ -491,7 +515,6 @@ def attention(q, cache: KVCache, pages, seq_lens, q_start=None, max_q: int = 1, 
     lse = torch.empty((n, heads), dtype=torch.float32, device=dev) if return_lse else None
     _on_gpu(q)
     handle = _stream_handle()
-    ws = cache.workspaces.get(handle)
 
     def call(ws):
         return _library().sph_attention(cache._ref, batch, n, heads, pq, qt, qh, start, max_q, pages.data_ptr(), row, lens, max_len,
@@ -499,23 +522,12 @@ def attention(q, cache: KVCache, pages, seq_lens, q_start=None, max_q: int = 1, 
                                         None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(),
                                         0 if ws is None else ws.numel(), handle)
 
-    if ws is not None and torch.cuda.is_current_stream_capturing():
-        need = attention_workspace_bytes(cache, batch, n, heads, max_q, max_len, window)
-        if need <= ws.numel():
-            # in the pool of its graph, whose replays may run beside any call and any other graph: let go when the call is captured, it
-            # serves only later calls of the graph
-            ws = torch.empty(need, dtype=torch.uint8, device=dev)
-    st = call(ws)
-    if st in (SPH_ERR_NULL, SPH_ERR_BUFFER_TOO_SMALL):
-        # the library found, before it launched anything, that it needs a workspace or a larger one
-        need = attention_workspace_bytes(cache, batch, n, heads, max_q, max_len, window)
-        if need > (0 if ws is None else ws.numel()):
-            st = call(_attention_workspace(cache, need, handle))
+    st = _with_workspace(cache, handle, call, lambda: attention_workspace_bytes(cache, batch, n, heads, max_q, max_len, window))
     _check(st, "sph_attention")
     return (out, lse) if return_lse else out
 
 
-# ------------------------------------------------------------------ eviction
+# ------------------------------------------------------------------ attention that tokens got
 
 def _sums(t, name: str, device, batch: int, heads, width: int):
     """Checks fp32 [batch][heads][width or more] sums with unit stride along the tokens; (pointer, sequence stride, head stride)."""
@@ -544,6 +556,63 @@ def _page_table(pages, name: str, device, batch: int):
         raise ValueError(f"rows of {name} must not overlap")
     return pages.data_ptr(), row, cols
 
+
+def attention_weights_workspace_bytes(cache: KVCache, batch: int, tokens: int, q_heads: int, heads: int, max_q: int, max_len: int,
+                                      window: int = 0) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_library().sph_attention_weights_workspace_bytes(cache._ref, batch, tokens, q_heads, heads, max_q, max_len, window, ctypes.byref(out)),
+           "sph_attention_weights_workspace_bytes")
+    return out.value
+
+
+def attention_weights(q, cache: KVCache, pages, seq_lens, lse, before=None, per_head: bool = True, q_start=None, max_q: int = 1,
+                      max_len: int | None = None, window: int = 0, scale: float | None = None, out=None, stream=None):
+    """How much attention every cached token got from the new ones (sph_attention_weights): their softmax weights added up, over the query
+    heads of each kv head (``per_head``) or over all, on top of ``before`` (fp32 [batch][kv heads or 1][tokens], the sums of
+    earlier calls). q, pages, seq_lens, q_start, max_q, max_len, window, scale: as ``attention`` had them; lse: what it
+    returned with ``return_lse``. Returns fp32 [batch][kv heads or 1][max_len], or ``out``, which may be ``before``; zeros from a sequence's length
+    on. ``kv_evict`` goes by these sums."""
+    import torch
+    if stream is not None:                      # what is made for the call belongs to its stream
+        with torch.cuda.stream(stream):
+            return attention_weights(q, cache, pages, seq_lens, lse, before, per_head, q_start, max_q, max_len, window, scale, out)
+    dev = cache.device
+    pq, qt, qh = _rows(q, "q", dev, (torch.float16,))
+    n, q_heads, dim = q.shape
+    if dim != cache.head_dim:
+        raise ValueError(f"q has {dim} channels a head, the cache {cache.head_dim}")
+    batch = seq_lens.shape[0] if isinstance(seq_lens, torch.Tensor) and seq_lens.dim() else 0
+    lens = _ints(seq_lens, "seq_lens", dev, batch)
+    pp, row, cols = _page_table(pages, "pages", dev, batch)
+    start = None if q_start is None else _ints(q_start, "q_start", dev, batch + 1)
+    held = cols * cache.page_size
+    if max_len is None:
+        max_len = held
+    elif max_len > held:
+        raise ValueError(f"max_len {max_len} is more than the {cols} columns of pages hold")
+    if not isinstance(lse, torch.Tensor) or lse.dtype is not torch.float32:
+        raise TypeError("lse must be a torch.float32 tensor")
+    if lse.device != dev or lse.shape != (n, q_heads) or not lse.is_contiguous():
+        raise ValueError(f"lse must be contiguous [{n}][{q_heads}] on {dev}, got shape {tuple(lse.shape)} and strides {tuple(lse.stride())}")
+    heads = cache.kv_heads if per_head else 1
+    pb, bs, bh = (None, 0, 0) if before is None else _sums(before, "before", dev, batch, (heads,), max_len)
+    if out is None:
+        out = torch.empty((batch, heads, max_len), dtype=torch.float32, device=dev)
+    po, os, oh = _sums(out, "out", dev, batch, (heads,), max_len)
+    _on_gpu(q)
+    handle = _stream_handle()
+
+    def call(ws):
+        return _library().sph_attention_weights(cache._ref, batch, n, q_heads, pq, qt, qh, start, max_q, pp, row, lens, max_len, window,
+                                                dim ** -0.5 if scale is None else scale, lse.data_ptr(), heads, pb, bs, bh, po, os, oh,
+                                                None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), handle)
+
+    st = _with_workspace(cache, handle, call, lambda: attention_weights_workspace_bytes(cache, batch, n, q_heads, heads, max_q, max_len, window))
+    _check(st, "sph_attention_weights")
+    return out
+
+
+# ------------------------------------------------------------------ eviction
 
 def kv_evict(cache: KVCache, pages, seq_lens, sums, keep: int, recent: int = 0, first: int = 0, to_pages=None, max_len: int | None = None,
              lens_out=None, sums_out=None, stream=None):

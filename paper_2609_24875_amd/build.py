@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 SOURCES = [os.path.join(CSRC, "sph_kernels.hip"), os.path.join(CSRC, "sph_encode.hip"),
            os.path.join(CSRC, "sph_train.hip"), os.path.join(CSRC, "sph_cache.hip"),
            os.path.join(CSRC, "sph_attn.hip"), os.path.join(CSRC, "sph_attn_wide.hip"),
-           os.path.join(CSRC, "sph_evict.hip"), os.path.join(CSRC, "sph_pack.cpp")]
+           os.path.join(CSRC, "sph_weights.hip"), os.path.join(CSRC, "sph_evict.hip"), os.path.join(CSRC, "sph_pack.cpp")]
 OUT = os.path.join(HERE, "libsph.so")
 # A separate measurement probe (plain streaming read), loaded by the benchmark only.
 PROBE_SOURCES = [os.path.join(CSRC, "sph_probe.hip")]
@@ -75,7 +75,7 @@ def _compile(sources, out: str, verbose: bool) -> str:
     # buffer or an accumulator put in scratch memory (a spill, or an array the compiler could not promote)
     # halves their speed without any other sign, so the build refuses it.
     bad = {k: v for k, v in kernel_resources(res.stderr).items()
-           if any(n in k for n in ("k_gemm", "k_rope", "k_kv_", "k_attn", "k_evict")) and (v.get("scratch", 0) or v.get("vgpr_spill", 0))}
+           if any(n in k for n in ("k_gemm", "k_rope", "k_kv_", "k_attn", "k_weights", "k_evict")) and (v.get("scratch", 0) or v.get("vgpr_spill", 0))}
     if bad:
         os.remove(tmp)
         raise RuntimeError(f"kernels using scratch memory: {bad}")

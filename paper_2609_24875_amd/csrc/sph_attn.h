@@ -74,7 +74,8 @@ struct Ref {
 struct Seq {
   int start, end, n, len;
   bool bad;
-  __device__ __forceinline__ void load(const AttnArgs& a, int b) {
+  template <typename A>
+  __device__ __forceinline__ void load(const A& a, int b) {
     start = a.q_start ? a.q_start[b] : b;
     end = a.q_start ? a.q_start[b + 1] : b + 1;
     len = a.lens[b];
@@ -156,6 +157,20 @@ struct Pages {
   __device__ __forceinline__ const char* row(const char* base, int64_t page_stride, int token_stride, int page, int key) const {
     return base + page * page_stride + (uint32_t)((key & mask) * token_stride);
   }
+};
+
+// A row's pieces of eight channels in LDS are permuted within it, piece p to place p ^ turn(row), so that lanes that read together (one
+// piece of 16 rows, or two neighbouring pieces of eight) find 16 different 16-byte places of the 256 bytes of banks. kSkip is what a row
+// adds to the place.
+template <int DIM>
+struct RowPlaces {
+  static constexpr int kPer = DIM / 8, kRow = DIM * 2, kSkip = kPer % 16;
+  __device__ static __forceinline__ int turn(int row) {
+    if constexpr (kSkip == 0) return (row & 7) << 1 | (row >> 3 & 1);
+    if constexpr (kSkip == 8) return (row >> 1 & 3) << 1 | (row >> 3 & 1);
+    return (row >> 2 & 1) << 1 | (row >> 3 & 1);
+  }
+  __device__ static __forceinline__ int at(int row, int piece) { return row * kRow + ((piece ^ turn(row)) << 4); }
 };
 
 // Keys that a workgroup's rows see: [k_lo, k_hi) at most, of them each row those in (pos - window, pos].

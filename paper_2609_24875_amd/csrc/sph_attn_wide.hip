@@ -24,21 +24,16 @@ struct Wide {
   static constexpr int kRow = DIM * 2;                       // bytes of a row in LDS
   static constexpr int kHalf = kTile * kRow;                 // keys, then values
   static_assert(kTile * kPer % kThreads == 0, "whole shares");
-  // A row's pieces are permuted within it, piece p to place p ^ turn(row), so that lanes that read together find 16 different 16-byte
-  // places of the 256 bytes of banks: for keys, one piece of 16 rows or two neighbouring pieces of eight; for values, four neighbouring
-  // pieces of four rows. kSkip is what a row adds to the place.
+  // Rows as in RowPlaces: for keys, one piece of 16 rows or two neighbouring pieces of eight are read together; for values, four
+  // neighbouring pieces of four rows.
   static constexpr int kSkip = kPer % 16;
-  __device__ static __forceinline__ int key_turn(int row) {
-    if constexpr (kSkip == 0) return (row & 7) << 1 | (row >> 3 & 1);
-    if constexpr (kSkip == 8) return (row >> 1 & 3) << 1 | (row >> 3 & 1);
-    return (row >> 2 & 1) << 1 | (row >> 3 & 1);
-  }
+  __device__ static __forceinline__ int key_turn(int row) { return RowPlaces<DIM>::turn(row); }
   __device__ static __forceinline__ int value_turn(int row) {
     if constexpr (kSkip == 0) return (row & 3) << 2;
     if constexpr (kSkip == 8) return (row >> 1 & 1) << 2;
     return 0;
   }
-  __device__ static __forceinline__ int key_at(int row, int piece) { return row * kRow + ((piece ^ key_turn(row)) << 4); }
+  __device__ static __forceinline__ int key_at(int row, int piece) { return RowPlaces<DIM>::at(row, piece); }
   __device__ static __forceinline__ int value_at(int row, int piece) { return row * kRow + ((piece ^ value_turn(row)) << 4); }
 };
 
