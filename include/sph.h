@@ -424,6 +424,30 @@ sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t token
 sph_status sph_attention_workspace_bytes(const sph_kv_cache* cache, int64_t batch, int64_t tokens, int32_t q_heads,
                                          int64_t max_q, int64_t max_len, int64_t window, size_t* bytes);
 
+/* sph_attention of sequences that share long prefixes (system prompts, documents, prompts with several answers), each prefix read once for all
+ * of them. A sequence's own tokens are d_pages, d_seq_lens (own tokens, with the new ones, 0..max_len), q, o, d_q_start, max_q, scale and d_lse as in sph_attention
+ * without a window; prefix g has d_prefix_lens[g] tokens (0..max_prefix) in d_prefix_pages[g * prefix_stride ..] (device int32[prefixes][prefix_stride],
+ * rows of at least ceil(max_prefix / page_size)) and comes before the own tokens of sequences d_first[g]..d_first[g+1]-1: device
+ * int32[prefixes + 1], ascending, prefixes 1..65536; sequences before d_first[0] or from the last on have none. Every query sees the
+ * whole prefix, and its own tokens up to its position. d_first may be NULL with one prefix, of all sequences. max_group (1..65536; at least batch where d_first is
+ * NULL): the host's bound of sequences behind a prefix, for which the launch is planned as for max_prefix, max_len and max_q: better close to the truth. Prefixes and own tokens
+ * are pages of the same cache, and a page may be in any number of rows.
+ * A sequence whose own values are wrong (see sph_attention), or whose prefix has a length outside 0..max_prefix, more tokens behind it than
+ * max_group * max_q, starts that do not ascend or a page outside the pool, gets NaN. Precision, empty rows and values that no row sees: as in sph_attention; repeated
+ * calls give bitwise identical results. d_ws: at least sph_attention_shared_workspace_bytes, 256-byte aligned, no
+ * initial contents; concurrent calls must not share one. Asynchronous. */
+sph_status sph_attention_shared(const sph_kv_cache* cache, int64_t prefixes, const int32_t* d_first, int64_t max_group,
+                                const int32_t* d_prefix_pages, int64_t prefix_stride, const int32_t* d_prefix_lens, int64_t max_prefix,
+                                int64_t batch, int64_t tokens, int32_t q_heads, const void* d_q, int64_t q_token_stride,
+                                int64_t q_head_stride, const int32_t* d_q_start, int64_t max_q, const int32_t* d_pages,
+                                int64_t pages_stride, const int32_t* d_seq_lens, int64_t max_len, float scale, void* d_o,
+                                int64_t o_token_stride, int64_t o_head_stride, float* d_lse, void* d_ws, size_t ws_bytes, void* stream);
+
+/* Device workspace of sph_attention_shared with these arguments on the current device: the parts of every row. */
+sph_status sph_attention_shared_workspace_bytes(const sph_kv_cache* cache, int64_t prefixes, int64_t max_group, int64_t max_prefix,
+                                                int64_t batch, int64_t tokens, int32_t q_heads, int64_t max_q, int64_t max_len,
+                                                size_t* bytes);
+
 /* How much attention every cached token got: for each token j of a sequence, the sum over the new tokens and query heads that see it of
  * exp(scale q.k_j - lse), their softmax's weight for it, added to what it got before (d_before). Arguments as in sph_attention (whose d_q, d_q_start, d_pages,
  * d_seq_lens, window and scale give the same weights); d_lse: device fp32[tokens][q_heads] as sph_attention writes it, -inf for rows that

@@ -55,12 +55,16 @@ def _library():
         lib.sph_attention.argtypes = [pc, I64, I64, I32, P, I64, I64, P, I64, P, I64, P, I64, I64, ctypes.c_float,
                                       P, I64, I64, P, P, SZ, P]
         lib.sph_attention_workspace_bytes.argtypes = [pc, I64, I64, I32, I64, I64, I64, ctypes.POINTER(SZ)]
+        lib.sph_attention_shared.argtypes = [pc, I64, P, I64, P, I64, P, I64, I64, I64, I32, P, I64, I64, P, I64, P, I64, P, I64,
+                                             ctypes.c_float, P, I64, I64, P, P, SZ, P]
+        lib.sph_attention_shared_workspace_bytes.argtypes = [pc, I64, I64, I64, I64, I64, I32, I64, I64, ctypes.POINTER(SZ)]
         lib.sph_attention_weights.argtypes = [pc, I64, I64, I32, P, I64, I64, P, I64, P, I64, P, I64, I64, ctypes.c_float, P, I32,
                                               P, I64, I64, P, I64, I64, P, SZ, P]
         lib.sph_attention_weights_workspace_bytes.argtypes = [pc, I64, I64, I32, I32, I64, I64, I64, ctypes.POINTER(SZ)]
         lib.sph_kv_evict.argtypes = [pc, I64, P, I64, P, I64, P, I32, I64, I64, I64, I64, I64, P, I64, P, P, I64, I64, I64, P, P]
         for name in ("sph_rope_table", "sph_rope", "sph_rope_axes", "sph_kv_append", "sph_kv_append_axes", "sph_kv_read",
-                     "sph_attention", "sph_attention_workspace_bytes", "sph_attention_weights", "sph_attention_weights_workspace_bytes",
+                     "sph_attention", "sph_attention_workspace_bytes", "sph_attention_shared",
+                     "sph_attention_shared_workspace_bytes", "sph_attention_weights", "sph_attention_weights_workspace_bytes",
                      "sph_kv_evict"):
             getattr(lib, name).restype = ctypes.c_int
         _declared = lib
@@ -527,7 +531,7 @@ def attention(q, cache: KVCache, pages, seq_lens, q_start=None, max_q: int = 1, 
     return (out, lse) if return_lse else out
 
 
-# ------------------------------------------------------------------ attention that tokens got
+# ------------------------------------------------------------------ shared prefixes
 
 def _sums(t, name: str, device, batch: int, heads, width: int):
     """Checks fp32 [batch][heads][width or more] sums with unit stride along the tokens; (pointer, sequence stride, head stride)."""
@@ -556,6 +560,74 @@ def _page_table(pages, name: str, device, batch: int):
         raise ValueError(f"rows of {name} must not overlap")
     return pages.data_ptr(), row, cols
 
+
+def attention_shared_workspace_bytes(cache: KVCache, prefixes: int, max_group: int, max_prefix: int, batch: int, tokens: int, q_heads: int,
+                                     max_q: int, max_len: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_library().sph_attention_shared_workspace_bytes(cache._ref, prefixes, max_group, max_prefix, batch, tokens, q_heads, max_q, max_len,
+                                                           ctypes.byref(out)), "sph_attention_shared_workspace_bytes")
+    return out.value
+
+
+def attention_shared(q, cache: KVCache, prefix_pages, prefix_lens, pages, seq_lens, first=None, q_start=None, max_q: int = 1,
+                     max_group: int | None = None, max_prefix: int | None = None, max_len: int | None = None, scale: float | None = None,
+                     out=None, return_lse: bool = False, stream=None):
+    """``attention`` of sequences that share long prefixes, each of which is read once for all of them (sph_attention_shared).
+
+    prefix_pages: int32 [prefixes][columns], prefix_lens: int32 [prefixes], the tokens that come before the own ones of sequences
+    first[g] .. first[g+1]-1 (``first``: int32 [prefixes + 1], ascending; default, with one prefix: of all; sequences outside have none). pages,
+    seq_lens: a sequence's own tokens, with the new ones; q, q_start, max_q, scale, out, return_lse: as in ``attention``. A query
+    sees the whole prefix and its own tokens up to its position. max_group, max_prefix, max_len: bounds of the sequences behind a
+    prefix (default: all), of its tokens and of the own ones (default: what the columns hold) that the launch is planned for. There is no window."""
+    import torch
+    if stream is not None:                      # what is made for the call belongs to its stream
+        with torch.cuda.stream(stream):
+            return attention_shared(q, cache, prefix_pages, prefix_lens, pages, seq_lens, first, q_start, max_q, max_group, max_prefix, max_len,
+                                    scale, out, return_lse)
+    dev, half = cache.device, (torch.float16,)
+    pq, qt, qh = _rows(q, "q", dev, half)
+    n, heads, dim = q.shape
+    if dim != cache.head_dim:
+        raise ValueError(f"q has {dim} channels a head, the cache {cache.head_dim}")
+    batch = seq_lens.shape[0] if isinstance(seq_lens, torch.Tensor) and seq_lens.dim() else 0
+    lens = _ints(seq_lens, "seq_lens", dev, batch)
+    pp, row, cols = _page_table(pages, "pages", dev, batch)
+    prefixes = prefix_lens.shape[0] if isinstance(prefix_lens, torch.Tensor) and prefix_lens.dim() else 0
+    plens = _ints(prefix_lens, "prefix_lens", dev, prefixes)
+    pf, prow, pcols = _page_table(prefix_pages, "prefix_pages", dev, prefixes)
+    if prefixes < 1 or (first is None and prefixes > 1):
+        raise ValueError(f"{prefixes} prefixes: at least one, and several need first")
+    at = None if first is None else _ints(first, "first", dev, prefixes + 1)
+    start = None if q_start is None else _ints(q_start, "q_start", dev, batch + 1)
+    if max_group is None or first is None:
+        max_group = max(1, batch)
+    page = cache.page_size
+    max_len = cols * page if max_len is None else max_len
+    max_prefix = pcols * page if max_prefix is None else max_prefix
+    if max_len > cols * page or max_prefix > pcols * page:
+        raise ValueError(f"max_len {max_len} or max_prefix {max_prefix} is more than the {cols} and {pcols} columns of pages hold")
+    if out is None:
+        out = _new(q)
+        po, ot, oh = out.data_ptr(), heads * dim, dim
+    else:
+        po, ot, oh = _rows(out, "out", dev, half, (n, heads, dim))
+    lse = torch.empty((n, heads), dtype=torch.float32, device=dev) if return_lse else None
+    _on_gpu(q)
+    handle = _stream_handle()
+
+    def call(ws):
+        return _library().sph_attention_shared(cache._ref, prefixes, at, max_group, pf, prow, plens, max_prefix, batch, n, heads, pq, qt, qh,
+                                               start, max_q, pp, row, lens, max_len, dim ** -0.5 if scale is None else scale, po, ot, oh,
+                                               None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(),
+                                               0 if ws is None else ws.numel(), handle)
+
+    st = _with_workspace(cache, handle, call, lambda: attention_shared_workspace_bytes(cache, prefixes, max_group, max_prefix, batch, n, heads,
+                                                                                       max_q, max_len))
+    _check(st, "sph_attention_shared")
+    return (out, lse) if return_lse else out
+
+
+# ------------------------------------------------------------------ attention that tokens got
 
 def attention_weights_workspace_bytes(cache: KVCache, batch: int, tokens: int, q_heads: int, heads: int, max_q: int, max_len: int,
                                       window: int = 0) -> int:

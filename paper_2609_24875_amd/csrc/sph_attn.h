@@ -12,6 +12,9 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 struct AttnArgs {
+  // (what sph_attention_shared's kernels do otherwise)
+  static constexpr bool kParts = false;   // rows are always written as parts
+  static constexpr bool kFlat = false;    // every row sees every key
   CacheView c;
   const char* q;
   char* o;
@@ -76,8 +79,12 @@ struct Seq {
   bool bad;
   template <typename A>
   __device__ __forceinline__ void load(const A& a, int b) {
-    start = a.q_start ? a.q_start[b] : b;
-    end = a.q_start ? a.q_start[b + 1] : b + 1;
+    if constexpr (A::kFlat) {
+      a.tokens_of(b, start, end);
+    } else {
+      start = a.q_start ? a.q_start[b] : b;
+      end = a.q_start ? a.q_start[b + 1] : b + 1;
+    }
     len = a.lens[b];
     // (compared before they are subtracted: the difference of two arbitrary numbers need not fit)
     bad = len < 0 || len > a.max_len || start < 0 || end < start || end > a.tokens;
@@ -112,8 +119,7 @@ __device__ __forceinline__ int64_t part_at(const AttnArgs& a, int slot, int kvh,
   return ((int64_t)slot * a.c.kv_heads + kvh) * ((int64_t)a.max_q * a.group) + row;
 }
 
-__device__ __forceinline__ void write_part(const AttnArgs& a, int slot, int kvh, int row, int ch, f32x4 acc, float m, float l) {
-  const int64_t at = part_at(a, slot, kvh, row);
+__device__ __forceinline__ void write_part(const AttnArgs& a, int64_t at, int ch, f32x4 acc, float m, float l) {
   *(f32x4*)(a.part + at * a.c.dim + ch) = acc;
   if (ch == 0) a.ml[at] = make_float2(m, l);
 }

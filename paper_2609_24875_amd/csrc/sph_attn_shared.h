@@ -1,0 +1,109 @@
+// The kernels of sph_attention_shared, whose sources are a file for each number of bits (see sph_attn_shared.hip).
+#pragma once
+#include "sph_attn_few.h"
+#include "sph_attn_many.h"
+
+// Which of the two ways (up to 32 rows of a kv head, or more) the prefixes and the own tokens go. Behind a prefix are at least as many rows as
+// of any of its sequences.
+enum SharedKind { kFewFew, kManyFew, kManyMany };
+
+// The kernel for a number of bits; nb: blocks of 16 rows of the way for up to 32, uni: pages of 16 tokens and more.
+const void* sph_attn_shared_kernel16(int dim, SharedKind kind, int nb, bool uni);
+const void* sph_attn_shared_kernel8(int dim, SharedKind kind, int nb, bool uni);
+const void* sph_attn_shared_kernel4(int dim, SharedKind kind, int nb, bool uni);
+
+namespace {
+
+// A sequence's own tokens.
+struct OwnArgs : AttnArgs {
+  static constexpr bool kParts = true;
+};
+
+// A prefix as a sequence whose new tokens are those of all sequences behind it: first[g] .. first[g + 1] - 1 of `seqs`, or with
+// first NULL all.
+struct PrefixArgs : AttnArgs {
+  static constexpr bool kParts = true, kFlat = true;
+  const int32_t* first;
+  int seqs;
+  __device__ __forceinline__ void tokens_of(int g, int& start, int& end) const {
+    const int s0 = first ? first[g] : 0, s1 = first ? first[g + 1] : seqs;
+    const bool there = s0 >= 0 && s0 <= s1 && s1 <= seqs;
+    start = !there ? -1 : q_start ? q_start[s0] : s0;
+    end = !there ? -1 : q_start ? q_start[s1] : s1;
+  }
+};
+
+struct SharedArgs {
+  OwnArgs own;
+  PrefixArgs pre;
+  uint32_t pre_blocks;
+  int64_t pre_part;        // rows of parts before the prefixes'
+  bool pre_many, own_many;
+};
+
+template <int DIM, int BITS, int NB, int KIND>
+struct SharedLds {
+  static constexpr int kFew = kWaves * (kTile * Lay<DIM, BITS>::kVStride > 16 * NB * (DIM + 4) * 4 ? kTile * Lay<DIM, BITS>::kVStride : 16 * NB * (DIM + 4) * 4);
+  static constexpr int kMany = 2 * Wide<DIM, BITS>::kHalf;
+  static constexpr int kA = KIND == kFewFew ? kFew : KIND == kManyMany || kMany > kFew ? kMany : kFew, kB = KIND == kFewFew ? 16 : kMany;
+};
+
+template <int DIM, int BITS, int NB, bool UNI, int KIND>
+__global__ __launch_bounds__(kThreads, (DIM * NB <= 128 ? 2 : 1)) void k_attn_shared(SharedArgs) {
+  const SharedArgs& both = *(const SharedArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  typedef SharedLds<DIM, BITS, NB, KIND> L;
+  // (two arrays, as k_attn_wide's; the other way uses the first)
+  __shared__ __attribute__((aligned(16))) char lds_a[L::kA], lds_b[L::kB];
+  __shared__ float2 ml_s[KIND == kManyMany ? 1 : kWaves][16 * NB];
+  __shared__ int before[KIND == kManyMany ? 1 : kEvenBatch + 1], sums[KIND == kManyMany ? 1 : kEvenBatch / 32];
+  if (blockIdx.x < both.pre_blocks) {
+    typedef PrefixArgs A;
+    const A& a = both.pre;
+    const uint32_t block = blockIdx.x;
+    if constexpr (KIND == kFewFew) {
+      char* lds = lds_a;
+#include "sph_attn_few.inc"
+    } else {
+      typedef Wide<DIM, BITS> W;
+#include "sph_attn_many.inc"
+    }
+  } else {
+    typedef OwnArgs A;
+    const A& a = both.own;
+    const uint32_t block = blockIdx.x - both.pre_blocks;
+    if constexpr (KIND == kManyMany) {
+      typedef Wide<DIM, BITS> W;
+#include "sph_attn_many.inc"
+    } else {
+      char* lds = lds_a;
+#include "sph_attn_few.inc"
+    }
+  }
+}
+
+template <int DIM, int BITS>
+const void* shared_kernel(SharedKind kind, int nb, bool uni) {
+  if (kind == kManyMany) return (const void*)k_attn_shared<DIM, BITS, 1, true, kManyMany>;
+  if constexpr (DIM > 128) {
+    if (kind == kFewFew) return uni ? (const void*)k_attn_shared<DIM, BITS, 1, true, kFewFew> : (const void*)k_attn_shared<DIM, BITS, 1, false, kFewFew>;
+    return uni ? (const void*)k_attn_shared<DIM, BITS, 1, true, kManyFew> : (const void*)k_attn_shared<DIM, BITS, 1, false, kManyFew>;
+  } else {
+    // (pages of less than 16 tokens always by two blocks of rows, which serve one as well)
+    if (!uni) return kind == kFewFew ? (const void*)k_attn_shared<DIM, BITS, 2, false, kFewFew> : (const void*)k_attn_shared<DIM, BITS, 2, false, kManyFew>;
+    if (kind == kFewFew) return nb == 1 ? (const void*)k_attn_shared<DIM, BITS, 1, true, kFewFew> : (const void*)k_attn_shared<DIM, BITS, 2, true, kFewFew>;
+    return nb == 1 ? (const void*)k_attn_shared<DIM, BITS, 1, true, kManyFew> : (const void*)k_attn_shared<DIM, BITS, 2, true, kManyFew>;
+  }
+}
+
+template <int BITS>
+const void* shared_kernel(int dim, SharedKind kind, int nb, bool uni) {
+  switch (dim) {
+    case 64: return shared_kernel<64, BITS>(kind, nb, uni);
+    case 96: return shared_kernel<96, BITS>(kind, nb, uni);
+    case 128: return shared_kernel<128, BITS>(kind, nb, uni);
+    case 192: return shared_kernel<192, BITS>(kind, nb, uni);
+    default: return shared_kernel<256, BITS>(kind, nb, uni);
+  }
+}
+
+}  // namespace

@@ -1,0 +1,245 @@
+// Attention of sequences that share long prefixes (sph_attention_shared).
+//
+// The rows of all sequences behind a prefix go through its keys together, as one sequence of so many rows that see all of it: what is read
+// once serves all of them, and makes rows enough for the matrix products that prompts have. Beside that every sequence goes through its own tokens
+// as ever. Both write parts (o, m, l), sums relative to 2^m, and the join adds a row's: o = sum_i o_i 2^(m_i - m), l = sum_i l_i 2^(m_i - m)
+// with m the largest, and o / l at the end. One launch does both kinds, so that the prefix's products run beside the own tokens' reads; the
+// join is the second.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "sph_attn_plan.h"
+#include "sph_attn_shared.h"
+
+const void* sph_attn_shared_kernel16(int dim, SharedKind kind, int nb, bool uni) { return shared_kernel<16>(dim, kind, nb, uni); }
+
+namespace {
+
+// The prefix whose sequences are first[g] .. first[g + 1] - 1 with b among them, -1 for none. By a whole wave, 64 places at once.
+__device__ __forceinline__ int prefix_of(const PrefixArgs& a, int b) {
+  if (!a.first) return 0;
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = a.batch + 1;                               // among the n entries from lo on, the last that is not above b
+  while (n > 1) {
+    const int step = (n + 63) / 64, at = lane * step;
+    const uint64_t not_above = __ballot(at < n && a.first[lo + min(at, n - 1)] <= b);
+    // (ascending, the lanes are the first few)
+    const int last = 63 - __builtin_clzll(not_above | 1);
+    lo += last * step;
+    n = min(step, n - last * step);
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  return lo < a.batch && a.first[lo] <= b && b < a.first[lo + 1] ? lo : -1;
+}
+
+// Joins the parts of a row, its own tokens' and then its prefix's: as k_attn_join.
+template <bool FEW>
+__global__ __launch_bounds__(kThreads) void k_attn_shared_join(SharedArgs both) {
+  const OwnArgs& a = both.own;
+  const int lane = threadIdx.x & 63;
+  const uint32_t per = FEW ? a.c.dim / 4 : kJoinCh / 4, groups = 64 / per, chunks = FEW ? 1 : a.c.dim / kJoinCh, rows = a.max_q * a.group;
+  uint32_t id = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (id >= chunks * a.c.kv_heads * rows * a.batch) return;
+  const uint32_t group = lane / per, ch = id % chunks * kJoinCh + lane % per * 4;
+  id /= chunks;
+  const int kvh = id % a.c.kv_heads;
+  id /= a.c.kv_heads;
+  const int row = id % rows, b = id / rows, head = kvh * a.group + row % a.group;
+  Seq s, p;
+  s.load(a, b);
+  const int64_t token = (int64_t)s.start + row / a.group;
+  bool bad = s.bad;
+  if (!bad && row >= s.n * a.group) return;
+  int64_t first = 0, step = 0, pre_first = 0, pre_step = 0;
+  int parts = 0, pre_parts = 0;
+  if (!bad) {
+    const int g = prefix_of(both.pre, b);
+    if (g >= 0) {
+      p.load(both.pre, g);
+      // (a token that is not among the prefix's has starts that do not ascend)
+      bad = p.bad || token < p.start || token >= p.end;
+      if (!bad && both.pre_many) {
+        step = (int64_t)a.c.kv_heads * (a.tokens * a.group);
+        pre_first = both.pre_part + (int64_t)kvh * (a.tokens * a.group) + token * a.group + row % a.group, pre_step = step, pre_parts = both.pre.splits;
+      } else if (!bad) {
+        const int2 w = both.pre.shares ? both.pre.where[g] : make_int2(g, 1);
+        const int r = (int)(token - p.start) * a.group + row % a.group;
+        pre_first = part_at(both.pre, w.x, kvh, r), pre_step = part_at(both.pre, w.x + 1, kvh, r) - pre_first, pre_parts = w.y;
+        pre_first += both.pre_part;
+      }
+    }
+    const int2 w = both.own_many ? make_int2(b, a.splits) : a.shares ? a.where[b] : make_int2(b, 1);
+    first = part_at(a, w.x, kvh, row), step = part_at(a, w.x + (both.own_many ? a.batch : 1), kvh, row) - first, parts = w.y;
+  }
+  if (bad) {
+    // every token that the sequence claims, though there may be more than max_q
+    const float nan = __builtin_nanf("");
+    const int64_t end = s.bad ? min((int64_t)s.end, a.tokens) : token + 1;
+    if (group == 0)
+      for (int64_t t = token; t < end; t += a.max_q)
+        if (t >= 0) write_out(a, t, head, ch, f32x4{nan, nan, nan, nan}, 0.0f, nan);
+    return;
+  }
+  const int all = parts + pre_parts;
+  auto at_of = [&](int i) { return i < parts ? first + i * step : pre_first + (i - parts) * pre_step; };
+  float mm = -INFINITY;
+  for (int i = lane; i < all; i += 64) mm = fmaxf(mm, a.ml[at_of(i)].x);
+#pragma unroll
+  for (int d = 32; d; d >>= 1) mm = fmaxf(mm, __shfl_xor(mm, d));
+  const float ref = mm == -INFINITY ? 0.0f : mm;
+  f32x4 acc = {};
+  float l = 0.0f;
+  if (group < groups) {
+#pragma unroll 4
+    for (int i = group; i < all; i += groups) {
+      const int64_t at = at_of(i);
+      const float2 ml = a.ml[at];
+      const f32x4 part = *(const f32x4*)(a.part + at * a.c.dim + ch);
+      const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+      l += f * ml.y;
+      acc += f * part;
+    }
+  }
+  // the groups' sums, in order, to the first
+  for (uint32_t g = 1; g < groups; ++g) {
+    const float more = __shfl(l, (int)(g * per + lane % per));
+    l += group ? 0.0f : more;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x = __shfl(acc[i], (int)(g * per + lane % per));
+      acc[i] += group ? 0.0f : x;
+    }
+  }
+  if (group == 0) write_out(a, token, head, ch, acc, mm, l);
+}
+
+// ------------------------------------------------------------------ host side
+
+struct SharedPlan {
+  Plan own, pre;
+  int64_t pre_q;                           // tokens behind a prefix at most
+  size_t own_parts, pre_parts, bytes;
+  int64_t joins;
+  bool few;
+  SharedKind kind;
+};
+
+SharedPlan shared_plan(const sph_kv_cache* c, int64_t prefixes, int64_t max_group, int64_t max_prefix, int64_t batch, int64_t tokens,
+                       int q_heads, int64_t max_q, int64_t max_len) {
+  SharedPlan p{};
+  const int64_t group = q_heads / c->kv_heads, rows = max_q * group;
+  p.pre_q = std::max(max_q, std::min(tokens, max_group * max_q));
+  p.own = plan_of(c, batch, q_heads, max_q, max_len, 0);
+  p.pre = plan_of(c, prefixes, q_heads, p.pre_q, max_prefix, 0);
+  p.own.fold = p.pre.fold = 0;             // (for workgroups that are alone in their launch)
+  p.kind = p.own.wide ? kManyMany : p.pre.wide ? kManyFew : kFewFew;
+  const auto slots = [](const Plan& q, int64_t n) { return q.wide ? q.splits * n : q.shares ? q.shares + n : n; };
+  p.own_parts = (size_t)slots(p.own, batch) * c->kv_heads * rows;
+  p.pre_parts = p.pre.wide ? (size_t)p.pre.splits * tokens * q_heads : (size_t)slots(p.pre, prefixes) * c->kv_heads * p.pre_q * group;
+  p.bytes = (p.own_parts + p.pre_parts) * (c->head_dim + 2) * sizeof(float) + (size_t)(batch + prefixes) * sizeof(int2);
+  const int64_t each = (p.own.wide ? p.own.splits : 1) + (p.pre.wide ? p.pre.splits : p.pre.shares / prefixes);
+  p.few = each <= kFewParts;
+  p.joins = (int64_t)c->kv_heads * batch * rows * (p.few ? 1 : c->head_dim / kJoinCh);
+  return p;
+}
+
+bool launchable(const SharedPlan& p) { return p.own.grid + p.pre.grid < (1 << 24) && p.joins < (1 << 26); }
+
+sph_status check_shared(const sph_kv_cache* c, int64_t prefixes, int64_t max_group, int64_t max_prefix, int64_t batch, int64_t tokens,
+                        int32_t q_heads, int64_t max_q, int64_t max_len) {
+  if (const sph_status st = check_sizes(c, batch, tokens, q_heads, max_q, max_len, 0)) return st;
+  if (prefixes < 1 || prefixes > 65536 || max_group < 1 || max_group > 65536 || max_prefix < 0 || max_prefix > (1 << 30) ||
+      std::min(tokens, max_group * max_q) > (1 << 24))
+    return SPH_ERR_SHAPE;
+  return SPH_OK;
+}
+
+bool launch_ok(const void* fn, int64_t blocks, hipStream_t s, SharedArgs& a) {
+  void* kargs[] = {(void*)&a};
+  return hipLaunchKernel(fn, dim3((unsigned)blocks), dim3(kThreads), kargs, 0, s) == hipSuccess && hipGetLastError() == hipSuccess;
+}
+
+}  // namespace
+
+extern "C" {
+
+sph_status sph_attention_shared_workspace_bytes(const sph_kv_cache* cache, int64_t prefixes, int64_t max_group, int64_t max_prefix,
+                                                int64_t batch, int64_t tokens, int32_t q_heads, int64_t max_q, int64_t max_len,
+                                                size_t* bytes) {
+  if (!bytes) return SPH_ERR_NULL;
+  if (const sph_status st = check_shared(cache, prefixes, max_group, max_prefix, batch, tokens, q_heads, max_q, max_len)) return st;
+  *bytes = 0;
+  if (!batch || !tokens) return SPH_OK;
+  const SharedPlan p = shared_plan(cache, prefixes, max_group, max_prefix, batch, tokens, q_heads, max_q, max_len);
+  if (!launchable(p)) return SPH_ERR_SHAPE;
+  *bytes = p.bytes;
+  return SPH_OK;
+}
+
+sph_status sph_attention_shared(const sph_kv_cache* cache, int64_t prefixes, const int32_t* d_first, int64_t max_group,
+                                const int32_t* d_prefix_pages, int64_t prefix_stride, const int32_t* d_prefix_lens, int64_t max_prefix,
+                                int64_t batch, int64_t tokens, int32_t q_heads, const void* d_q, int64_t q_token_stride,
+                                int64_t q_head_stride, const int32_t* d_q_start, int64_t max_q, const int32_t* d_pages,
+                                int64_t pages_stride, const int32_t* d_seq_lens, int64_t max_len, float scale, void* d_o,
+                                int64_t o_token_stride, int64_t o_head_stride, float* d_lse, void* d_ws, size_t ws_bytes, void* stream) {
+  if (const sph_status st = check_shared(cache, prefixes, max_group, max_prefix, batch, tokens, q_heads, max_q, max_len)) return st;
+  if (!std::isfinite(scale)) return SPH_ERR_BAD_VALUE;
+  if ((!d_q_start && (max_q != 1 || tokens != batch)) || (!d_first && (prefixes != 1 || max_group < batch))) return SPH_ERR_SHAPE;
+  const int64_t ps = cache->page_size;
+  if (pages_stride < (max_len + ps - 1) / ps || pages_stride > INT32_MAX || prefix_stride < (max_prefix + ps - 1) / ps || prefix_stride > INT32_MAX)
+    return SPH_ERR_SHAPE;
+  if (!batch || !tokens) return SPH_OK;
+  if (!d_q || !d_o || !d_seq_lens || !d_prefix_lens || (!d_pages && max_len > 0) || (!d_prefix_pages && max_prefix > 0)) return SPH_ERR_NULL;
+  const int64_t lim = int64_t(1) << 40;
+  for (int64_t s : {q_token_stride, q_head_stride, o_token_stride, o_head_stride})
+    if (s < 0 || s >= lim || s % 8) return SPH_ERR_SHAPE;
+  if ((uintptr_t)d_q % 16 || (uintptr_t)d_o % 16 || (uintptr_t)d_ws % 256) return SPH_ERR_SHAPE;
+  for (const void* x : {(const void*)d_first, (const void*)d_prefix_pages, (const void*)d_prefix_lens, (const void*)d_q_start, (const void*)d_pages,
+                        (const void*)d_seq_lens, (const void*)d_lse})
+    if ((uintptr_t)x % 4) return SPH_ERR_SHAPE;
+  if ((tokens > 1 && o_token_stride == 0) || (q_heads > 1 && o_head_stride == 0)) return SPH_ERR_SHAPE;  // rows written twice
+  const SharedPlan p = shared_plan(cache, prefixes, max_group, max_prefix, batch, tokens, q_heads, max_q, max_len);
+  if (!launchable(p)) return SPH_ERR_SHAPE;
+  if (!d_ws) return SPH_ERR_NULL;
+  if (ws_bytes < p.bytes) return SPH_ERR_BUFFER_TOO_SMALL;
+  const int bits = cache->bits, dim = cache->head_dim;
+  SharedArgs both{};
+  AttnArgs& a = both.own;
+  a.c = sph_cache_view(cache);
+  a.q = (const char*)d_q, a.o = (char*)d_o;
+  a.qt = 2 * q_token_stride, a.qh = 2 * q_head_stride, a.ot = 2 * o_token_stride, a.oh = 2 * o_head_stride;
+  a.q_start = d_q_start, a.lse = d_lse, a.tokens = tokens, a.q_heads = q_heads, a.group = q_heads / cache->kv_heads;
+  a.scale = scale * kLog2e;
+  a.stream = cache->n_pages * cache->page_size * cache->kv_heads * (int64_t)dim * bits / 4 > kLastCache;
+  a.part = (float*)d_ws;
+  a.ml = (float2*)(a.part + (p.own_parts + p.pre_parts) * dim);
+  a.where = (int2*)(a.ml + p.own_parts + p.pre_parts);
+  (AttnArgs&)both.pre = a;
+  const auto planned = [](AttnArgs& x, const Plan& q) { x.tiles = (int)q.tiles, x.splits = q.splits, x.chunk = q.chunk, x.shares = q.shares; };
+  planned(a, p.own);
+  a.pages = d_pages, a.pages_stride = pages_stride, a.lens = d_seq_lens;
+  a.batch = (int)batch, a.max_q = (int)max_q, a.max_len = (int)max_len;
+  PrefixArgs& b = both.pre;
+  planned(b, p.pre);
+  b.pages = d_prefix_pages, b.pages_stride = prefix_stride, b.lens = d_prefix_lens;
+  b.batch = (int)prefixes, b.max_q = (int)p.pre_q, b.max_len = (int)max_prefix;
+  b.first = d_first, b.seqs = (int)batch;
+  b.part = a.part + p.own_parts * dim, b.ml = a.ml + p.own_parts, b.where = a.where + batch;
+  both.pre_blocks = (uint32_t)p.pre.grid, both.pre_part = (int64_t)p.own_parts;
+  both.pre_many = p.pre.wide, both.own_many = p.own.wide;
+  const bool uni = cache->page_size >= 16;
+  const int nb = p.kind == kFewFew ? p.pre.nb : p.own.nb;
+  const void* fn = bits == 16  ? sph_attn_shared_kernel16(dim, p.kind, nb, uni)
+                   : bits == 8 ? sph_attn_shared_kernel8(dim, p.kind, nb, uni)
+                               : sph_attn_shared_kernel4(dim, p.kind, nb, uni);
+  if (!launch_ok(fn, p.pre.grid + p.own.grid, (hipStream_t)stream, both)) return SPH_ERR_HIP;
+  if (!launch_ok(p.few ? (const void*)k_attn_shared_join<true> : (const void*)k_attn_shared_join<false>, (p.joins + kWaves - 1) / kWaves,
+                 (hipStream_t)stream, both))
+    return SPH_ERR_HIP;
+  return SPH_OK;
+}
+
+}  // extern "C"

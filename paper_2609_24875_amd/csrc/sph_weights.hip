@@ -14,6 +14,7 @@
 namespace {
 
 struct WeightArgs {
+  static constexpr bool kFlat = false;
   CacheView c;
   const char* q;
   int64_t qt, qh;          // strides in bytes

@@ -31,7 +31,8 @@ EXPORTS = ("sph_packed_bytes", "sph_pack_weights", "sph_gemv", "sph_gemm_small",
            "sph_angular_logits", "sph_direction_groups", "sph_fake_quant_init_rho",
            "sph_fake_quant_forward", "sph_fake_quant_backward_workspace_bytes",
            "sph_fake_quant_backward", "sph_rope_table", "sph_rope", "sph_rope_axes", "sph_kv_append", "sph_kv_append_axes", "sph_kv_read", "sph_attention",
-           "sph_attention_workspace_bytes", "sph_attention_weights",
+           "sph_attention_workspace_bytes", "sph_attention_shared",
+           "sph_attention_shared_workspace_bytes", "sph_attention_weights",
            "sph_attention_weights_workspace_bytes", "sph_kv_evict", "sph_format_supported", "sph_status_str")
 
 FORMATS = {
