@@ -9,7 +9,7 @@
 
 #include <algorithm>
 
-#include "sph_attn.h"
+#include "sph_attn_few.h"
 
 namespace {
 
@@ -85,28 +85,31 @@ struct Keys {
 // Base-2 logarithm of a row's softmax sum; a row without one (it sees nothing, or only scores of -inf) gives no weight.
 __device__ __forceinline__ float log2_sum(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
 
-// The weights that rows 0 .. rows - 1 of 32 give to the lane's key, added up: scores st, logarithms lse_s and positions pos_s of all 32 in LDS.
-template <bool WHOLE>
-__device__ __forceinline__ float weigh(const f32x16& st, const float* lse_s, const int* pos_s, float scale, int rows, int key, int window, bool gone, int h) {
+// The weights that rows 8 j + 4 h .. + 3 of 32 give to the lane's key: scores st, logarithms l of these rows.
+__device__ __forceinline__ float weigh(const f32x16& st, int j, const f32x4& l, float scale) {
+  float x[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(st[4 * j + i], scale, -l[i]));
+  return (x[0] + x[1]) + (x[2] + x[3]);
+}
+
+// Those of all 32 where not every row sees the key: those whose position pos_s hides it give nothing.
+__device__ __forceinline__ float weigh_seen(const f32x16& st, const float* lse_s, const int* pos_s, float scale, int key, int window, bool gone, int h) {
   float sum = 0.0f;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    if (8 * j < rows) {
-      const f32x4 l = *(const f32x4*)(lse_s + 8 * j + 4 * h);
-      float x[4];
+    const f32x4 l = *(const f32x4*)(lse_s + 8 * j + 4 * h);
+    const int4 p = *(const int4*)(pos_s + 8 * j + 4 * h);
+    const int pos[4] = {p.x, p.y, p.z, p.w};
+    float x[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(st[4 * j + i], scale, -l[i]));
-      if constexpr (!WHOLE) {
-        const int4 p = *(const int4*)(pos_s + 8 * j + 4 * h);
-        const int pos[4] = {p.x, p.y, p.z, p.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const bool seen = key <= pos[i] && (!window || key > pos[i] - window);
-          x[i] = !seen ? 0.0f : gone ? __builtin_nanf("") : x[i];
-        }
-      }
-      sum += (x[0] + x[1]) + (x[2] + x[3]);
+    for (int i = 0; i < 4; ++i) {
+      x[i] = __builtin_amdgcn_exp2f(fmaf(st[4 * j + i], scale, -l[i]));
+      // (a select, not a branch around the exponential)
+      asm("" : "+v"(x[i]));
+      x[i] = key > pos[i] || (window && key <= pos[i] - window) ? 0.0f : gone ? __builtin_nanf("") : x[i];
     }
+    sum += (x[0] + x[1]) + (x[2] + x[3]);
   }
   return sum;
 }
@@ -119,91 +122,216 @@ __device__ __forceinline__ void write_sum(const WeightArgs& a, int b, int head, 
   a.out[b * a.os + head * a.oh + key] = x;
 }
 
-// Up to 32 rows a kv head (single tokens, short drafts): each wave has keys of its own and goes through them once, or with one sum for
-// all heads the workgroup's waves take the heads in turn and meet in LDS.
+// A wave's step of up to 32 rows: kBlocks times 16 keys in registers as they are stored, 8 KiB of 128 channels. Products are
+// v_mfma_f32_16x16x32_f16 with a column per key, whose 16 rows' scores lie in four lanes.
 template <int DIM, int BITS>
+struct Step {
+  typedef Lay<DIM, BITS> L;
+  static constexpr int kWords = DIM * BITS / 128;            // a lane's registers of 16 keys
+  static constexpr int kBlocks = kWords >= 32 ? 1 : kWords >= 16 ? 2 : 4, kKeys = 16 * kBlocks;
+  uint32_t k[kBlocks][L::kLoads][L::kPiece / 4], par[kBlocks][L::kLoads];
+  // Keys from kt on, lane l with those at 16 u + l % 16 in pages page[u] (those outside the pool: any, their rows are not used).
+  __device__ __forceinline__ void load(const Pages& pg, const int* page, int kt, int lane) {
+    const int col = lane & 15, g4 = lane >> 4;
+#pragma unroll
+    for (int u = 0; u < kBlocks; ++u) {
+      const int p = pg.there(page[u]) ? page[u] : 0, key = kt + 16 * u + col;
+      const char* row = pg.row(pg.k, pg.stride, pg.token, p, key) + g4 * L::kPiece;
+#pragma unroll
+      for (int i = 0; i < L::kLoads; ++i) load_words<L::kPiece>(row + 4 * i * L::kPiece, k[u][i]);
+      if constexpr (BITS < 16) {
+        const char* pr = pg.row(pg.k_par, pg.par_stride, pg.par_token, p, key) + g4 * L::kPieceCh / 32 * 4;
+#pragma unroll
+        for (int i = 0; i < L::kLoads; ++i) par[u][i] = *(const uint32_t*)(pr + i * L::kPieceCh / 8 * 4);
+      }
+    }
+  }
+  __device__ __forceinline__ f16x8 piece(int u, int i, int j) const {
+    if constexpr (BITS == 16)
+      return __builtin_bit_cast(f16x8, make_uint4(k[u][i][0], k[u][i][1], k[u][i][2], k[u][i][3]));
+    else if constexpr (BITS == 8)
+      return decode8w<8>(k[u][i][2 * j], k[u][i][2 * j + 1], par[u][i]);
+    else
+      return decode8w<4>(k[u][i][j], 0, par[u][i]);
+  }
+};
+
+// Up to 32 rows a kv head (single tokens, short drafts): each wave goes through keys of its own, kRun steps of them, the next step's loads issued
+// when one's products are done; with one sum for all heads the workgroup's waves take the heads in turn and meet in LDS.
+constexpr int kRun = 2;
+
+template <int DIM, int BITS, int NB>
 __global__ __launch_bounds__(kThreads) void k_weights_few(WeightArgs) {
   const WeightArgs& a = *(const WeightArgs*)__builtin_amdgcn_kernarg_segment_ptr();
-  typedef Keys<DIM, BITS> K;
-  __shared__ __attribute__((aligned(16))) float lse_s[kWaves][32];
-  __shared__ __attribute__((aligned(16))) int pos_s[kWaves][32];
-  __shared__ float sum_s[kWaves][64];
+  typedef Step<DIM, BITS> K;
+  typedef Lay<DIM, BITS> L;
+  __shared__ float sum_s[kWaves][K::kKeys];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 31, h = lane >> 5;
+  const int col = lane & 15, g4 = lane >> 4;
   uint32_t id = blockIdx.x;
   const int head = id % a.heads;
   id /= a.heads;
   const bool each = a.heads > 1 || a.c.kv_heads == 1;
-  const int kt = (each ? id % a.tiles * kWaves + wave : id % a.tiles) * K::kKeys, b = id / a.tiles;
-  if (kt >= a.max_len) return;                               // (with one sum for all heads for all waves alike)
+  // (turned by the sequence's number: otherwise the first tiles, which all sequences have, come to the same part of the chip)
+  const int b = id / a.tiles, tile = (id + b) % a.tiles;
+  const int t0 = (each ? tile * kWaves + wave : tile) * (each ? kRun : 1) * K::kKeys;
+  if (t0 >= a.max_len) return;                               // (with one sum for all heads for all waves alike)
   Seq s;
   s.load(a, b);
   const int nrow = s.n * a.group, first = s.len - s.n;
   const int lo = a.window ? max(0, first - a.window + 1) : 0;
-  float sum = s.bad ? __builtin_nanf("") : 0.0f;
-  if (!s.bad && nrow && kt < s.len && kt + K::kKeys > lo) {
-    const int r = min(col, nrow - 1), t = r / a.group, pos = col < nrow ? first + t : -1;
-    // every row sees every key
-    const bool all = nrow == 32 && kt + K::kKeys <= first + 1 && (!a.window || kt > s.len - 1 - a.window);
-    float acc[K::kBlocks] = {};
-    if (h == 0) pos_s[wave][col] = pos;
-    for (int kvh = each ? head : wave; kvh < a.c.kv_heads; kvh += each ? a.c.kv_heads : kWaves) {
-      Pages pg;
-      pg.set(a.c, kvh);
-      const int hq = kvh * a.group + r % a.group;
-      K keys;
-      keys.load(pg, a.pages + b * a.pages_stride, kt, lo, s.len, lane);
-      const char* qr = a.q + (s.start + t) * a.qt + hq * a.qh;
-      f16x8 q[K::kSteps];
+  const int t1 = min(a.max_len, t0 + (each ? kRun : 1) * K::kKeys), len = s.bad ? a.max_len : s.len;
+  // the steps of keys that a row may see: k_lo .. k_hi
+  const bool none = s.bad || nrow == 0;
+  const int k_lo = none ? t1 : min(t1, max(t0, lo / K::kKeys * K::kKeys)), k_hi = none ? t1 : min(t1, s.len);
+  const float nothing = s.bad ? __builtin_nanf("") : 0.0f;
+  if (each)
+    for (int kt = t0; kt < t1; kt += K::kKeys)
+      if ((kt < k_lo || kt >= k_hi) && lane < K::kKeys) write_sum(a, b, head, kt + lane, len, nothing);
+  float sum[K::kBlocks];
 #pragma unroll
-      for (int i = 0; i < K::kSteps; ++i) q[i] = *(const f16x8*)(qr + 16 * K::piece(i, h));
-      if (h == 0) lse_s[wave][col] = log2_sum(a.lse[(int64_t)(s.start + t) * a.q_heads + hq]);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
+  for (int u = 0; u < K::kBlocks; ++u) sum[u] = nothing;
+  int kvh = each ? head : wave;
+  if (k_lo < k_hi && kvh < a.c.kv_heads) {
+    Pages pg;
+    pg.set(a.c, kvh);
+    const int32_t* pages = a.pages + b * a.pages_stride;
+    const int e_lo = lo >> pg.shift, e_hi = (s.len - 1) >> pg.shift;
+    // keys outside those that are seen take a page inside: they are read and not used
+    auto pages_of = [&](int kt, int* page) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < K::kBlocks; ++u) page[u] = pages[min(max((kt + 16 * u + col) >> pg.shift, e_lo), e_hi)];
+    };
+    f16x8 q[NB][L::kSteps];
+    float lse[NB][4];
+    int pos[NB][4];
+    // (asked for before the next step's keys, which would hold up what is loaded behind them)
+    auto old_sum = [&](int k) { return each && a.before && lane < K::kKeys && k + lane < min(s.len, a.max_len) ? a.before[b * a.bs + head * a.bh + k + lane] : 0.0f; };
+    auto load_rows = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        const int r = min(16 * n + col, nrow - 1);
+        const char* qr = a.q + (int64_t)(s.start + r / a.group) * a.qt + (kvh * a.group + r % a.group) * a.qh;
+#pragma unroll
+        for (int i = 0; i < L::kLoads; ++i)
+#pragma unroll
+          for (int j = 0; j < L::kBlocks; ++j) q[n][i * L::kBlocks + j] = *(const f16x8*)(qr + 2 * ((4 * i + g4) * L::kPieceCh + 8 * j));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          // rows behind the last give nothing
+          const int row = 16 * n + 4 * g4 + i, rr = min(row, nrow - 1), t = rr / a.group;
+          const float x = log2_sum(a.lse[(int64_t)(s.start + t) * a.q_heads + kvh * a.group + rr % a.group]);
+          lse[n][i] = row < nrow ? x : INFINITY;
+          pos[n][i] = row < nrow ? first + t : -1;
+        }
+      }
+    };
+    K T;
+    int kt = k_lo, page[K::kBlocks], next[K::kBlocks];
+    pages_of(kt, page);
+    float old = old_sum(kt);
+    T.load(pg, page, kt, lane);
+    load_rows();
+    while (true) {
+      // the next step: of this head, or with one sum for all heads the same keys of the wave's next one
+      const int to = each ? kt + K::kKeys : kt, to_head = each ? kvh : kvh + kWaves;
+      const bool more = each ? to < k_hi : to_head < a.c.kv_heads;
+      pages_of(more ? to : kt, next);
+      f32x4 st[K::kBlocks][NB] = {};
+#pragma unroll
+      for (int u = 0; u < K::kBlocks; ++u)
+#pragma unroll
+        for (int i = 0; i < L::kLoads; ++i)
+#pragma unroll
+          for (int j = 0; j < L::kBlocks; ++j) {
+            const f16x8 kf = T.piece(u, i, j);
+#pragma unroll
+            for (int n = 0; n < NB; ++n) st[u][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(q[n][i * L::kBlocks + j], kf, st[u][n], 0, 0, 0);
+          }
+      // not above the products: the loads would take registers of their own beside those that they refill
+      __builtin_amdgcn_sched_barrier(0);
+      const float old_now = old;
+      if (more) {
+        if (!each) pg.set(a.c, to_head);
+        old = old_sum(to);
+        T.load(pg, next, to, lane);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      const bool whole = kt >= lo && kt + K::kKeys - 1 <= first && (!a.window || kt > s.len - 1 - a.window);
 #pragma unroll
       for (int u = 0; u < K::kBlocks; ++u) {
-        f32x16 st = {};
+        const int key = kt + 16 * u + col;
+        const bool gone = !pg.there(page[u]), plain = whole && !__any(gone);
 #pragma unroll
-        for (int i = 0; i < K::kSteps; ++i) st = __builtin_amdgcn_mfma_f32_32x32x16_f16(q[i], keys.k[u][i], st, 0, 0, 0);
-        const int key = kt + 32 * u + col;
-        if (all && !__any(keys.gone[u]))
-          acc[u] += weigh<true>(st, lse_s[wave], pos_s[wave], a.scale, nrow, key, a.window, false, h);
-        else
-          acc[u] += weigh<false>(st, lse_s[wave], pos_s[wave], a.scale, nrow, key, a.window, keys.gone[u], h);
+        for (int n = 0; n < NB; ++n) {
+          float x[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(st[u][n][i], a.scale, -lse[n][i]));
+          if (!plain) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const bool seen = key <= pos[n][i] && (!a.window || key > pos[n][i] - a.window);
+              x[i] = !seen ? 0.0f : gone ? __builtin_nanf("") : x[i];
+            }
+          }
+          sum[u] += (x[0] + x[1]) + (x[2] + x[3]);
+        }
+        page[u] = next[u];
       }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
+      if (each) {
+        // lane 16 u + l has key 16 u + l
+        float mine = 0.0f;
+#pragma unroll
+        for (int u = 0; u < K::kBlocks; ++u) {
+          sum[u] += __shfl_xor(sum[u], 16);
+          sum[u] += __shfl_xor(sum[u], 32);
+          mine = g4 == u ? sum[u] : mine;
+          sum[u] = 0.0f;
+        }
+        if (lane < K::kKeys && kt + lane < a.max_len) a.out[b * a.os + head * a.oh + kt + lane] = kt + lane < len ? old_now + mine : 0.0f;
+      }
+      if (!more) break;
+      kt = to;
+      if (!each) {
+        kvh = to_head;
+        load_rows();
+      }
     }
-#pragma unroll
-    for (int u = 0; u < K::kBlocks; ++u) acc[u] += __shfl_xor(acc[u], 32);
-    sum = K::kBlocks == 2 && h ? acc[K::kBlocks - 1] : acc[0];
   }
-  if (!each) {
-    sum_s[wave][lane] = sum;
-    __syncthreads();
-    if (wave) return;
+  if (each) return;
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) sum += sum_s[w][lane];
+  for (int u = 0; u < K::kBlocks; ++u) {
+    sum[u] += __shfl_xor(sum[u], 16);
+    sum[u] += __shfl_xor(sum[u], 32);
+    if (g4 == 0) sum_s[wave][16 * u + col] = sum[u];
   }
-  // lane l has key kt + l
-  if (lane < K::kKeys) write_sum(a, b, head, kt + lane, s.bad ? a.max_len : s.len, sum);
+  __syncthreads();
+  if (wave || lane >= K::kKeys) return;
+  float x = sum_s[0][lane];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) x += sum_s[w][lane];
+  write_sum(a, b, head, t0 + lane, len, x);
 }
 
-constexpr int kManyRows = 64;                                // rows of a step
+
+// Rows of a step, so that two workgroups fit a CU's LDS.
+constexpr int many_rows(int dim) { return dim <= 128 ? 128 : 64; }
 
 // More rows (prompts, long drafts): a workgroup's waves have keys of their own in registers, and go together through the rows that see any of
-// them, which come 64 at a time through LDS.
+// them, which come 128 (64) at a time through LDS.
 template <int DIM, int BITS>
 __global__ __launch_bounds__(kThreads, 2) void k_weights_many(WeightArgs) {
   const WeightArgs& a = *(const WeightArgs*)__builtin_amdgcn_kernarg_segment_ptr();
   typedef Keys<DIM, BITS> K;
   typedef RowPlaces<DIM> L;
-  constexpr int kBytes = kManyRows * L::kRow, kShare = kManyRows * L::kPer / kThreads;
+  constexpr int kManyRows = many_rows(DIM), kBytes = kManyRows * L::kRow, kShare = kManyRows * L::kPer / kThreads;
   static_assert(kManyRows * L::kPer % kThreads == 0, "whole shares");
   // two arrays, not one of two: loads on their way into one do not hold up reads of the other
   __shared__ __attribute__((aligned(16))) char rows_a[kBytes], rows_b[kBytes];
-  __shared__ __attribute__((aligned(16))) float lse_s[2][kManyRows];
-  __shared__ __attribute__((aligned(16))) int pos_s[2][kManyRows];
+  // of the step before, this one, the next one, whose rows are on their way, and the one after it: rows' logarithms, positions and places
+  __shared__ __attribute__((aligned(16))) float lse_s[4][kManyRows];
+  __shared__ __attribute__((aligned(16))) int pos_s[4][kManyRows];
+  __shared__ int64_t off_s[4][kManyRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, h = lane >> 5;
   // the first keys are seen by most rows, so they come first
@@ -234,68 +362,135 @@ __global__ __launch_bounds__(kThreads, 2) void k_weights_many(WeightArgs) {
 #pragma unroll
       for (int u = 0; u < K::kBlocks; ++u) any_gone |= keys.gone[u];
       any_gone = __any(any_gone);
-      auto load_rows = [&](int r0, char* to) {
+      auto load_rows = [&](int slot, char* to) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < kShare; ++i) {
           const int idx = threadIdx.x + kThreads * i, row = idx / L::kPer, place = idx % L::kPer;
-          const uint32_t r = min(r0 + row, r_hi - 1), t = r / (uint32_t)a.group, hq = kvh * a.group + r % (uint32_t)a.group;
-          const char* from = a.q + (int64_t)(s.start + t) * a.qt + hq * a.qh + ((place ^ L::turn(row)) << 4);
+          const char* from = a.q + off_s[slot][row] + ((place ^ L::turn(row)) << 4);
           __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
                                            (__attribute__((address_space(3))) void*)(to + (kThreads * i + 64 * wave) * 16), 16, 0, 0);
         }
       };
-      // logarithm and position of a step's row `threadIdx.x`: rows behind the last see nothing
-      auto load_lse = [&](int r0, float& lse, int& pos) {
+      // Row `threadIdx.x` of a step, worked out once for all lanes that load or weigh it: those behind the last are read as it is and see nothing.
+      float lse = 0.0f;
+      int pos = 0;
+      int64_t off = 0;
+      auto find_row = [&](int r0) __attribute__((always_inline)) {
         const uint32_t r = min(r0 + (int)threadIdx.x, r_hi - 1), t = r / (uint32_t)a.group, hq = kvh * a.group + r % (uint32_t)a.group;
         lse = log2_sum(a.lse[(int64_t)(s.start + t) * a.q_heads + hq]);
         pos = r0 + (int)threadIdx.x < r_hi ? first + (int)t : -1;
+        off = (int64_t)(s.start + t) * a.qt + hq * a.qh;
       };
-      float lse = 0.0f;
-      int pos = 0;
-      load_rows(r_lo, rows_a);
-      if (threadIdx.x < kManyRows) {
-        load_lse(r_lo, lse, pos);
-        lse_s[0][threadIdx.x] = lse, pos_s[0][threadIdx.x] = pos;
+      auto keep_row = [&](int slot) __attribute__((always_inline)) { lse_s[slot][threadIdx.x] = lse, pos_s[slot][threadIdx.x] = pos, off_s[slot][threadIdx.x] = off; };
+      const bool finds = threadIdx.x < kManyRows;
+      if (finds) {
+        find_row(r_lo);
+        keep_row(0);
+        if (r_lo + kManyRows < r_hi) {
+          find_row(r_lo + kManyRows);
+          keep_row(1);
+        }
       }
+      __syncthreads();
+      load_rows(0, rows_a);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
-      auto step = [&](int r0, const char* from, char* to, int at) __attribute__((always_inline)) {
-        const bool more = r0 + kManyRows < r_hi;
-        if (more) {
-          load_rows(r0 + kManyRows, to);
-          if (threadIdx.x < kManyRows) load_lse(r0 + kManyRows, lse, pos);
-        }
+      int at = 0;                                            // the step's place of four
+      f32x16 st[2][K::kBlocks];
+      bool left = false;                                     // the weights of the last step's last block are still to be added: its scores are in st[1]
+      auto logs_of = [&](f32x4* l, int slot, int rb) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) l[j] = *(const f32x4*)(lse_s[slot] + 32 * rb + 8 * j + 4 * h);
+      };
+      auto weigh_piece = [&](const f32x16* of, const f32x4* l, int p) __attribute__((always_inline)) {
+        acc[p % K::kBlocks] += weigh(of[p % K::kBlocks], p / K::kBlocks, l[p / K::kBlocks], a.scale);
+      };
+      constexpr int kPieces = 4 * K::kBlocks;
+      auto add_left = [&]() __attribute__((always_inline)) {
+        f32x4 l[4];
+        logs_of(l, (at + 3) & 3, kManyRows / 32 - 1);
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) weigh_piece(st[1], l, p);
+      };
+      auto step = [&](int r0, const char* from, char* to) __attribute__((always_inline)) {
+        const bool more = r0 + 2 * kManyRows < r_hi;
+        const int next = (at + 1) & 3, after = (at + 2) & 3;
+        if (r0 + kManyRows < r_hi) load_rows(next, to);
+        if (more && finds) find_row(r0 + 2 * kManyRows);
         const int p_lo = first + r0 / a.group, p_hi = first + (min(r0 + kManyRows, r_hi) - 1) / a.group;
         const bool whole = r0 + kManyRows <= r_hi && kt + K::kKeys - 1 <= p_lo && (!a.window || kt > p_hi - a.window) && !any_gone;
-        if (kt <= p_hi && (!a.window || kt + K::kKeys > p_lo - a.window + 1)) {
+        const bool work = kt <= p_hi && (!a.window || kt + K::kKeys > p_lo - a.window + 1);
+        constexpr int kRowBlocks = kManyRows / 32;
+        auto read = [&](f16x8* q, int rb) __attribute__((always_inline)) {
 #pragma unroll
-          for (int rb = 0; rb < kManyRows / 32; ++rb) {
-            f32x16 st[K::kBlocks] = {};
+          for (int i = 0; i < K::kSteps; ++i) q[i] = *(const f16x8*)(from + L::at(32 * rb + col, K::piece(i, h)));
+        };
+        auto products = [&](f32x16* st, const f16x8* q) __attribute__((always_inline)) {
+#pragma unroll
+          for (int u = 0; u < K::kBlocks; ++u) st[u] = f32x16{};
+#pragma unroll
+          for (int i = 0; i < K::kSteps; ++i)
+#pragma unroll
+            for (int u = 0; u < K::kBlocks; ++u) st[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(q[i], keys.k[u][i], st[u], 0, 0, 0);
+        };
+        if (work && whole) {
+          // A block's products run beside the weights of the one before, a few of them behind each step of products (left to itself, the compiler puts
+          // all of one kind behind the other), the first block's beside those of the last step's last. A step's rows are read for the next block
+          // when its products are under way.
+          static_assert(kRowBlocks % 2 == 0, "the last block's scores are in st[1]");
+          // (a ring of kAhead steps of rows: of 256 channels, all steps of a block would not fit the registers)
+          constexpr int kAhead = K::kSteps == 16 ? 8 : K::kSteps;
+          f16x8 q[kAhead];
+          auto read_step = [&](int rb, int i) __attribute__((always_inline)) { q[i % kAhead] = *(const f16x8*)(from + L::at(32 * rb + col, K::piece(i, h))); };
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) read_step(0, i);
+#pragma unroll
+          for (int rb = 0; rb < kRowBlocks; ++rb) {
+            f32x4 l[4];
+            logs_of(l, rb ? at : (at + 3) & 3, rb ? rb - 1 : kRowBlocks - 1);
+            f32x16* now = st[rb & 1];
+            const f32x16* last = st[(rb + 1) & 1];
+#pragma unroll
+            for (int u = 0; u < K::kBlocks; ++u) now[u] = f32x16{};
 #pragma unroll
             for (int i = 0; i < K::kSteps; ++i) {
-              const f16x8 q = *(const f16x8*)(from + L::at(32 * rb + col, K::piece(i, h)));
 #pragma unroll
-              for (int u = 0; u < K::kBlocks; ++u) st[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(q, keys.k[u][i], st[u], 0, 0, 0);
-            }
+              for (int u = 0; u < K::kBlocks; ++u) now[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(q[i % kAhead], keys.k[u][i], now[u], 0, 0, 0);
+              if (i + kAhead < K::kSteps)
+                read_step(rb, i + kAhead);
+              else if (rb + 1 < kRowBlocks)
+                read_step(rb + 1, i + kAhead - K::kSteps);
+              if (rb > 0 || left)
 #pragma unroll
-            for (int u = 0; u < K::kBlocks; ++u) {
-              const int key = kt + 32 * u + col;
-              if (whole)
-                acc[u] += weigh<true>(st[u], lse_s[at] + 32 * rb, pos_s[at] + 32 * rb, a.scale, 32, key, a.window, false, h);
-              else
-                acc[u] += weigh<false>(st[u], lse_s[at] + 32 * rb, pos_s[at] + 32 * rb, a.scale, 32, key, a.window, keys.gone[u], h);
+                for (int p = i * kPieces / K::kSteps; p < (i + 1) * kPieces / K::kSteps; ++p) weigh_piece(last, l, p);
+              __builtin_amdgcn_sched_barrier(0);
             }
           }
+          left = true;
+        } else {
+          if (left) add_left();
+          left = false;
+#pragma unroll 1
+          for (int rb = work ? 0 : kRowBlocks; rb < kRowBlocks; ++rb) {
+            f16x8 q[K::kSteps];
+            read(q, rb);
+            products(st[0], q);
+#pragma unroll
+            for (int u = 0; u < K::kBlocks; ++u)
+              acc[u] += weigh_seen(st[0][u], lse_s[at] + 32 * rb, pos_s[at] + 32 * rb, a.scale, kt + 32 * u + col, a.window, keys.gone[u], h);
+          }
         }
-        if (more && threadIdx.x < kManyRows) lse_s[at ^ 1][threadIdx.x] = lse, pos_s[at ^ 1][threadIdx.x] = pos;
+        if (more && finds) keep_row(after);
+        at = next;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
       };
       for (int r0 = r_lo; r0 < r_hi; r0 += 2 * kManyRows) {
-        step(r0, rows_a, rows_b, 0);
+        step(r0, rows_a, rows_b);
         if (r0 + kManyRows >= r_hi) break;
-        step(r0 + kManyRows, rows_b, rows_a, 1);
+        step(r0 + kManyRows, rows_b, rows_a);
       }
+      if (left) add_left();
     }
   }
 #pragma unroll
@@ -333,7 +528,7 @@ constexpr int kFewRows = 32, kCus = 256;
 
 struct Plan {
   bool few, join;
-  int tiles, splits, window;
+  int nb, tiles, splits, window;
   int64_t grid, joins;
   size_t bytes;
 };
@@ -342,19 +537,22 @@ Plan plan_of(const sph_kv_cache* c, int64_t batch, int q_heads, int heads, int64
   Plan p{};
   // one that hides nothing is none (and positions minus a window stay inside 32 bits)
   p.window = window > max_len ? 0 : (int)window;
-  const int64_t rows = max_q * (q_heads / c->kv_heads), keys = c->head_dim <= 128 ? 64 : 32;
+  const int64_t rows = max_q * (q_heads / c->kv_heads);
   const bool each = heads > 1 || c->kv_heads == 1;
   p.few = rows <= kFewRows;
+  p.nb = rows <= 16 ? 1 : 2;
   p.splits = 1;
   if (p.few) {
-    p.tiles = (int)((max_len + keys * (each ? kWaves : 1) - 1) / (keys * (each ? kWaves : 1)));
+    const int64_t words = c->head_dim * c->bits / 128, keys = (words >= 32 ? 16 : words >= 16 ? 32 : 64) * (each ? kRun * kWaves : 1);   // (as Step has them)
+    p.tiles = (int)((max_len + keys - 1) / keys);
     p.grid = batch * heads * p.tiles;
     return p;
   }
+  const int64_t keys = c->head_dim <= 128 ? 64 : 32;
   p.tiles = (int)((max_len + keys * kWaves - 1) / (keys * kWaves));
   const int64_t units = batch * c->kv_heads * std::max(1, p.tiles);
-  // rows are split where keys alone leave the chip idle, in parts of four steps at least
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((2 * kCus + units - 1) / units, rows / (4 * kManyRows)));
+  // rows are split where keys alone leave the chip idle, in parts of 256 at least
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((2 * kCus + units - 1) / units, rows / 256));
   p.join = !each || p.splits > 1;
   p.grid = units * p.splits;
   p.joins = batch * heads * ((max_len + kThreads - 1) / kThreads);
@@ -375,14 +573,19 @@ sph_status check_sizes(const sph_kv_cache* c, int64_t batch, int64_t tokens, int
   return SPH_OK;
 }
 
+template <int DIM, int BITS>
+const void* kernel_for(const Plan& p) {
+  return !p.few ? (const void*)k_weights_many<DIM, BITS> : p.nb == 1 ? (const void*)k_weights_few<DIM, BITS, 1> : (const void*)k_weights_few<DIM, BITS, 2>;
+}
+
 template <int BITS>
-const void* kernel_for(bool few, int dim) {
+const void* kernel_for(const Plan& p, int dim) {
   switch (dim) {
-    case 64: return few ? (const void*)k_weights_few<64, BITS> : (const void*)k_weights_many<64, BITS>;
-    case 96: return few ? (const void*)k_weights_few<96, BITS> : (const void*)k_weights_many<96, BITS>;
-    case 128: return few ? (const void*)k_weights_few<128, BITS> : (const void*)k_weights_many<128, BITS>;
-    case 192: return few ? (const void*)k_weights_few<192, BITS> : (const void*)k_weights_many<192, BITS>;
-    default: return few ? (const void*)k_weights_few<256, BITS> : (const void*)k_weights_many<256, BITS>;
+    case 64: return kernel_for<64, BITS>(p);
+    case 96: return kernel_for<96, BITS>(p);
+    case 128: return kernel_for<128, BITS>(p);
+    case 192: return kernel_for<192, BITS>(p);
+    default: return kernel_for<256, BITS>(p);
   }
 }
 
@@ -451,7 +654,7 @@ sph_status sph_attention_weights(const sph_kv_cache* cache, int64_t batch, int64
   a.max_q = (int)max_q, a.max_len = (int)max_len, a.window = p.window, a.heads = heads, a.tiles = p.tiles, a.splits = p.splits;
   a.scale = scale * kLog2e;
   const int bits = cache->bits, dim = cache->head_dim;
-  const void* fn = bits == 16 ? kernel_for<16>(p.few, dim) : bits == 8 ? kernel_for<8>(p.few, dim) : kernel_for<4>(p.few, dim);
+  const void* fn = bits == 16 ? kernel_for<16>(p, dim) : bits == 8 ? kernel_for<8>(p, dim) : kernel_for<4>(p, dim);
   if (!launch_ok(fn, p.grid, (hipStream_t)stream, a)) return SPH_ERR_HIP;
   if (p.join && !launch_ok((const void*)k_weights_join, p.joins, (hipStream_t)stream, a)) return SPH_ERR_HIP;
   return SPH_OK;
