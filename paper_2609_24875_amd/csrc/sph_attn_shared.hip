@@ -48,68 +48,95 @@ __global__ __launch_bounds__(kThreads) void k_attn_shared_join(SharedArgs both) 
   const int kvh = id % a.c.kv_heads;
   id /= a.c.kv_heads;
   const int row = id % rows, b = id / rows, head = kvh * a.group + row % a.group;
-  Seq s, p;
+  // Where the row's parts are, whether or not its sequence and prefix turn out to be right: what is right is loaded beside the parts.
+  const PrefixArgs& p = both.pre;
+  Seq s;
   s.load(a, b);
   const int64_t token = (int64_t)s.start + row / a.group;
+  const int g = prefix_of(p, b);
+  int2 w = make_int2(b, both.own_many ? a.splits : 1);
+  if (!both.own_many && a.shares) w = a.where[b];
+  const int64_t first = part_at(a, w.x, kvh, row), step = part_at(a, w.x + (both.own_many ? a.batch : 1), kvh, row) - first;
+  int64_t pre_first = 0, pre_step = 0;
+  int parts = w.y, pre_parts = 0;
   bool bad = s.bad;
-  if (!bad && row >= s.n * a.group) return;
-  int64_t first = 0, step = 0, pre_first = 0, pre_step = 0;
-  int parts = 0, pre_parts = 0;
-  if (!bad) {
-    const int g = prefix_of(both.pre, b);
-    if (g >= 0) {
-      p.load(both.pre, g);
-      // (a token that is not among the prefix's has starts that do not ascend)
-      bad = p.bad || token < p.start || token >= p.end;
-      if (!bad && both.pre_many) {
-        step = (int64_t)a.c.kv_heads * (a.tokens * a.group);
-        pre_first = both.pre_part + (int64_t)kvh * (a.tokens * a.group) + token * a.group + row % a.group, pre_step = step, pre_parts = both.pre.splits;
-      } else if (!bad) {
-        const int2 w = both.pre.shares ? both.pre.where[g] : make_int2(g, 1);
-        const int r = (int)(token - p.start) * a.group + row % a.group;
-        pre_first = part_at(both.pre, w.x, kvh, r), pre_step = part_at(both.pre, w.x + 1, kvh, r) - pre_first, pre_parts = w.y;
-        pre_first += both.pre_part;
-      }
+  if (g >= 0) {
+    Seq q;
+    q.load(p, g);
+    // (a token that is not among the prefix's has starts that do not ascend)
+    bad |= q.bad || token < q.start || token >= q.end;
+    if (both.pre_many) {
+      const int64_t at = min(max(token, (int64_t)0), a.tokens - 1);
+      pre_step = (int64_t)a.c.kv_heads * (a.tokens * a.group);
+      pre_first = both.pre_part + (int64_t)kvh * (a.tokens * a.group) + at * a.group + row % a.group, pre_parts = p.splits;
+    } else {
+      w = p.shares ? p.where[g] : make_int2(g, 1);
+      const int r = (int)min(max(token - q.start, (int64_t)0), (int64_t)p.max_q - 1) * a.group + row % a.group;
+      pre_first = part_at(p, w.x, kvh, r), pre_step = part_at(p, w.x + 1, kvh, r) - pre_first, pre_parts = w.y;
+      pre_first += both.pre_part;
     }
-    const int2 w = both.own_many ? make_int2(b, a.splits) : a.shares ? a.where[b] : make_int2(b, 1);
-    first = part_at(a, w.x, kvh, row), step = part_at(a, w.x + (both.own_many ? a.batch : 1), kvh, row) - first, parts = w.y;
+  }
+  // (slots that no sequence wrote are anything)
+  if (!both.own_many && a.shares && (s.n == 0 || bad)) parts = 0;
+  if (!both.pre_many && p.shares && bad) pre_parts = 0;
+  const int all = parts + pre_parts;
+  auto at_of = [&](int i) { return i < parts ? first + i * step : pre_first + (i - parts) * pre_step; };
+  constexpr int kLoads = 5;                                  // of a lane before it knows the maximum
+  float2 ml[kLoads];
+  f32x4 part[kLoads];
+#pragma unroll
+  for (int u = 0; u < kLoads; ++u) {
+    const int i = group + u * groups;
+    ml[u] = make_float2(-INFINITY, 0.0f), part[u] = f32x4{};
+    if (group < groups && i < all) {
+      const int64_t at = at_of(i);
+      ml[u] = a.ml[at];
+      part[u] = *(const f32x4*)(a.part + at * a.c.dim + ch);
+    }
   }
   if (bad) {
     // every token that the sequence claims, though there may be more than max_q
     const float nan = __builtin_nanf("");
-    const int64_t end = s.bad ? min((int64_t)s.end, a.tokens) : token + 1;
+    const int64_t end = s.bad ? min((int64_t)s.end, a.tokens) : row < s.n * a.group ? token + 1 : token;
+    const int64_t t0 = token < 0 ? token + (a.max_q - 1 - token) / a.max_q * a.max_q : token;
     if (group == 0)
-      for (int64_t t = token; t < end; t += a.max_q)
-        if (t >= 0) write_out(a, t, head, ch, f32x4{nan, nan, nan, nan}, 0.0f, nan);
+      for (int64_t t = t0; t < end; t += a.max_q) write_out(a, t, head, ch, f32x4{nan, nan, nan, nan}, 0.0f, nan);
     return;
   }
-  const int all = parts + pre_parts;
-  auto at_of = [&](int i) { return i < parts ? first + i * step : pre_first + (i - parts) * pre_step; };
+  if (row >= s.n * a.group) return;
   float mm = -INFINITY;
-  for (int i = lane; i < all; i += 64) mm = fmaxf(mm, a.ml[at_of(i)].x);
+#pragma unroll
+  for (int u = 0; u < kLoads; ++u) mm = fmaxf(mm, ml[u].x);
+  for (int i = kLoads * groups + lane; i < all; i += 64) mm = fmaxf(mm, a.ml[at_of(i)].x);
 #pragma unroll
   for (int d = 32; d; d >>= 1) mm = fmaxf(mm, __shfl_xor(mm, d));
   const float ref = mm == -INFINITY ? 0.0f : mm;
   f32x4 acc = {};
   float l = 0.0f;
+#pragma unroll
+  for (int u = 0; u < kLoads; ++u) {
+    const float f = __builtin_amdgcn_exp2f(ml[u].x - ref);
+    l += f * ml[u].y;
+    acc += f * part[u];
+  }
   if (group < groups) {
 #pragma unroll 4
-    for (int i = group; i < all; i += groups) {
+    for (int i = group + kLoads * groups; i < all; i += groups) {
       const int64_t at = at_of(i);
-      const float2 ml = a.ml[at];
-      const f32x4 part = *(const f32x4*)(a.part + at * a.c.dim + ch);
-      const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-      l += f * ml.y;
-      acc += f * part;
+      const float2 m = a.ml[at];
+      const f32x4 x = *(const f32x4*)(a.part + at * a.c.dim + ch);
+      const float f = __builtin_amdgcn_exp2f(m.x - ref);
+      l += f * m.y;
+      acc += f * x;
     }
   }
   // the groups' sums, in order, to the first
-  for (uint32_t g = 1; g < groups; ++g) {
-    const float more = __shfl(l, (int)(g * per + lane % per));
+  for (uint32_t k = 1; k < groups; ++k) {
+    const float more = __shfl(l, (int)(k * per + lane % per));
     l += group ? 0.0f : more;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float x = __shfl(acc[i], (int)(g * per + lane % per));
+      const float x = __shfl(acc[i], (int)(k * per + lane % per));
       acc[i] += group ? 0.0f : x;
     }
   }
@@ -135,13 +162,24 @@ SharedPlan shared_plan(const sph_kv_cache* c, int64_t prefixes, int64_t max_grou
   p.own = plan_of(c, batch, q_heads, max_q, max_len, 0);
   p.pre = plan_of(c, prefixes, q_heads, p.pre_q, max_prefix, 0);
   p.own.fold = p.pre.fold = 0;             // (for workgroups that are alone in their launch)
+  if (p.pre.wide) {
+    // A workgroup a CU, beside which the own tokens' are, and two where prefixes are several, since ragged ones leave many with little to do. One
+    // prefix of 32768 tokens before 128 sequences of 1024 161 us, with two 195; 8 of up to 4099 before 8 each of up to 700 at 8 bits 48 and 46.
+    const int64_t units = c->kv_heads * prefixes * p.pre.tiles, tile = sph_attn_wide_tile(c->head_dim);
+    const int64_t want = std::max<int64_t>(1, (prefixes > 1 ? 2 : 1) * kCus / units);
+    p.pre.chunk = (int)std::max<int64_t>(4 * tile, ((max_prefix + want - 1) / want + tile - 1) / tile * tile);
+    p.pre.splits = (int)std::max<int64_t>(1, (max_prefix + p.pre.chunk - 1) / p.pre.chunk);
+    p.pre.grid = units * p.pre.splits;
+  }
   p.kind = p.own.wide ? kManyMany : p.pre.wide ? kManyFew : kFewFew;
   const auto slots = [](const Plan& q, int64_t n) { return q.wide ? q.splits * n : q.shares ? q.shares + n : n; };
   p.own_parts = (size_t)slots(p.own, batch) * c->kv_heads * rows;
   p.pre_parts = p.pre.wide ? (size_t)p.pre.splits * tokens * q_heads : (size_t)slots(p.pre, prefixes) * c->kv_heads * p.pre_q * group;
   p.bytes = (p.own_parts + p.pre_parts) * (c->head_dim + 2) * sizeof(float) + (size_t)(batch + prefixes) * sizeof(int2);
   const int64_t each = (p.own.wide ? p.own.splits : 1) + (p.pre.wide ? p.pre.splits : p.pre.shares / prefixes);
-  p.few = each <= kFewParts;
+  // a wave a row where they are many and of few parts, otherwise one for 32 channels of it: 4096 rows of 9 parts 13 us against 21, 2560 of 17 7 against 12;
+  // 128 of 8 6 against 4.5, 1024 of 33 10 against 7
+  p.few = each <= 20 && batch * max_q * q_heads >= 2048;
   p.joins = (int64_t)c->kv_heads * batch * rows * (p.few ? 1 : c->head_dim / kJoinCh);
   return p;
 }

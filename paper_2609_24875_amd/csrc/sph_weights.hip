@@ -124,7 +124,9 @@ __device__ __forceinline__ void write_sum(const WeightArgs& a, int b, int head, 
 
 // A wave's step of up to 32 rows: kBlocks times 16 keys in registers as they are stored, 8 KiB of 128 channels. Products are
 // v_mfma_f32_16x16x32_f16 with a column per key, whose 16 rows' scores lie in four lanes.
-template <int DIM, int BITS>
+//
+// UNI: pages of 16 tokens and more, each block of keys in one, so that scalars hold its address; smaller ones: each lane has its own key's.
+template <int DIM, int BITS, bool UNI>
 struct Step {
   typedef Lay<DIM, BITS> L;
   static constexpr int kWords = DIM * BITS / 128;            // a lane's registers of 16 keys
@@ -136,13 +138,23 @@ struct Step {
 #pragma unroll
     for (int u = 0; u < kBlocks; ++u) {
       const int p = pg.there(page[u]) ? page[u] : 0, key = kt + 16 * u + col;
-      const char* row = pg.row(pg.k, pg.stride, pg.token, p, key) + g4 * L::kPiece;
+      if constexpr (UNI) {
+        const int in_page = (kt + 16 * u) & pg.mask;
+        const int64_t off = p * pg.stride + (uint32_t)(in_page * pg.token), par_off = p * pg.par_stride + (uint32_t)(in_page * pg.par_token);
 #pragma unroll
-      for (int i = 0; i < L::kLoads; ++i) load_words<L::kPiece>(row + 4 * i * L::kPiece, k[u][i]);
-      if constexpr (BITS < 16) {
+        for (int i = 0; i < L::kLoads; ++i) {
+          load_row<L::kPiece, true>(pg.k, &off, pg.token, 0, col, col, (4 * i + g4) * L::kPiece, k[u][i]);
+          if constexpr (BITS < 16)
+            load_row<4, true>(pg.k_par, &par_off, pg.par_token, 0, col, col, g4 * L::kPieceCh / 32 * 4 + i * L::kPieceCh / 8 * 4, &par[u][i]);
+        }
+      } else {
+        const char* row = pg.row(pg.k, pg.stride, pg.token, p, key) + g4 * L::kPiece;
         const char* pr = pg.row(pg.k_par, pg.par_stride, pg.par_token, p, key) + g4 * L::kPieceCh / 32 * 4;
 #pragma unroll
-        for (int i = 0; i < L::kLoads; ++i) par[u][i] = *(const uint32_t*)(pr + i * L::kPieceCh / 8 * 4);
+        for (int i = 0; i < L::kLoads; ++i) {
+          load_words<L::kPiece>(row + 4 * i * L::kPiece, k[u][i]);
+          if constexpr (BITS < 16) par[u][i] = *(const uint32_t*)(pr + i * L::kPieceCh / 8 * 4);
+        }
       }
     }
   }
@@ -160,10 +172,10 @@ struct Step {
 // when one's products are done; with one sum for all heads the workgroup's waves take the heads in turn and meet in LDS.
 constexpr int kRun = 2;
 
-template <int DIM, int BITS, int NB>
-__global__ __launch_bounds__(kThreads) void k_weights_few(WeightArgs) {
+template <int DIM, int BITS, int NB, bool UNI>
+__global__ __launch_bounds__(kThreads, NB == 1 && DIM <= 128 && (UNI || BITS != 8) ? 4 : 2) void k_weights_few(WeightArgs) {
   const WeightArgs& a = *(const WeightArgs*)__builtin_amdgcn_kernarg_segment_ptr();
-  typedef Step<DIM, BITS> K;
+  typedef Step<DIM, BITS, UNI> K;
   typedef Lay<DIM, BITS> L;
   __shared__ float sum_s[kWaves][K::kKeys];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -200,7 +212,7 @@ __global__ __launch_bounds__(kThreads) void k_weights_few(WeightArgs) {
     // keys outside those that are seen take a page inside: they are read and not used
     auto pages_of = [&](int kt, int* page) __attribute__((always_inline)) {
 #pragma unroll
-      for (int u = 0; u < K::kBlocks; ++u) page[u] = pages[min(max((kt + 16 * u + col) >> pg.shift, e_lo), e_hi)];
+      for (int u = 0; u < K::kBlocks; ++u) page[u] = pages[min(max((kt + 16 * u + (UNI ? 0 : col)) >> pg.shift, e_lo), e_hi)];
     };
     f16x8 q[NB][L::kSteps];
     float lse[NB][4];
@@ -247,6 +259,8 @@ __global__ __launch_bounds__(kThreads) void k_weights_few(WeightArgs) {
             const f16x8 kf = T.piece(u, i, j);
 #pragma unroll
             for (int n = 0; n < NB; ++n) st[u][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(q[n][i * L::kBlocks + j], kf, st[u][n], 0, 0, 0);
+            // (decoded when they are needed: keys of all blocks at once would cost a wave a SIMD)
+            if (j == L::kBlocks - 1) __builtin_amdgcn_sched_barrier(0);
           }
       // not above the products: the loads would take registers of their own beside those that they refill
       __builtin_amdgcn_sched_barrier(0);
@@ -573,19 +587,24 @@ sph_status check_sizes(const sph_kv_cache* c, int64_t batch, int64_t tokens, int
   return SPH_OK;
 }
 
+template <int DIM, int BITS, int NB>
+const void* few_for(bool uni) {
+  return uni ? (const void*)k_weights_few<DIM, BITS, NB, true> : (const void*)k_weights_few<DIM, BITS, NB, false>;
+}
+
 template <int DIM, int BITS>
-const void* kernel_for(const Plan& p) {
-  return !p.few ? (const void*)k_weights_many<DIM, BITS> : p.nb == 1 ? (const void*)k_weights_few<DIM, BITS, 1> : (const void*)k_weights_few<DIM, BITS, 2>;
+const void* kernel_for(const Plan& p, bool uni) {
+  return !p.few ? (const void*)k_weights_many<DIM, BITS> : p.nb == 1 ? few_for<DIM, BITS, 1>(uni) : few_for<DIM, BITS, 2>(uni);
 }
 
 template <int BITS>
-const void* kernel_for(const Plan& p, int dim) {
+const void* kernel_for(const Plan& p, int dim, bool uni) {
   switch (dim) {
-    case 64: return kernel_for<64, BITS>(p);
-    case 96: return kernel_for<96, BITS>(p);
-    case 128: return kernel_for<128, BITS>(p);
-    case 192: return kernel_for<192, BITS>(p);
-    default: return kernel_for<256, BITS>(p);
+    case 64: return kernel_for<64, BITS>(p, uni);
+    case 96: return kernel_for<96, BITS>(p, uni);
+    case 128: return kernel_for<128, BITS>(p, uni);
+    case 192: return kernel_for<192, BITS>(p, uni);
+    default: return kernel_for<256, BITS>(p, uni);
   }
 }
 
@@ -654,7 +673,8 @@ sph_status sph_attention_weights(const sph_kv_cache* cache, int64_t batch, int64
   a.max_q = (int)max_q, a.max_len = (int)max_len, a.window = p.window, a.heads = heads, a.tiles = p.tiles, a.splits = p.splits;
   a.scale = scale * kLog2e;
   const int bits = cache->bits, dim = cache->head_dim;
-  const void* fn = bits == 16 ? kernel_for<16>(p, dim) : bits == 8 ? kernel_for<8>(p, dim) : kernel_for<4>(p, dim);
+  const bool uni = cache->page_size >= 16;
+  const void* fn = bits == 16 ? kernel_for<16>(p, dim, uni) : bits == 8 ? kernel_for<8>(p, dim, uni) : kernel_for<4>(p, dim, uni);
   if (!launch_ok(fn, p.grid, (hipStream_t)stream, a)) return SPH_ERR_HIP;
   if (p.join && !launch_ok((const void*)k_weights_join, p.joins, (hipStream_t)stream, a)) return SPH_ERR_HIP;
   return SPH_OK;

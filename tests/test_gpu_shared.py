@@ -251,7 +251,8 @@ def test_wrong_values_are_nan(size, new):
 
 def test_wrong_starts_of_tokens():
     c = Case([70], [4], [60] * 4, [40] * 4)
-    for start in ([0, -1, 80, 120, 160], [0, 40, 39, 120, 160], [0, 40, 80, 120, 161], [0, 40, 80, 2 ** 31 - 1, -2 ** 31], [7, 7, 7, 7, 7]):
+    for start in ([0, -1, 80, 120, 160], [0, 40, 39, 120, 160], [0, 40, 80, 120, 161], [0, 40, 80, 2 ** 31 - 1, -2 ** 31], [7, 7, 7, 7, 7],
+                  [-2 ** 31, 40, 80, 120, 160], [-2 ** 31, 2 ** 31 - 1, -5, 2 ** 31 - 1, 160]):
         c.run(q_start=_i32(start))
     torch.cuda.synchronize()
     # one sequence claims more than max_q: all its tokens are NaN, and the others' prefix holds no more than it may
