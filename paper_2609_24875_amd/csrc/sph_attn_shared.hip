@@ -162,6 +162,12 @@ SharedPlan shared_plan(const sph_kv_cache* c, int64_t prefixes, int64_t max_grou
   p.own = plan_of(c, batch, q_heads, max_q, max_len, 0);
   p.pre = plan_of(c, prefixes, q_heads, p.pre_q, max_prefix, 0);
   p.own.fold = p.pre.fold = 0;             // (for workgroups that are alone in their launch)
+  if (!p.pre.wide && !p.pre.shares && prefixes == 1 && max_prefix > kTile * kWaves) {
+    // (joined anyway, and one prefix is shared out without counting: 1031 tokens by one workgroup a kv head .. us, by nine .. )
+    const int64_t steps = (max_prefix + kTile * kWaves - 1) / (kTile * kWaves);
+    p.pre.shares = (int)std::min<int64_t>(steps + 1, std::max<int64_t>(1, kCus * workgroups_per_cu(c) / c->kv_heads));
+    p.pre.grid = (int64_t)c->kv_heads * p.pre.shares;
+  }
   if (p.pre.wide) {
     // A workgroup a CU, beside which the own tokens' are, and two where prefixes are several, since ragged ones leave many with little to do. One
     // prefix of 32768 tokens before 128 sequences of 1024 161 us, with two 195; 8 of up to 4099 before 8 each of up to 700 at 8 bits 48 and 46.

@@ -1,7 +1,7 @@
 // Eviction from the paged cache by accumulated attention weight: sph_kv_evict.
 //
 // Two launches. k_evict_choose, a workgroup a sequence and row of sums, finds the sum of the last token that is kept (the m-th largest
-// among those that have to compete) digit by digit, then gives every kept token its place by counting in order. k_evict_move takes their keys and
+// among those that have to compete) digit by digit (of 12, 12 and 8 bits), then gives every kept token its place by counting in order. k_evict_move takes their keys and
 // values there. Tokens keep their order, so a token's place is never behind where it was: moved inside the same pages, in ascending
 // order and read before the same step's places are written, none is overwritten before it is read.
 #include <hip/hip_runtime.h>
@@ -30,7 +30,8 @@ struct EvictArgs {
   int heads, keep, recent, first, bits, chunks;
 };
 
-constexpr int kChooseThreads = 1024, kChooseWaves = kChooseThreads / 64, kDigits = 256, kCopies = 4;
+// (digits of 12, 12 and 8 bits: the first has a sum's sign, exponent and three bits more, the second mostly decides)
+constexpr int kChooseThreads = 1024, kChooseWaves = kChooseThreads / 64, kDigits = 4096;
 
 // Sums in the order of whole numbers: NaN above everything, -0 as 0. No sum gives 0, which stands for none.
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -48,12 +49,28 @@ struct Keys {
   uint32_t k[R ? R : 1];
   const float* row;
   int count;               // tokens of the wave, 0 and less for none
-  __device__ __forceinline__ uint32_t read(int c, int lane) const { return 64 * c + lane < count ? ordered(row[64 * c + lane]) : 0u; }
+  // keys of chunks c .. c + N - 1 (all loads on their way together: none is behind a branch)
+  template <int N>
+  __device__ __forceinline__ void read(int c, int lane, uint32_t* x) const {
+    float v[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = row[min(64 * (c + i) + lane, count - 1)];
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = 64 * (c + i) + lane < count ? ordered(v[i]) : 0u;
+  }
   __device__ __forceinline__ void load(const float* r, int n, int lane) {
     row = r, count = n;
-    if constexpr (R > 0)
+    if constexpr (R > 0) {
+      if (count <= 0) return;
 #pragma unroll
-      for (int c = 0; c < R; ++c) k[c] = read(c, lane);
+      for (int c = 0; c < R; c += 16) {
+        if (64 * c < count)
+          read<16>(c, lane, k + c);
+        else
+#pragma unroll
+          for (int i = 0; i < 16; ++i) k[c + i] = 0u;
+      }
+    }
   }
   template <typename F>
   __device__ __forceinline__ void each(int lane, F f) const {
@@ -65,8 +82,7 @@ struct Keys {
       // (eight loads on their way together)
       for (int c0 = 0; 64 * c0 < count; c0 += 8) {
         uint32_t x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = read(c0 + i, lane);
+        read<8>(c0, lane, x);
 #pragma unroll
         for (int i = 0; i < 8; ++i) f(c0 + i, x[i]);
       }
@@ -74,12 +90,13 @@ struct Keys {
   }
 };
 
-// Bound by the latency of its passes over the sums (which stay in registers), four of them at most, one for each digit.
+// Bound by the latency of its passes over the sums (which stay in registers), three of them at most, one for each digit.
 template <int R>
 __global__ __launch_bounds__(kChooseThreads) void k_evict_choose(EvictArgs a) {
-  __shared__ uint32_t hist[kCopies][kDigits];
+  __shared__ __attribute__((aligned(16))) uint32_t hist[kDigits];
   __shared__ int found[3];                                   // digit, tokens above it, tokens with it
   __shared__ int gts[kChooseWaves], eqs[kChooseWaves];
+  __shared__ uint32_t totals[kChooseWaves];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int b = blockIdx.x / a.heads, h = blockIdx.x % a.heads;
   const int n = a.lens[b];
@@ -105,50 +122,46 @@ __global__ __launch_bounds__(kChooseThreads) void k_evict_choose(EvictArgs a) {
     if (m > 0) {
       bool open = true;
 #pragma unroll 1
-      for (int shift = 24; shift >= 0 && open; shift -= 8) {
-        for (int i = threadIdx.x; i < kCopies * kDigits; i += kChooseThreads) (&hist[0][0])[i] = 0;
+      for (int shift = 20; shift >= 0 && open; shift = shift == 20 ? 8 : shift == 8 ? 0 : -1) {
+        const uint32_t digits = shift ? kDigits : 256;
+        ((uint4*)hist)[threadIdx.x] = make_uint4(0, 0, 0, 0);
         __syncthreads();
-        uint32_t* mine = hist[wave % kCopies];
         keys.each(lane, [&](int, uint32_t key) {
           const bool in = key != 0 && (key & mask) == prefix;
           const uint64_t act = __ballot(in);
           if (!act) return;
           // one digit often has most of the tokens (those that got nothing): the first lane's is counted at once
-          const uint32_t digit = key >> shift & (kDigits - 1);
+          const uint32_t digit = key >> shift & (digits - 1);
           const int lead = __builtin_ctzll(act);
           const uint32_t lead_digit = __builtin_amdgcn_readlane(digit, lead);
           const uint64_t same = __ballot(in && digit == lead_digit);
           if (lane == lead)
-            atomicAdd(&mine[lead_digit], (uint32_t)__builtin_popcountll(same));
+            atomicAdd(&hist[lead_digit], (uint32_t)__builtin_popcountll(same));
           else if (in && digit != lead_digit)
-            atomicAdd(&mine[digit], 1u);
+            atomicAdd(&hist[digit], 1u);
         });
         __syncthreads();
-        if (wave == 0) {
-          // lane l has digits 255 - 4 l .. 252 - 4 l: tokens from the top down to each
-          uint32_t cnt[4], sum = 0;
+        // thread t has digits 4095 - 4 t .. 4092 - 4 t: tokens from the top down to each
+        const uint4 four = ((const uint4*)hist)[kDigits / 4 - 1 - threadIdx.x];
+        const uint32_t cnt[4] = {four.w, four.z, four.y, four.x}, sum = (cnt[0] + cnt[1]) + (cnt[2] + cnt[3]);
+        uint32_t upto = sum;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            cnt[i] = 0;
-            for (int c = 0; c < kCopies; ++c) cnt[i] += hist[c][kDigits - 1 - 4 * lane - i];
-            sum += cnt[i];
-          }
-          uint32_t upto = sum;
+        for (int d = 1; d < 64; d <<= 1) {
+          const uint32_t v = __shfl_up(upto, d);
+          upto += lane >= d ? v : 0;
+        }
+        if (lane == 63) totals[wave] = upto;
+        __syncthreads();
+        uint32_t above = upto - sum;
+        for (int w = 0; w < wave; ++w) above += totals[w];
 #pragma unroll
-          for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t v = __shfl_up(upto, d);
-            upto += lane >= d ? v : 0;
-          }
-          uint32_t above = upto - sum;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (above < (uint32_t)want && above + cnt[i] >= (uint32_t)want) found[0] = kDigits - 1 - 4 * lane - i, found[1] = above, found[2] = cnt[i];
-            above += cnt[i];
-          }
+        for (int i = 0; i < 4; ++i) {
+          if (above < (uint32_t)want && above + cnt[i] >= (uint32_t)want) found[0] = kDigits - 1 - 4 * threadIdx.x - i, found[1] = above, found[2] = cnt[i];
+          above += cnt[i];
         }
         __syncthreads();
         prefix |= (uint32_t)found[0] << shift;
-        mask |= (uint32_t)(kDigits - 1) << shift;
+        mask |= (digits - 1) << shift;
         want -= found[1];
         open = want < found[2];                              // otherwise all tokens with these digits are kept
       }
