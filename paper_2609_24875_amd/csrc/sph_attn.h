@@ -34,6 +34,7 @@ struct AttnArgs {
   // (fold: tiles of rows between k_attn_wide's workgroups that share a CU, 0 for the longest first)
   bool stream;             // k_attn reads values past the caches
   float scale;             // times log2 e
+  int each;                // of kParts: workgroups a sequence and kv head, 0: one, or shares that are counted
 };
 
 // The kernel for more rows a kv head than k_attn takes, and its rows a workgroup and keys a tile.

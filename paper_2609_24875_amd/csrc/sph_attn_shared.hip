@@ -55,7 +55,7 @@ __global__ __launch_bounds__(kThreads) void k_attn_shared_join(SharedArgs both) 
   const int64_t token = (int64_t)s.start + row / a.group;
   const int g = prefix_of(p, b);
   int2 w = make_int2(b, both.own_many ? a.splits : 1);
-  if (!both.own_many && a.shares) w = a.where[b];
+  if (!both.own_many && (a.shares || a.each)) w = a.where[b];
   const int64_t first = part_at(a, w.x, kvh, row), step = part_at(a, w.x + (both.own_many ? a.batch : 1), kvh, row) - first;
   int64_t pre_first = 0, pre_step = 0;
   int parts = w.y, pre_parts = 0;
@@ -70,15 +70,15 @@ __global__ __launch_bounds__(kThreads) void k_attn_shared_join(SharedArgs both) 
       pre_step = (int64_t)a.c.kv_heads * (a.tokens * a.group);
       pre_first = both.pre_part + (int64_t)kvh * (a.tokens * a.group) + at * a.group + row % a.group, pre_parts = p.splits;
     } else {
-      w = p.shares ? p.where[g] : make_int2(g, 1);
+      w = p.shares || p.each ? p.where[g] : make_int2(g, 1);
       const int r = (int)min(max(token - q.start, (int64_t)0), (int64_t)p.max_q - 1) * a.group + row % a.group;
       pre_first = part_at(p, w.x, kvh, r), pre_step = part_at(p, w.x + 1, kvh, r) - pre_first, pre_parts = w.y;
       pre_first += both.pre_part;
     }
   }
   // (slots that no sequence wrote are anything)
-  if (!both.own_many && a.shares && (s.n == 0 || bad)) parts = 0;
-  if (!both.pre_many && p.shares && bad) pre_parts = 0;
+  if (!both.own_many && (a.shares || a.each) && (s.n == 0 || bad)) parts = 0;
+  if (!both.pre_many && (p.shares || p.each) && bad) pre_parts = 0;
   const int all = parts + pre_parts;
   auto at_of = [&](int i) { return i < parts ? first + i * step : pre_first + (i - parts) * pre_step; };
   constexpr int kLoads = 5;                                  // of a lane before it knows the maximum
@@ -148,11 +148,25 @@ __global__ __launch_bounds__(kThreads) void k_attn_shared_join(SharedArgs both) 
 struct SharedPlan {
   Plan own, pre;
   int64_t pre_q;                           // tokens behind a prefix at most
+  int own_each, pre_each;                  // workgroups a sequence (see AttnArgs)
   size_t own_parts, pre_parts, bytes;
   int64_t joins;
   bool few;
   SharedKind kind;
 };
+
+// Rows that are joined anyway can do with more workgroups than k_attn's plan gives short sequences: up to one a CU, by the host's bounds and without
+// counting shares, and so for one sequence of any length. Three sequences behind 512 tokens 8.8 us with four workgroups a kv head for the prefix, 11.7
+// with one; behind 768 8.5 and 14.3; four behind 1031 9.6, with shares that are counted 11.9.
+int each_of(const sph_kv_cache* c, Plan& p, int64_t n, int64_t max_len) {
+  if (p.wide || !n || (p.shares && n > 1)) return 0;
+  const int64_t steps = (max_len + kTile * kWaves - 1) / (kTile * kWaves);
+  const int64_t most = n == 1 ? std::max<int64_t>(1, kCus * workgroups_per_cu(c) / c->kv_heads) : kCus / (c->kv_heads * n);
+  const int64_t each = std::min({steps, most, (int64_t)kMaxSplits});
+  if (each < 2) return 0;
+  p.shares = 0, p.grid = c->kv_heads * n * each;
+  return (int)each;
+}
 
 SharedPlan shared_plan(const sph_kv_cache* c, int64_t prefixes, int64_t max_group, int64_t max_prefix, int64_t batch, int64_t tokens,
                        int q_heads, int64_t max_q, int64_t max_len) {
@@ -162,12 +176,7 @@ SharedPlan shared_plan(const sph_kv_cache* c, int64_t prefixes, int64_t max_grou
   p.own = plan_of(c, batch, q_heads, max_q, max_len, 0);
   p.pre = plan_of(c, prefixes, q_heads, p.pre_q, max_prefix, 0);
   p.own.fold = p.pre.fold = 0;             // (for workgroups that are alone in their launch)
-  if (!p.pre.wide && !p.pre.shares && prefixes == 1 && max_prefix > kTile * kWaves) {
-    // (joined anyway, and one prefix is shared out without counting: 1031 tokens by one workgroup a kv head .. us, by nine .. )
-    const int64_t steps = (max_prefix + kTile * kWaves - 1) / (kTile * kWaves);
-    p.pre.shares = (int)std::min<int64_t>(steps + 1, std::max<int64_t>(1, kCus * workgroups_per_cu(c) / c->kv_heads));
-    p.pre.grid = (int64_t)c->kv_heads * p.pre.shares;
-  }
+  p.own_each = each_of(c, p.own, batch, max_len), p.pre_each = each_of(c, p.pre, prefixes, max_prefix);
   if (p.pre.wide) {
     // A workgroup a CU, beside which the own tokens' are, and two where prefixes are several, since ragged ones leave many with little to do. One
     // prefix of 32768 tokens before 128 sequences of 1024 161 us, with two 195; 8 of up to 4099 before 8 each of up to 700 at 8 bits 48 and 46.
@@ -178,11 +187,12 @@ SharedPlan shared_plan(const sph_kv_cache* c, int64_t prefixes, int64_t max_grou
     p.pre.grid = units * p.pre.splits;
   }
   p.kind = p.own.wide ? kManyMany : p.pre.wide ? kManyFew : kFewFew;
-  const auto slots = [](const Plan& q, int64_t n) { return q.wide ? q.splits * n : q.shares ? q.shares + n : n; };
-  p.own_parts = (size_t)slots(p.own, batch) * c->kv_heads * rows;
-  p.pre_parts = p.pre.wide ? (size_t)p.pre.splits * tokens * q_heads : (size_t)slots(p.pre, prefixes) * c->kv_heads * p.pre_q * group;
+  const auto slots = [](const Plan& q, int each, int64_t n) { return q.wide ? q.splits * n : each ? each * n : q.shares ? q.shares + n : n; };
+  p.own_parts = (size_t)slots(p.own, p.own_each, batch) * c->kv_heads * rows;
+  p.pre_parts = p.pre.wide ? (size_t)p.pre.splits * tokens * q_heads : (size_t)slots(p.pre, p.pre_each, prefixes) * c->kv_heads * p.pre_q * group;
   p.bytes = (p.own_parts + p.pre_parts) * (c->head_dim + 2) * sizeof(float) + (size_t)(batch + prefixes) * sizeof(int2);
-  const int64_t each = (p.own.wide ? p.own.splits : 1) + (p.pre.wide ? p.pre.splits : p.pre.shares / prefixes);
+  const int64_t each = (p.own.wide ? p.own.splits : std::max(1, p.own_each)) +
+                       (p.pre.wide ? p.pre.splits : p.pre_each ? p.pre_each : 1 + p.pre.shares / prefixes);
   // a wave a row where they are many and of few parts, otherwise one for 32 channels of it: 4096 rows of 9 parts 13 us against 21, 2560 of 17 7 against 12;
   // 128 of 8 6 against 4.5, 1024 of 33 10 against 7
   p.few = each <= 20 && batch * max_q * q_heads >= 2048;
@@ -264,10 +274,12 @@ sph_status sph_attention_shared(const sph_kv_cache* cache, int64_t prefixes, con
   (AttnArgs&)both.pre = a;
   const auto planned = [](AttnArgs& x, const Plan& q) { x.tiles = (int)q.tiles, x.splits = q.splits, x.chunk = q.chunk, x.shares = q.shares; };
   planned(a, p.own);
+  both.own.each = p.own_each;
   a.pages = d_pages, a.pages_stride = pages_stride, a.lens = d_seq_lens;
   a.batch = (int)batch, a.max_q = (int)max_q, a.max_len = (int)max_len;
   PrefixArgs& b = both.pre;
   planned(b, p.pre);
+  b.each = p.pre_each;
   b.pages = d_prefix_pages, b.pages_stride = prefix_stride, b.lens = d_prefix_lens;
   b.batch = (int)prefixes, b.max_q = (int)p.pre_q, b.max_len = (int)max_prefix;
   b.first = d_first, b.seqs = (int)batch;

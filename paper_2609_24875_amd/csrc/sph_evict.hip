@@ -90,13 +90,20 @@ struct Keys {
   }
 };
 
+// The sum of the numbers of the waves before this one, all read at once.
+__device__ __forceinline__ uint32_t before_wave(const uint32_t* of, int wave) {
+  uint32_t sum = 0;
+#pragma unroll
+  for (int w = 0; w < kChooseWaves; ++w) sum += w < wave ? of[w] : 0u;
+  return sum;
+}
+
 // Bound by the latency of its passes over the sums (which stay in registers), three of them at most, one for each digit.
 template <int R>
 __global__ __launch_bounds__(kChooseThreads) void k_evict_choose(EvictArgs a) {
   __shared__ __attribute__((aligned(16))) uint32_t hist[kDigits];
   __shared__ int found[3];                                   // digit, tokens above it, tokens with it
-  __shared__ int gts[kChooseWaves], eqs[kChooseWaves];
-  __shared__ uint32_t totals[kChooseWaves];
+  __shared__ __attribute__((aligned(16))) uint32_t gts[kChooseWaves], eqs[kChooseWaves], totals[kChooseWaves];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int b = blockIdx.x / a.heads, h = blockIdx.x % a.heads;
   const int n = a.lens[b];
@@ -130,15 +137,13 @@ __global__ __launch_bounds__(kChooseThreads) void k_evict_choose(EvictArgs a) {
           const bool in = key != 0 && (key & mask) == prefix;
           const uint64_t act = __ballot(in);
           if (!act) return;
-          // one digit often has most of the tokens (those that got nothing): the first lane's is counted at once
+          // (tokens that are all alike, as those that got nothing yet, are counted at once)
           const uint32_t digit = key >> shift & (digits - 1);
-          const int lead = __builtin_ctzll(act);
-          const uint32_t lead_digit = __builtin_amdgcn_readlane(digit, lead);
-          const uint64_t same = __ballot(in && digit == lead_digit);
-          if (lane == lead)
-            atomicAdd(&hist[lead_digit], (uint32_t)__builtin_popcountll(same));
-          else if (in && digit != lead_digit)
+          if (act == ~0ull && __all(digit == (uint32_t)__builtin_amdgcn_readfirstlane(digit))) {
+            if (lane == 0) atomicAdd(&hist[digit], 64u);
+          } else if (in) {
             atomicAdd(&hist[digit], 1u);
+          }
         });
         __syncthreads();
         // thread t has digits 4095 - 4 t .. 4092 - 4 t: tokens from the top down to each
@@ -152,8 +157,7 @@ __global__ __launch_bounds__(kChooseThreads) void k_evict_choose(EvictArgs a) {
         }
         if (lane == 63) totals[wave] = upto;
         __syncthreads();
-        uint32_t above = upto - sum;
-        for (int w = 0; w < wave; ++w) above += totals[w];
+        uint32_t above = upto - sum + before_wave(totals, wave);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           if (above < (uint32_t)want && above + cnt[i] >= (uint32_t)want) found[0] = kDigits - 1 - 4 * threadIdx.x - i, found[1] = above, found[2] = cnt[i];
@@ -175,8 +179,7 @@ __global__ __launch_bounds__(kChooseThreads) void k_evict_choose(EvictArgs a) {
     });
     if (lane == 0) gts[wave] = gt, eqs[wave] = eq;
     __syncthreads();
-    gt = eq = 0;
-    for (int w = 0; w < wave; ++w) gt += gts[w], eq += eqs[w];
+    gt = (int)before_wave(gts, wave), eq = (int)before_wave(eqs, wave);
     keys.each(lane, [&](int c, uint32_t key) {
       const uint64_t g = __ballot(key > bar), e = __ballot(key == bar);
       const int eq_before = eq + lanes_below(e);
