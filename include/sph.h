@@ -457,7 +457,8 @@ sph_status sph_attention_shared_workspace_bytes(const sph_kv_cache* cache, int64
  * Keys that no row sees are never used, whatever they hold. A sequence whose length, start or count is outside its range gets NaN, a token of a page outside
  * the pool that some row sees, too. Sums are held in fp32, in an order fixed by the arguments: repeated calls give bitwise
  * identical results. d_ws: at least sph_attention_weights_workspace_bytes, 256-byte aligned, no initial contents; concurrent calls must not share one.
- * SPH_ERR_SHAPE also where a launch would pass 2^24 workgroups, of 128 (above 128 channels a head) or 256 tokens of max_len each and more. Asynchronous. */
+ * SPH_ERR_SHAPE also where a launch would pass 2^24 workgroups: up to 32 new rows a kv head, one for every sequence, kv head and 128 to 512 tokens of max_len (by the
+ * bytes of a token's key; with one sum for all heads one for every sequence and 16 to 64 tokens), otherwise for every sequence, kv head and 128 or 256. Asynchronous. */
 sph_status sph_attention_weights(const sph_kv_cache* cache, int64_t batch, int64_t tokens, int32_t q_heads, const void* d_q,
                                  int64_t q_token_stride, int64_t q_head_stride, const int32_t* d_q_start, int64_t max_q,
                                  const int32_t* d_pages, int64_t pages_stride, const int32_t* d_seq_lens, int64_t max_len, int64_t window,

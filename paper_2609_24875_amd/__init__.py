@@ -4,6 +4,6 @@ from .sph import (EXPORTS, FORMATS, LIB_PATH, SphError, SphLibraryMissing, SphWe
                   kmeans_codebook, kmeans_workspace_bytes, load_library, pack, packed_bytes, status_str,
                   unpack, workspace_bytes)
 from .attn import (KVCache, attention, attention_shared, attention_shared_workspace_bytes,  # noqa: F401
-                   attention_weights, attention_weights_workspace_bytes, attention_workspace_bytes, kv_append, kv_evict, kv_read, rope, rope_axes, rope_frequencies,
-                   rope_table)
+                   attention_weights, attention_weights_workspace_bytes, attention_workspace_bytes, kv_append, kv_evict,
+                   kv_read, rope, rope_axes, rope_frequencies, rope_table)
 from .block import AttentionBlock  # noqa: F401
