@@ -69,7 +69,7 @@ struct Axes {
 
 // As Turn, with each pair at the position along its own axis; NaN too for an axis that there is not. A row's runs mostly lie in one
 // axis's share of the pairs, so that lanes read whole lines of the table; where axes alternate, its pairs come from as many rows. These
-// stay in the caches, so that memory bounds the kernels as before (8192 tokens of 48 heads of 128 fp16 channels along three axes 38 us, along one 35.5).
+// stay in the caches, so that memory bounds k_rope as before (8192 tokens of 48 heads of 128 fp16 channels along three axes 38 us, along one 35.5).
 template <int N>
 struct TurnAxes : Turn<N> {
   __device__ __forceinline__ void load(const float* table, int64_t max_pos, int half, const int32_t* pos, const Axes& x, int pair, float sign) {
@@ -281,29 +281,66 @@ __device__ __forceinline__ float quad_max(float v) {
   return fmaxf(v, quad<0x4E>(v));
 }
 
+// With several axes the angles of a block's tokens come together in LDS, since all heads of a token turn alike: `count` tokens' from t0 on, each pair's
+// from the table by one thread (8192 tokens of 32 query and 8 kv heads into 4 bits 44 us; each thread's eight pairs by itself 53; along one axis 39.5). At most 7 tokens of 96 pairs (256 units of eight channels, of which a token of one head of 192 has 48).
+constexpr int kBlockPairs = 7 * 96;
+
+__device__ __forceinline__ void load_pairs(const AppendArgs& a, int64_t t0, int count, float2* pairs) {
+  const int half = a.rot / 2, all = count * half;
+  for (int i = threadIdx.x; i < all; i += kThreads) {
+    const int t = i / half, pair = i - t * half, axis = a.q.axes.of[pair];
+    const bool known = axis < a.q.axes.count;
+    const int p = a.pos[t0 + t + (known ? axis * a.q.axes.stride : 0)];
+    const bool there = known && (unsigned)p < (uint64_t)a.max_pos;
+    const float one = there ? 1.0f : __builtin_nanf("");
+    const float2 w = ((const float2*)a.table)[(there ? (int64_t)p : 0) * half + pair];
+    pairs[i] = make_float2(one * w.x, a.sign * one * w.y);
+  }
+}
+
+template <int N>
+__device__ __forceinline__ void take_pairs(Turn<N>& w, const float2* pairs) {
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    const f32x4 x = ((const f32x4*)pairs)[i];
+    w.c[2 * i] = x[0], w.s[2 * i] = x[1], w.c[2 * i + 1] = x[2], w.s[2 * i + 1] = x[3];
+  }
+}
+
 // One thread writes eight channels of one key or value row; four neighbouring lanes share an offset and a step.
-// A rotated key's partner channels are read beside its own.
+// A rotated key's partner channels are read beside its own. AXES: all threads of a block come here, those behind the last token with it.
 template <typename T, int BITS, bool INTER, bool AXES>
-__device__ __forceinline__ void append_unit(const AppendArgs& a, int64_t token, uint32_t unit) {
+__device__ __forceinline__ void append_unit(const AppendArgs& a, int64_t token, uint32_t unit, int64_t t0 = 0, int count = 0, float2* pairs = nullptr) {
   const CacheView& c = a.c;
   const uint32_t per_row = (uint32_t)c.dim / 8, per_kind = per_row * c.kv_heads;
   const bool is_v = unit >= per_kind;
   unit -= is_v ? per_kind : 0;
   const int head = unit / per_row, ch = 8 * (unit % per_row);
+  const bool last = AXES && token >= a.tokens;
+  if constexpr (AXES) token = min(token, a.tokens - 1);
   const int slot = a.slots[token];
-  if ((unsigned)slot >= (uint64_t)c.n_slots) return;  // the four lanes of a token's 32 channels leave together
+  if (!AXES && (unsigned)slot >= (uint64_t)c.n_slots) return;  // the four lanes of a token's 32 channels leave together
   const char* row = is_v ? a.v + token * a.vt + head * a.vh : a.k + token * a.kt + head * a.kh;
   Row8<T> r;
   r.load(row + ch * sizeof(T));
   float x[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = r.at(i);
+  Row8<T> other;
+  if constexpr (AXES) {
+    // (rows on their way beside the angles)
+    const int half = a.rot / 2;
+    if (!INTER && !is_v && ch < a.rot) other.load(row + (ch < half ? ch + half : ch - half) * sizeof(T));
+    load_pairs(a, t0, count, pairs);
+    __syncthreads();
+    if (last || (unsigned)slot >= (uint64_t)c.n_slots) return;
+  }
   if (!is_v && a.pos && ch < a.rot) {
     const int half = a.rot / 2;
     Turn<8> w;
     if constexpr (AXES && INTER) {
-      TurnAxes<4> u;
-      u.load(a.table, a.max_pos, half, a.pos + token, a.q.axes, ch / 2, a.sign);
+      Turn<4> u;
+      take_pairs(u, pairs + (token - t0) * half + ch / 2);
 #pragma unroll
       for (int j = 0; j < 4; ++j) turn(x[2 * j], x[2 * j + 1], u.c[j], u.s[j]);
     } else if (INTER) {
@@ -319,14 +356,15 @@ __device__ __forceinline__ void append_unit(const AppendArgs& a, int64_t token, 
     } else {
       const bool low = ch < half;
       if constexpr (AXES) {
-        TurnAxes<8> u;
-        u.load(a.table, a.max_pos, half, a.pos + token, a.q.axes, low ? ch : ch - half, a.sign);
-        w = u;
+        take_pairs(w, pairs + (token - t0) * half + (low ? ch : ch - half));
       } else {
         w.load(a.table, a.max_pos, half, a.pos[token], low ? ch : ch - half, a.sign);
       }
       Row8<T> o;
-      o.load(row + (low ? ch + half : ch - half) * sizeof(T));
+      if constexpr (AXES)
+        o = other;
+      else
+        o.load(row + (low ? ch + half : ch - half) * sizeof(T));
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         float first = low ? x[i] : o.at(i), second = low ? o.at(i) : x[i];
@@ -400,7 +438,15 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(AppendArgs a) {
       return;
     }
   }
-  place(kv_block, (uint32_t)(a.c.dim / 8) * 2 * a.c.kv_heads, token, unit);
+  const uint32_t per = (uint32_t)(a.c.dim / 8) * 2 * a.c.kv_heads;
+  place(kv_block, per, token, unit);
+  if constexpr (AXES) {
+    __shared__ __attribute__((aligned(16))) float2 pairs[kBlockPairs];
+    const uint64_t at = (uint64_t)kv_block * kThreads;
+    const int64_t t0 = (int64_t)(at / per);
+    append_unit<T, BITS, INTER, AXES>(a, token, unit, t0, (int)(min((int64_t)((at + kThreads - 1) / per), a.tokens - 1) - t0) + 1, pairs);
+    return;
+  }
   if (token >= a.tokens) return;
   append_unit<T, BITS, INTER, AXES>(a, token, unit);
 }
@@ -458,9 +504,11 @@ bool blocks_for(int64_t tokens, int64_t per, uint32_t* blocks) {
 
 // Heads a thread rotates: as many as leave about four waves a SIMD (2^18 threads), four at a time, so that a token's
 // angles are read once for them.
-int heads_per_thread(int64_t tokens, int heads, int units) {
+// Angles along several axes are dearer to read, so four heads at least, whose loads are on their way together anyway: 1369 tokens of 32 query and 8 kv
+// heads of 128 fp16 channels into 8 bits 12 us, one head a thread 18.
+int heads_per_thread(int64_t tokens, int heads, int units, bool axes) {
   const int64_t threads = tokens * heads * units;
-  const int64_t want = std::max<int64_t>(1, threads >> 18);
+  const int64_t want = std::max<int64_t>(axes ? std::min(heads, 4) : 1, threads >> 18);
   return want < 4 ? (int)want : (int)std::min<int64_t>((want + 3) / 4 * 4, std::min(heads, 16));
 }
 
@@ -568,7 +616,7 @@ sph_status rope_call(const sph_rope_desc* rope, const Axes* axes, sph_dtype dtyp
   a.pos = d_pos, a.table = rope->d_table, a.max_pos = rope->max_pos;
   a.tokens = tokens, a.heads = heads, a.dim = head_dim, a.rot = rope->rot_dim;
   const int units = head_dim * size / 32;
-  a.hpt = heads_per_thread(tokens, heads, units);
+  a.hpt = heads_per_thread(tokens, heads, units, axes);
   a.sign = rope->flags & SPH_ROPE_INVERSE ? -1.0f : 1.0f;
   uint32_t blocks;
   if (!blocks_for(tokens, units, &blocks)) return SPH_ERR_SHAPE;
@@ -625,7 +673,7 @@ sph_status append_call(const sph_kv_cache* cache, const sph_rope_desc* rope, con
     q.pos = d_pos, q.table = rope->d_table, q.max_pos = rope->max_pos, q.sign = a.sign;
     q.tokens = tokens, q.heads = q_heads, q.dim = cache->head_dim, q.rot = rope->rot_dim;
     const int units = cache->head_dim * size / 32;
-    q.hpt = heads_per_thread(tokens, q_heads, units);
+    q.hpt = heads_per_thread(tokens, q_heads, units, axes);
     if (!blocks_for(tokens, units, &unit_blocks)) return SPH_ERR_SHAPE;
     a.q_head_blocks = (uint32_t)((q_heads + q.hpt - 1) / q.hpt);
     q_blocks = (uint64_t)unit_blocks * a.q_head_blocks;

@@ -185,6 +185,34 @@ def test_cache_written_with_axes_holds_the_rotated_rows(dim, sections, cycled, b
         assert torch.equal(a.k_par, b.k_par) and torch.equal(a.v_par, b.v_par)
 
 
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("tokens", [1, 2, 6, 21, 131])
+@pytest.mark.parametrize("kv,dim,rot", [(1, 64, 64), (1, 96, 96), (1, 192, 192), (3, 64, 48), (5, 96, 96), (2, 192, 176), (1, 256, 256), (16, 256, 64)])
+def test_cache_tokens_that_begin_anywhere_in_a_workgroup(kv, dim, rot, tokens, inter):
+    """Tokens of few and many heads, also such that a workgroup ends inside one: keys as rope turns them, with wrong positions and axes and
+    padding tokens among them."""
+    n_axes = 3
+    table = pkg.rope_table(rot, 50)
+    axes = torch.randint(0, n_axes, (rot // 2,), generator=_gen(31), device=DEV).to(torch.uint8)
+    axes[5] = 77
+    pos = _positions(n_axes, tokens, 50, seed=32)
+    pos[1, tokens // 2] = 50
+    rows = _randn(tokens, 2 * kv, dim, seed=33)
+    slots = torch.randperm(2 * tokens + 16, generator=_gen(34), device=DEV)[:tokens].int()
+    if tokens > 5:
+        slots[tokens - 2] = -1
+    cache = pkg.KVCache.empty((2 * tokens + 16 + 7) // 8, kv, dim, page_size=8)
+    cache.k.zero_(), cache.v.zero_()
+    want_k, want_v = torch.zeros_like(cache.k), torch.zeros_like(cache.v)
+    pkg.kv_append(cache, rows[:, :kv], rows[:, kv:], slots, positions=pos, table=table, interleaved=inter, axes=axes)
+    turned = pkg.rope(rows[:, :kv].contiguous(), pos, table, interleaved=inter, axes=axes)
+    live = slots >= 0
+    at = slots[live].long()
+    want_k[at // 8, :, at % 8], want_v[at // 8, :, at % 8] = turned[live], rows[:, kv:][live]
+    torch.testing.assert_close(cache.k, want_k, rtol=0, atol=0, equal_nan=True)
+    assert torch.equal(cache.v, want_v) and torch.isnan(cache.k).any()
+
+
 def test_streams_graphs_and_the_block():
     """On a stream of its own, and captured and replayed with positions that move on in place."""
     table, axes = pkg.rope_table(64, 200), pkg.rope_axes([8, 12, 12])
