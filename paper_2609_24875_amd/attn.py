@@ -540,11 +540,14 @@ def _sums(t, name: str, device, batch: int, heads, width: int):
         raise TypeError(f"{name} must be a torch.float32 tensor")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, expected {device}")
-    if t.dim() != 3 or t.shape[0] != batch or t.shape[1] not in heads or t.shape[2] < width or (t.shape[2] > 1 and t.stride(2) != 1):
-        raise ValueError(f"{name} must be [{batch}][{' or '.join(str(h) for h in heads)}][{width} or more] with unit stride along the tokens, "
-                         f"got shape {tuple(t.shape)} and strides {tuple(t.stride())}")
-    # (the stride of a dimension of one element is never used and may hold anything)
-    return t.data_ptr(), t.stride(0) if batch > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
+    sh = t.shape
+    if len(sh) == 3 and sh[0] == batch and sh[1] in heads and sh[2] >= width:
+        s0, s1, s2 = t.stride()
+        if s2 == 1 or sh[2] <= 1:
+            # (the stride of a dimension of one element is never used and may hold anything)
+            return t.data_ptr(), s0 if batch > 1 else 0, s1 if sh[1] > 1 else 0
+    raise ValueError(f"{name} must be [{batch}][{' or '.join(str(h) for h in heads)}][{width} or more] with unit stride along the tokens, "
+                     f"got shape {tuple(t.shape)} and strides {tuple(t.stride())}")
 
 
 def _page_table(pages, name: str, device, batch: int):
@@ -552,10 +555,12 @@ def _page_table(pages, name: str, device, batch: int):
     import torch
     if not isinstance(pages, torch.Tensor) or pages.dtype is not torch.int32:
         raise TypeError(f"{name} must be a torch.int32 tensor")
-    rows, cols = pages.shape if pages.dim() == 2 else (-1, 0)
-    if rows != batch or pages.device != device or (cols > 1 and rows > 0 and pages.stride(1) != 1):
+    sh = pages.shape
+    rows, cols = sh if len(sh) == 2 else (-1, 0)
+    row, one = pages.stride() if rows >= 0 else (0, 0)
+    if rows != batch or pages.device != device or (cols > 1 and rows > 0 and one != 1):
         raise ValueError(f"{name} must be [{batch}][columns] on {device} with unit stride along the columns")
-    row = pages.stride(0) if batch > 1 else cols
+    row = row if batch > 1 else cols
     if row < cols:
         raise ValueError(f"rows of {name} must not overlap")
     return pages.data_ptr(), row, cols
@@ -670,7 +675,9 @@ def attention_weights(q, cache: KVCache, pages, seq_lens, lse, before=None, per_
     pb, bs, bh = (None, 0, 0) if before is None else _sums(before, "before", dev, batch, (heads,), max_len)
     if out is None:
         out = torch.empty((batch, heads, max_len), dtype=torch.float32, device=dev)
-    po, os, oh = _sums(out, "out", dev, batch, (heads,), max_len)
+        po, os, oh = out.data_ptr(), heads * max_len, max_len
+    else:
+        po, os, oh = _sums(out, "out", dev, batch, (heads,), max_len)
     _on_gpu(q)
     handle = _stream_handle()
 
@@ -721,10 +728,14 @@ def kv_evict(cache: KVCache, pages, seq_lens, sums, keep: int, recent: int = 0, 
     heads = sums.shape[1]
     if sums_out is None:
         sums_out = torch.empty((batch, heads, max_len), dtype=torch.float32, device=dev)
-    pn, ns, nh = _sums(sums_out, "sums_out", dev, batch, (heads,), most)
+        pn, ns, nh = sums_out.data_ptr(), heads * max_len, max_len
+    else:
+        pn, ns, nh = _sums(sums_out, "sums_out", dev, batch, (heads,), most)
     if lens_out is None:
         lens_out = torch.empty_like(seq_lens)
-    pl = _ints(lens_out, "lens_out", dev, batch)
+        pl = lens_out.data_ptr()
+    else:
+        pl = _ints(lens_out, "lens_out", dev, batch)
     _on_gpu(seq_lens)
     kept = torch.empty((batch, heads, keep), dtype=torch.int32, device=dev)
     st = _library().sph_kv_evict(cache._ref, batch, pp, row, lens, max_len, ps, heads, ss, sh, keep, recent, first, pt, to_row, pl, pn,

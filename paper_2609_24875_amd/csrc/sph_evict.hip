@@ -381,7 +381,7 @@ sph_status sph_kv_evict(const sph_kv_cache* cache, int64_t batch, const int32_t*
                         (const void*)d_new_sums, (const void*)d_kept})
     if ((uintptr_t)p % 4) return SPH_ERR_SHAPE;
   // sums rewritten in place have to be so row by row
-  if (d_new_sums == d_sums && ((batch > 1 && new_seq_stride != sums_seq_stride) || (heads > 1 && new_head_stride != sums_head_stride)))
+  if (d_sums && d_new_sums == d_sums && ((batch > 1 && new_seq_stride != sums_seq_stride) || (heads > 1 && new_head_stride != sums_head_stride)))
     return SPH_ERR_SHAPE;
   const bool within = d_to_pages == d_pages;
   if (within && batch > 1 && to_stride != pages_stride) return SPH_ERR_SHAPE;

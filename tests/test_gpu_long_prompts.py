@@ -1,0 +1,137 @@
+"""A run of the operators for long prompts, as a program uses them: a video's tokens written once with positions along three axes, text of several
+sequences behind them, attention, the weights that the text's tokens got, eviction within their pages, and decode steps in a replayed graph
+that add to the same sums. Every result against 64 bits from what the cache holds.
+
+Tolerances are those of the operators by themselves (test_gpu_shared.py, test_gpu_weights.py)."""
+from __future__ import annotations
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+import paper_2609_24875_amd as pkg  # noqa: E402
+from test_gpu_shared import DEV, Case, _gen, _i32  # noqa: E402
+
+KV, GROUP, DIM, PAGE, COLS = 2, 4, 64, 16, 6
+PREFIX, LENS, KEEP, RECENT, FIRST = 150, [40, 17, 64], 24, 8, 2
+
+
+def _state(cache, ppages, pages, lens, new, q):
+    c = Case.__new__(Case)
+    c.plens, c.lens, c.new, c.of = [PREFIX], lens, new, [0] * len(lens)
+    c.kv, c.group, c.dim, c.page, c.cache, c.ppages, c.pages, c.q, c.scale = KV, GROUP, DIM, PAGE, cache, ppages, pages, q, DIM ** -0.5
+    return c
+
+
+def _check_attention(c, o, lse):
+    ro, rl, ob, lb = c.exact()
+    assert ((o.double() - ro).abs() <= ob).all() and ((lse.double() - rl).abs() <= lb).all()
+
+
+def _check_sums(c, lse, before, got):
+    t = 0
+    for b, (n, m) in enumerate(zip(c.lens, c.new)):
+        k = c.tokens(c.pages[b], n)[0]
+        seen = (torch.arange(n, device=DEV)[None] <= n - m + torch.arange(m, device=DEV)[:, None]).repeat_interleave(GROUP, dim=0)
+        for h in range(KV):
+            q = c.q[t:t + m, h * GROUP:h * GROUP + GROUP].double().reshape(m * GROUP, DIM)
+            kt = k[:, h].t().contiguous()
+            x, big = q @ kt * c.scale, q.abs() @ kt.abs() * c.scale
+            ls = lse[t:t + m, h * GROUP:h * GROUP + GROUP].double().reshape(m * GROUP, 1)
+            w = torch.where(seen, (x - ls).exp(), 0.0)
+            rel = DIM * 2.0 ** -23 * big + 2.0 ** -23 * (x.abs() + ls.abs()) + 2.0 ** -21
+            old = before[b, h, :n].double()
+            off = (w * rel).sum(dim=0) + 2.0 ** -24 * (m * GROUP + 2) * w.sum(dim=0) + 2.0 ** -23 * (old + w.sum(dim=0))
+            assert ((got[b, h, :n].double() - old - w.sum(dim=0)).abs() <= off).all()
+        assert not got[b, :, n:].any()
+        t += m
+
+
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("bits", [16, 8, 4])
+def test_a_run_of_all(bits, inter):
+    batch, rows = len(LENS), KV * (GROUP + 2)
+    table, axes = pkg.rope_table(DIM, 400), pkg.rope_axes((8, 12, 12), cycled=inter)
+    ppages_n = -(-PREFIX // PAGE)
+    order = torch.randperm(ppages_n + batch * COLS, generator=_gen(1), device=DEV).int()
+    ppages, pages = order[:ppages_n].view(1, -1), order[ppages_n:].view(batch, COLS)
+    cache = pkg.KVCache.empty(len(order), KV, DIM, page_size=PAGE, bits=bits)
+
+    def slots_of(row, at):
+        return (row[at // PAGE] * PAGE + at % PAGE).int()
+
+    def split(x):
+        return x[:, :KV * GROUP], x[:, KV * GROUP:KV * GROUP + KV], x[:, KV * GROUP + KV:]
+
+    # the video: 6 frames of 5 x 5
+    i = torch.arange(PREFIX, device=DEV)
+    _, k, v = split(torch.randn((PREFIX, rows, DIM), generator=_gen(2), device=DEV).half())
+    pkg.kv_append(cache, k, v, slots_of(ppages[0], i), positions=torch.stack([i // 25, i // 5 % 5, i % 5]).int(), table=table, interleaved=inter, axes=axes)
+    # the text of every sequence behind it: one position along all axes
+    x = torch.randn((sum(LENS), rows, DIM), generator=_gen(3), device=DEV).half()
+    at = torch.cat([torch.arange(n, device=DEV) for n in LENS])
+    slots = torch.cat([slots_of(pages[b], torch.arange(n, device=DEV)) for b, n in enumerate(LENS)])
+    q, k, v = split(x)
+    q = pkg.kv_append(cache, k, v, slots, positions=(6 + at).int().expand(3, -1).contiguous(), table=table, interleaved=inter, q=q, axes=axes)
+    lens, start, plens = _i32(LENS), _i32([sum(LENS[:b]) for b in range(batch + 1)]), _i32([PREFIX])
+    most = COLS * PAGE
+    o, lse = pkg.attention_shared(q, cache, ppages, plens, pages, lens, q_start=start, max_q=max(LENS), max_len=most, return_lse=True)
+    c = _state(cache, ppages, pages, LENS, LENS, q)
+    _check_attention(c, o, lse)
+    sums = pkg.attention_weights(q, cache, pages, lens, lse, q_start=start, max_q=max(LENS), max_len=most)
+    _check_sums(c, lse, torch.zeros_like(sums), sums)
+
+    # the least looked at leave; each kv head its own
+    held = [pkg.kv_read(cache, slots_of(pages[b], torch.arange(n, device=DEV))) for b, n in enumerate(LENS)]
+    old = sums.clone()
+    lens, sums, kept = pkg.kv_evict(cache, pages, lens, sums, KEEP, RECENT, FIRST, max_len=most, sums_out=sums)
+    left = [min(n, KEEP) for n in LENS]
+    assert lens.tolist() == left
+    for b, n in enumerate(LENS):
+        now = pkg.kv_read(cache, slots_of(pages[b], torch.arange(left[b], device=DEV)))
+        for h in range(KV):
+            want = torch.arange(n, device=DEV)
+            if n > KEEP:
+                mid = old[b, h, FIRST:n - RECENT].sort(descending=True, stable=True).indices[:KEEP - FIRST - RECENT] + FIRST
+                want = torch.cat([want[:FIRST], mid.sort().values, want[n - RECENT:]])
+            assert torch.equal(kept[b, h, :left[b]].long(), want) and torch.equal(sums[b, h, :left[b]], old[b, h, want])
+            assert all(torch.equal(t[:, h], w[want, h]) for t, w in zip(now, held[b]))
+
+    # decode steps in a graph: positions go on where the prompts ended, slots where the kept tokens do
+    x = torch.randn((batch, rows, DIM), generator=_gen(4), device=DEV).half()
+    q, k, v = split(x)
+    pos = (6 + _i32(LENS)).expand(3, -1).contiguous()
+    slots = torch.stack([slots_of(pages[b], lens[b].long()) for b in range(batch)])
+    lens += 1
+    qt = torch.empty((batch, KV * GROUP, DIM), dtype=torch.float16, device=DEV)
+    out = {}
+
+    def step():
+        pkg.kv_append(cache, k, v, slots, positions=pos, table=table, interleaved=inter, q=q, q_out=qt, axes=axes)
+        out["o"], out["lse"] = pkg.attention_shared(qt, cache, ppages, plens, pages, lens, max_len=most, return_lse=True)
+        pkg.attention_weights(qt, cache, pages, lens, out["lse"], before=sums, max_len=most, out=sums)
+
+    kept_sums, side = sums.clone(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    sums.copy_(kept_sums)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for n in range(4):
+        before = sums.clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        c = _state(cache, ppages, pages, [m + n + 1 for m in left], [1] * batch, qt)
+        _check_attention(c, out["o"], out["lse"])
+        _check_sums(c, out["lse"], before, sums)
+        x.copy_(torch.randn(x.shape, generator=_gen(10 + n), device=DEV))
+        pos += 1
+        slots.copy_(torch.stack([slots_of(pages[b], lens[b].long()) for b in range(batch)]))
+        lens += 1
