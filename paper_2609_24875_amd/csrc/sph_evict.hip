@@ -290,7 +290,8 @@ __global__ __launch_bounds__(kMoveThreads) void k_evict_move(EvictArgs a) {
 }
 
 // Within the sequence's own pages: a workgroup takes up to 64 bytes of every key or value row of a sequence and head, or all offsets and steps, through
-// all tokens in ascending order: nobody else reads or writes these bytes, and a step's tokens are read before any of its places is written.
+// all tokens in ascending order: nobody else reads or writes these bytes, and a step's tokens are read before any of its places is written. 32 sequences to
+// 4096 tokens each, 8 heads of 128 fp16 channels 286 us (3.7 TB/s read and written), one sequence 24: the latency of its steps, of 1024 tokens each.
 constexpr int kWithinThreads = 1024, kWithinEach = 4;
 
 template <typename T>
