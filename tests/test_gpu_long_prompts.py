@@ -135,3 +135,70 @@ def test_a_run_of_all(bits, inter):
         pos += 1
         slots.copy_(torch.stack([slots_of(pages[b], lens[b].long()) for b in range(batch)]))
         lens += 1
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_pools_of_more_than_32_bits(bits):
+    """Pages whose bytes lie behind 2^32: the same bits as in a small pool, for single tokens and for many."""
+    pages = 45000 if bits == 16 else 170000
+    big, small = (pkg.KVCache.empty(n, 8, 128, bits=bits) for n in (pages, 24))
+    assert big.k.numel() * big.k.element_size() > 2 ** 32 + 2 ** 30
+    at_small = torch.randperm(24, generator=_gen(1), device=DEV).int()
+    at_big = (pages - 1 - 977 * torch.arange(24, device=DEV)).int()[torch.randperm(24, generator=_gen(2), device=DEV)]
+    i = torch.arange(24 * 64, device=DEV)
+    k, v = (torch.randn((24 * 64, 8, 128), generator=_gen(s), device=DEV).half() for s in (3, 4))
+    got = []
+    for cache, at in ((big, at_big), (small, at_small)):
+        pkg.kv_append(cache, k, v, (at.long()[i // 64] * 64 + i % 64).int())
+        ppages, own, to = at[:10].view(1, 10), at[10:18].view(2, 4), at[18:24].view(2, 3)
+        out = []
+        for new in (1, 40):
+            lens, start = _i32([201, 177]), _i32([0, new, 2 * new])
+            q = torch.randn((2 * new, 32, 128), generator=_gen(5), device=DEV).half()
+            o, lse = pkg.attention_shared(q, cache, ppages, _i32([611]), own, lens, q_start=start, max_q=new, return_lse=True)
+            sums = pkg.attention_weights(q, cache, own, lens, lse, q_start=start, max_q=new)
+            out += [o, lse, sums]
+        out += pkg.kv_evict(cache, own, lens, sums, 150, 20, 3, to_pages=to)
+        out += pkg.kv_evict(cache, own, lens, sums, 100, 20, 3)
+        for t in (own[:, :2], to):
+            j = torch.arange(t.shape[1] * 64, device=DEV)[:100]
+            for row in t:
+                out += pkg.kv_read(cache, (row.long()[j // 64] * 64 + j % 64).int())
+        got.append(out)
+    for x, y in zip(*got):
+        assert torch.equal(x, y)
+
+
+def test_two_graphs_at_once():
+    """Graphs of the same cache, replayed on two streams beside each other and beside eager calls: each has its own parts."""
+    cache = pkg.KVCache.empty(200, 4, 128)
+    i = torch.arange(200 * 64, device=DEV)
+    pkg.kv_append(cache, *(torch.randn((200 * 64, 4, 128), generator=_gen(s), device=DEV).half() for s in (1, 2)), i.int())
+    at = torch.randperm(200, generator=_gen(3), device=DEV).int()
+    ppages, plens, own = at[:100].view(1, 100), _i32([6000]), at[100:196].view(12, 8)
+    lens = _i32([37 * (b + 1) for b in range(12)])
+    qs = [torch.randn((12, 16, 128), generator=_gen(4 + s), device=DEV).half() for s in range(3)]
+
+    def call(q):
+        o, lse = pkg.attention_shared(q, cache, ppages, plens, own, lens, return_lse=True)
+        return o, lse, pkg.attention_weights(q, cache, own, lens, lse, per_head=False)
+
+    want = [call(q) for q in qs]
+    streams, graphs, outs = [torch.cuda.Stream() for _ in range(2)], [], []
+    torch.cuda.synchronize()
+    for s, q in zip(streams, qs):
+        with torch.cuda.stream(s):
+            call(q)                                           # (a stream that captures has had a call)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            outs.append(call(q))
+        graphs.append(graph)
+    for _ in range(20):
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        eager = call(qs[2])
+        torch.cuda.synchronize()
+        for got, ref in zip([*outs, eager], want):
+            assert all(torch.equal(x, y) for x, y in zip(got, ref))
