@@ -11,6 +11,8 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
+constexpr int kAlone = -1;
+
 struct AttnArgs {
   // (what sph_attention_shared's kernels do otherwise)
   static constexpr bool kParts = false;   // rows are always written as parts
@@ -34,7 +36,7 @@ struct AttnArgs {
   // (fold: tiles of rows between k_attn_wide's workgroups that share a CU, 0 for the longest first)
   bool stream;             // k_attn reads values past the caches
   float scale;             // times log2 e
-  int each;                // of kParts: workgroups a sequence and kv head, 0: one, or shares that are counted
+  int each;                // of kParts: workgroups a sequence and kv head, 0: one, or shares that are counted; kAlone: a wave
 };
 
 // The kernel for more rows a kv head than k_attn takes, and its rows a workgroup and keys a tile.

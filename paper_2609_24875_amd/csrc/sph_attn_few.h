@@ -133,10 +133,12 @@ __device__ __forceinline__ int wave_scan(int v) {
 // 32 query heads over 8 kv heads of 128 channels: one sequence of 131072 tokens in fp16 87 us (6.2 TB/s), 64 of up to 8192 at 8 bits
 // 78 us (5.2 TB/s), 16 of 32768 under 40 query heads at 4 bits 124 us (5.4 TB/s: the vector ALU, which decodes, is 54% busy beside the reads); one
 // of 517 tokens 11.3 us (512 tokens 9.4, one 5.8).
-template <int DIM, int BITS, int NB, bool UNI, typename A>
+//
+// ALONE: a wave by itself, beside others that have other sequences. It writes its part, without waiting for anyone.
+template <int DIM, int BITS, int NB, bool UNI, bool ALONE, typename A>
 __device__ __forceinline__ void attend(const A& a, char* lds, float2 (*ml_s)[16 * NB], int kvh, int b, int c_lo, int c_hi, int slot) {
   typedef Lay<DIM, BITS> L;
-  constexpr int kRows = 16 * NB, kVBytes = kTile * L::kVStride, kOStride = DIM + 4;
+  constexpr int kRows = 16 * NB, kVBytes = kTile * L::kVStride, kOStride = DIM + 4, kStep = kTile * (ALONE ? 1 : kWaves);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, g4 = lane >> 4;
   Seq s;
@@ -163,7 +165,7 @@ __device__ __forceinline__ void attend(const A& a, char* lds, float2 (*ml_s)[16 
   float l[NB];
 #pragma unroll
   for (int n = 0; n < NB; ++n) ref[n] = {-INFINITY, 0.0f}, l[n] = 0.0f;
-  const int t0 = (k_lo & ~(kTile - 1)) + kTile * wave;
+  const int t0 = (k_lo & ~(kTile - 1)) + (ALONE ? 0 : kTile * wave);
   if (t0 < k_hi) {
     f16x8 q[NB][L::kSteps];
 #pragma unroll
@@ -183,7 +185,7 @@ __device__ __forceinline__ void attend(const A& a, char* lds, float2 (*ml_s)[16 
     char* vs = lds + wave * kVBytes;
 
     Tile<DIM, BITS> T;
-    int kt = t0, nt = t0 + kTile * kWaves < k_hi ? t0 + kTile * kWaves : t0;
+    int kt = t0, nt = t0 + kStep < k_hi ? t0 + kStep : t0;
     int page = page_of(kt), next = page_of(nt);
     uint64_t gone = __ballot(!pg.there(page));
     page = pg.there(page) ? page : 0;
@@ -198,7 +200,7 @@ __device__ __forceinline__ void attend(const A& a, char* lds, float2 (*ml_s)[16 
     };
     load_v();
     while (true) {
-      const bool last = kt + kTile * kWaves >= k_hi;
+      const bool last = kt + kStep >= k_hi;
       // every row sees the whole tile
       const bool whole = span.whole(kt) && !gone;
       const uint64_t next_gone = __ballot(!pg.there(next));
@@ -246,7 +248,7 @@ __device__ __forceinline__ void attend(const A& a, char* lds, float2 (*ml_s)[16 
       __builtin_amdgcn_sched_barrier(0);
       load_v();
       __builtin_amdgcn_sched_barrier(0);
-      const int nnt = nt + kTile * kWaves < k_hi ? nt + kTile * kWaves : nt;
+      const int nnt = nt + kStep < k_hi ? nt + kStep : nt;
       next = page_of(nnt);
       f16x8 p[NB];
       bool rise = false;
@@ -333,6 +335,23 @@ __device__ __forceinline__ void attend(const A& a, char* lds, float2 (*ml_s)[16 
       l[n] += __shfl_xor(l[n], 16);
       l[n] += __shfl_xor(l[n], 32);
     }
+  }
+
+  if constexpr (ALONE) {
+    const bool some_odd = __any(odd);
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      const int row = 16 * n + col;
+      if (row >= nrow) continue;
+      const int64_t part = part_at(a, slot, kvh, row);
+#pragma unroll
+      for (int i = 0; i < DIM / 16; ++i) {
+        f32x4 acc = o[n][i];
+        if (some_odd) acc += odd_values<DIM, BITS>(span, pg, pages, A::kFlat ? first : first + row / a.group, 16 * i + 4 * g4);
+        write_part(a, part, 16 * i + 4 * g4, acc, ref[n].log(), l[n]);
+      }
+    }
+    return;
   }
 
   // the waves' parts meet

@@ -61,7 +61,7 @@ __global__ __launch_bounds__(kThreads) void k_attn_shared_join(SharedArgs both) 
   const int64_t token = (int64_t)s.start + row / a.group;
   const int g = prefix_of(p, b);
   int2 w = make_int2(b, both.own_many ? a.splits : 1);
-  if (!both.own_many && (a.shares || a.each)) w = a.where[b];
+  if (!both.own_many && (a.shares || a.each > 0)) w = a.where[b];
   const int64_t first = part_at(a, w.x, kvh, row), step = part_at(a, w.x + (both.own_many ? a.batch : 1), kvh, row) - first;
   int64_t pre_first = 0, pre_step = 0;
   int parts = w.y, pre_parts = 0;
@@ -76,15 +76,15 @@ __global__ __launch_bounds__(kThreads) void k_attn_shared_join(SharedArgs both) 
       pre_step = (int64_t)a.c.kv_heads * (a.tokens * a.group);
       pre_first = both.pre_part + (int64_t)kvh * (a.tokens * a.group) + at * a.group + row % a.group, pre_parts = p.splits;
     } else {
-      w = p.shares || p.each ? p.where[g] : make_int2(g, 1);
+      w = p.shares || p.each > 0 ? p.where[g] : make_int2(g, 1);
       const int r = (int)min(max(token - q.start, (int64_t)0), (int64_t)p.max_q - 1) * a.group + row % a.group;
       pre_first = part_at(p, w.x, kvh, r), pre_step = part_at(p, w.x + 1, kvh, r) - pre_first, pre_parts = w.y;
       pre_first += both.pre_part;
     }
   }
   // (slots that no sequence wrote are anything)
-  if (!both.own_many && (a.shares || a.each) && (s.n == 0 || bad)) parts = 0;
-  if (!both.pre_many && (p.shares || p.each) && bad) pre_parts = 0;
+  if (!both.own_many && (a.shares || a.each > 0) && (s.n == 0 || bad)) parts = 0;
+  if (!both.pre_many && (p.shares || p.each > 0) && bad) pre_parts = 0;
   const int all = parts + pre_parts;
   auto at_of = [&](int i) { return i < parts ? first + i * step : pre_first + (i - parts) * pre_step; };
   constexpr int kLoads = 5;                                  // of a lane before it knows the maximum
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(kThreads) void k_attn_shared_join(SharedArgs both) 
 struct SharedPlan {
   Plan own, pre;
   int64_t pre_q;                           // tokens behind a prefix at most
-  int own_each, pre_each;                  // workgroups a sequence (see AttnArgs)
+  int own_each, pre_each;                  // as AttnArgs has it
   size_t own_parts, pre_parts, bytes;
   int64_t joins;
   bool few;
@@ -164,8 +164,15 @@ struct SharedPlan {
 // Rows that are joined anyway can do with more workgroups than k_attn's plan gives short sequences: up to one a CU, by the host's bounds and without
 // counting shares, and so for one sequence of any length. Three sequences behind 512 tokens 8.8 us with four workgroups a kv head for the prefix, 11.7
 // with one; behind 768 8.5 and 14.3; four behind 1031 9.6, with shares that are counted 11.9.
+// Many short ones go the other way: a wave for each and kv head, four to a workgroup, where there are waves enough for as many steps more (32 tokens
+// a step). 8 kv heads of 128 channels behind 4096: 128 sequences of 128 tokens 39.4 -> 33.8 us, of 512 71 -> 66, of 2048 106 -> 108; 64 of 128 28.0 -> 25.9, of 512
+// 49.5 -> 55; 32 of 128 23.0 -> 21.8, of 256 24.3 -> 24.5; 80 of 36 under 16 heads of 256, where a CU has one workgroup, behind 166 67 -> 37.
 int each_of(const sph_kv_cache* c, Plan& p, int64_t n, int64_t max_len) {
   if (p.wide || !n || (p.shares && n > 1)) return 0;
+  if (!p.shares && max_len <= kTile * std::min<int64_t>(32, n * c->kv_heads / 64)) {
+    p.grid = c->kv_heads * ((n + kWaves - 1) / kWaves);
+    return kAlone;
+  }
   const int64_t steps = (max_len + kTile * kWaves - 1) / (kTile * kWaves);
   const int64_t most = n == 1 ? std::max<int64_t>(1, kCus * workgroups_per_cu(c) / c->kv_heads) : kCus / (c->kv_heads * n);
   const int64_t each = std::min({steps, most, (int64_t)kMaxSplits});
@@ -193,12 +200,12 @@ SharedPlan shared_plan(const sph_kv_cache* c, int64_t prefixes, int64_t max_grou
     p.pre.grid = units * p.pre.splits;
   }
   p.kind = p.own.wide ? kManyMany : p.pre.wide ? kManyFew : kFewFew;
-  const auto slots = [](const Plan& q, int each, int64_t n) { return q.wide ? q.splits * n : each ? each * n : q.shares ? q.shares + n : n; };
+  const auto slots = [](const Plan& q, int each, int64_t n) { return q.wide ? q.splits * n : each > 0 ? each * n : q.shares ? q.shares + n : n; };
   p.own_parts = (size_t)slots(p.own, p.own_each, batch) * c->kv_heads * rows;
   p.pre_parts = p.pre.wide ? (size_t)p.pre.splits * tokens * q_heads : (size_t)slots(p.pre, p.pre_each, prefixes) * c->kv_heads * p.pre_q * group;
   p.bytes = (p.own_parts + p.pre_parts) * (c->head_dim + 2) * sizeof(float) + (size_t)(batch + prefixes) * sizeof(int2);
   const int64_t each = (p.own.wide ? p.own.splits : std::max(1, p.own_each)) +
-                       (p.pre.wide ? p.pre.splits : p.pre_each ? p.pre_each : 1 + p.pre.shares / prefixes);
+                       (p.pre.wide ? p.pre.splits : p.pre_each > 0 ? p.pre_each : 1 + p.pre.shares / prefixes);
   // a wave a row where they are many and of few parts, otherwise one for 32 channels of it: 4096 rows of 9 parts 13 us against 21, 2560 of 17 7 against 12;
   // 128 of 8 6 against 4.5, 1024 of 33 10 against 7
   p.few = each <= 20 && batch * max_q * q_heads >= 2048;

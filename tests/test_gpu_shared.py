@@ -249,6 +249,52 @@ def test_wrong_values_are_nan(size, new):
     torch.cuda.synchronize()
 
 
+def _many_short(dim=64, page=16, bits=16, new=1, kv=4, several=False):
+    """More sequences than there are workgroups' places: each by a wave, of no token to eight steps of them."""
+    n = 131
+    lens = [(37 * b) % 231 for b in range(n)]
+    lens[5], lens[6], lens[7], lens[n - 1] = 0, 32, 33, 1
+    rows = [1 + b % new for b in range(n)]
+    if several:
+        return Case([(13 * g) % 90 for g in range(65)], [2] * 65, lens, rows, kv=kv, dim=dim, page=page, bits=bits)
+    return Case([150], [n], lens, rows, kv=kv, dim=dim, page=page, bits=bits)
+
+
+@pytest.mark.parametrize("several", [False, True])
+@pytest.mark.parametrize("new", [1, 3, 8])
+@pytest.mark.parametrize("dim,page,bits", [(64, 16, 16), (64, 4, 8), (96, 8, 16), (96, 32, 4), (128, 16, 16), (128, 64, 8), (128, 8, 4), (192, 32, 8),
+                                           (256, 16, 16), (256, 8, 4)])
+def test_many_short_sequences(dim, page, bits, new, several):
+    _many_short(dim, page, bits, new, several=several).check()
+
+
+@pytest.mark.parametrize("several", [False, True])
+def test_many_short_sequences_with_wrong_and_odd_values(several):
+    c = _many_short(several=several)
+    want = c.run()
+    lens, pages = c.seq_lens.clone(), c.pages.clone()
+    lens[3], lens[40], pages[17, 1] = -1, 10 ** 9, 10 ** 9
+    c.cache.v[int(c.pages[70, 2]), 1, 3, 9] = NAN
+    c.cache.v[int(c.pages[71, 0]), 2, 3, 5] = -INF
+    # behind a length, and in pages that nobody's length reaches: anything
+    for b in (7, 12, 50):
+        n = c.lens[b]
+        c.cache.v[int(c.pages[b, n // 16]), :, n % 16] = NAN
+        c.cache.k[int(c.pages[b, n // 16]), :, n % 16] = NAN
+    pages[130, 1:] = -7
+    o, lse = c.run(seq_lens=lens, pages=pages)
+    bad = torch.zeros(131, dtype=torch.bool, device=DEV)
+    bad[[3, 40, 17]] = True
+    assert o[bad].isnan().all() and lse[bad].isnan().all()
+    odd = torch.zeros_like(o, dtype=torch.bool)
+    odd[70, 4:8, 9] = odd[71, 8:12, 5] = True
+    assert o[70, 4:8, 9].isnan().all() and (o[71, 8:12, 5] == -INF).all()
+    same = ~odd & ~bad[:, None, None]
+    assert torch.equal(o[same], want[0][same]) and torch.equal(lse[~bad], want[1][~bad])
+    again = c.run(seq_lens=lens, pages=pages)
+    assert torch.equal(o[same], again[0][same])
+
+
 def test_wrong_starts_of_tokens():
     c = Case([70], [4], [60] * 4, [40] * 4)
     for start in ([0, -1, 80, 120, 160], [0, 40, 39, 120, 160], [0, 40, 80, 120, 161], [0, 40, 80, 2 ** 31 - 1, -2 ** 31], [7, 7, 7, 7, 7],
