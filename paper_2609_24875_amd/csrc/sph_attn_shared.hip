@@ -192,9 +192,10 @@ SharedPlan shared_plan(const sph_kv_cache* c, int64_t prefixes, int64_t max_grou
   p.own_each = each_of(c, p.own, batch, max_len), p.pre_each = each_of(c, p.pre, prefixes, max_prefix);
   if (p.pre.wide) {
     // A workgroup a CU, beside which the own tokens' are, and two where prefixes are several, since ragged ones leave many with little to do. One
-    // prefix of 32768 tokens before 128 sequences of 1024 161 us, with two 195; 8 of up to 4099 before 8 each of up to 700 at 8 bits 48 and 46.
+    // prefix of 32768 tokens before 128 sequences of 1024 161 us, with two 195; 8 of up to 4099 before 8 each of up to 700 at 8 bits 48 and 46. Above 128 channels
+    // a CU holds one workgroup: one then, too (256 channels at 8 bits, 4 prefixes of up to 2000 before 32 each of up to 200: 76 us, with two 87).
     const int64_t units = c->kv_heads * prefixes * p.pre.tiles, tile = sph_attn_wide_tile(c->head_dim);
-    const int64_t want = std::max<int64_t>(1, (prefixes > 1 ? 2 : 1) * kCus / units);
+    const int64_t want = std::max<int64_t>(1, (prefixes > 1 && c->head_dim <= 128 ? 2 : 1) * kCus / units);
     p.pre.chunk = (int)std::max<int64_t>(4 * tile, ((max_prefix + want - 1) / want + tile - 1) / tile * tile);
     p.pre.splits = (int)std::max<int64_t>(1, (max_prefix + p.pre.chunk - 1) / p.pre.chunk);
     p.pre.grid = units * p.pre.splits;
