@@ -411,7 +411,8 @@ sph_status sph_kv_read(const sph_kv_cache* cache, int64_t tokens, const int32_t*
  * logarithm of sum_j exp(scale q.k_j) (-inf where nothing is seen), or NULL. scale must be finite. d_ws: at
  * least sph_attention_workspace_bytes, 256-byte aligned, no initial contents; concurrent calls must not share one.
  * Keys and values that no query sees are never used, whatever they hold. Queries of a sequence whose length is outside 0..max_len, whose start and count are
- * outside their range, or that see a page outside the pool get NaN. Every sum runs in an order fixed by the
+ * outside their range, or that see a page outside the pool get NaN. Where d_q_start descends, several sequences may claim a token, which then gets
+ * anything. Every sum runs in an order fixed by the
  * arguments, so repeated calls give bitwise identical results. Asynchronous. */
 sph_status sph_attention(const sph_kv_cache* cache, int64_t batch, int64_t tokens, int32_t q_heads, const void* d_q,
                          int64_t q_token_stride, int64_t q_head_stride, const int32_t* d_q_start, int64_t max_q,
@@ -433,7 +434,7 @@ sph_status sph_attention_workspace_bytes(const sph_kv_cache* cache, int64_t batc
  * NULL): the host's bound of sequences behind a prefix, for which the launch is planned as for max_prefix, max_len and max_q: better close to the truth. Prefixes and own tokens
  * are pages of the same cache, and a page may be in any number of rows.
  * A sequence whose own values are wrong (see sph_attention), or whose prefix has a length outside 0..max_prefix, more tokens behind it than
- * max_group * max_q, starts that do not ascend or a page outside the pool, gets NaN. Precision, empty rows and values that no row sees: as in sph_attention; repeated
+ * max_group * max_q or a page outside the pool, gets NaN, and so does every sequence of a call whose d_first descends anywhere. Precision, empty rows and values that no row sees: as in sph_attention; repeated
  * calls give bitwise identical results. d_ws: at least sph_attention_shared_workspace_bytes, 256-byte aligned, no
  * initial contents; concurrent calls must not share one. Asynchronous. */
 sph_status sph_attention_shared(const sph_kv_cache* cache, int64_t prefixes, const int32_t* d_first, int64_t max_group,

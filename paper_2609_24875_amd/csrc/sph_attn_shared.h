@@ -36,7 +36,8 @@ struct PrefixArgs : AttnArgs {
 struct SharedArgs {
   OwnArgs own;
   PrefixArgs pre;
-  uint32_t pre_blocks;
+  int* descends;           // of more prefixes than a wave looks at at once: 1 if their starts descend anywhere, else 0
+  uint32_t pre_blocks, blocks;   // workgroups of the prefixes; of them and the own tokens
   int64_t pre_part;        // rows of parts before the prefixes'
   bool pre_many, own_many;
 };
@@ -67,7 +68,7 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 128 ? 2 : 1)) void k_attn_sh
       typedef Wide<DIM, BITS> W;
 #include "sph_attn_many.inc"
     }
-  } else {
+  } else if (blockIdx.x < both.blocks) {
     typedef OwnArgs A;
     const A& a = both.own;
     const uint32_t block = blockIdx.x - both.pre_blocks;
@@ -78,6 +79,13 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 128 ? 2 : 1)) void k_attn_sh
       char* lds = lds_a;
 #include "sph_attn_few.inc"
     }
+  } else {
+    // one workgroup more, where there is a `descends` to write
+    const PrefixArgs& a = both.pre;
+    bool down = false;
+    for (int g = threadIdx.x; g < a.batch; g += kThreads) down |= a.first[g] > a.first[g + 1];
+    const bool any = __syncthreads_or(down);
+    if (threadIdx.x == 0) *both.descends = any;
   }
 }
 

@@ -23,11 +23,13 @@ const void* sph_attn_shared_kernel16(int dim, SharedKind kind, int nb, bool uni)
 
 namespace {
 
-// The prefix whose sequences are first[g] .. first[g + 1] - 1 with b among them, -1 for none. By a whole wave, 64 places at once.
-__device__ __forceinline__ int prefix_of(const PrefixArgs& a, int b) {
+// The prefix whose sequences are first[g] .. first[g + 1] - 1 with b among them, -1 for none. By a whole wave, 64 places at once. down: the starts descend
+// anywhere, so that two prefixes may claim a sequence (and have written its parts over each other's), or one that belongs to a prefix be found by none.
+__device__ __forceinline__ int prefix_of(const PrefixArgs& a, const int* descends, int b, bool& down) {
   if (!a.first) return 0;
-  const int lane = threadIdx.x & 63;
-  int lo = 0, n = a.batch + 1;                               // among the n entries from lo on, the last that is not above b
+  const int lane = threadIdx.x & 63, all = a.batch + 1;
+  const int mine = all > 64 ? *descends : a.first[min(lane, all - 1)];
+  int lo = 0, n = all;                                       // among the n entries from lo on, the last that is not above b
   while (n > 1) {
     const int step = (n + 63) / 64, at = lane * step;
     const uint64_t not_above = __ballot(at < n && a.first[lo + min(at, n - 1)] <= b);
@@ -37,6 +39,8 @@ __device__ __forceinline__ int prefix_of(const PrefixArgs& a, int b) {
     n = min(step, n - last * step);
   }
   lo = __builtin_amdgcn_readfirstlane(lo);
+  const int below = __shfl_up(mine, 1);                      // (lane 0: its own)
+  down = __any(all > 64 ? mine != 0 : below > mine);
   return lo < a.batch && a.first[lo] <= b && b < a.first[lo + 1] ? lo : -1;
 }
 
@@ -59,13 +63,14 @@ __global__ __launch_bounds__(kThreads) void k_attn_shared_join(SharedArgs both) 
   Seq s;
   s.load(a, b);
   const int64_t token = (int64_t)s.start + row / a.group;
-  const int g = prefix_of(p, b);
+  bool down = false;
+  const int g = prefix_of(p, both.descends, b, down);
   int2 w = make_int2(b, both.own_many ? a.splits : 1);
   if (!both.own_many && (a.shares || a.each > 0)) w = a.where[b];
   const int64_t first = part_at(a, w.x, kvh, row), step = part_at(a, w.x + (both.own_many ? a.batch : 1), kvh, row) - first;
   int64_t pre_first = 0, pre_step = 0;
   int parts = w.y, pre_parts = 0;
-  bool bad = s.bad;
+  bool bad = s.bad | down;
   if (g >= 0) {
     Seq q;
     q.load(p, g);
@@ -156,6 +161,7 @@ struct SharedPlan {
   int64_t pre_q;                           // tokens behind a prefix at most
   int own_each, pre_each;                  // as AttnArgs has it
   size_t own_parts, pre_parts, bytes;
+  size_t flag;                             // of the bytes: SharedArgs::descends, behind everything else
   int64_t joins;
   bool few;
   SharedKind kind;
@@ -205,6 +211,8 @@ SharedPlan shared_plan(const sph_kv_cache* c, int64_t prefixes, int64_t max_grou
   p.own_parts = (size_t)slots(p.own, p.own_each, batch) * c->kv_heads * rows;
   p.pre_parts = p.pre.wide ? (size_t)p.pre.splits * tokens * q_heads : (size_t)slots(p.pre, p.pre_each, prefixes) * c->kv_heads * p.pre_q * group;
   p.bytes = (p.own_parts + p.pre_parts) * (c->head_dim + 2) * sizeof(float) + (size_t)(batch + prefixes) * sizeof(int2);
+  p.flag = prefixes > 63 ? sizeof(int2) : 0;
+  p.bytes += p.flag;
   const int64_t each = (p.own.wide ? p.own.splits : std::max(1, p.own_each)) +
                        (p.pre.wide ? p.pre.splits : p.pre_each > 0 ? p.pre_each : 1 + p.pre.shares / prefixes);
   // a wave a row where they are many and of few parts, otherwise one for 32 channels of it: 4096 rows of 9 parts 13 us against 21, 2560 of 17 7 against 12;
@@ -298,14 +306,15 @@ sph_status sph_attention_shared(const sph_kv_cache* cache, int64_t prefixes, con
   b.batch = (int)prefixes, b.max_q = (int)p.pre_q, b.max_len = (int)max_prefix;
   b.first = d_first, b.seqs = (int)batch;
   b.part = a.part + p.own_parts * dim, b.ml = a.ml + p.own_parts, b.where = a.where + batch;
-  both.pre_blocks = (uint32_t)p.pre.grid, both.pre_part = (int64_t)p.own_parts;
+  both.descends = (int*)(a.where + batch + prefixes);
+  both.pre_blocks = (uint32_t)p.pre.grid, both.blocks = (uint32_t)(p.pre.grid + p.own.grid), both.pre_part = (int64_t)p.own_parts;
   both.pre_many = p.pre.wide, both.own_many = p.own.wide;
   const bool uni = cache->page_size >= 16;
   const int nb = p.kind == kFewFew ? p.pre.nb : p.own.nb;
   const void* fn = bits == 16  ? sph_attn_shared_kernel16(dim, p.kind, nb, uni)
                    : bits == 8 ? sph_attn_shared_kernel8(dim, p.kind, nb, uni)
                                : sph_attn_shared_kernel4(dim, p.kind, nb, uni);
-  if (!launch_ok(fn, p.pre.grid + p.own.grid, (hipStream_t)stream, both)) return SPH_ERR_HIP;
+  if (!launch_ok(fn, p.pre.grid + p.own.grid + (d_first && p.flag ? 1 : 0), (hipStream_t)stream, both)) return SPH_ERR_HIP;
   if (!launch_ok(p.few ? (const void*)k_attn_shared_join<true> : (const void*)k_attn_shared_join<false>, (p.joins + kWaves - 1) / kWaves,
                  (hipStream_t)stream, both))
     return SPH_ERR_HIP;
