@@ -1,8 +1,7 @@
-"""Attention behind shared prefixes on the GPU, what else its arguments allow: starts of prefixes that descend. Cases, results in
+"""Attention behind shared prefixes on the GPU, what else its arguments allow: starts of prefixes that descend, long prefixes with few rows each, whose tiles are
+counted and shared out by their lengths. Cases, results in
 64 bits and bounds are test_gpu_shared's."""
 from __future__ import annotations
-
-import math
 
 import pytest
 
@@ -13,8 +12,6 @@ if not torch.cuda.is_available():
     pytest.skip("needs a GPU", allow_module_level=True)
 
 from test_gpu_shared import DEV, Case, _i32  # noqa: E402
-
-INF = math.inf
 
 
 def _all_nan(c, first, **kw):
@@ -81,3 +78,98 @@ def test_starts_that_change_under_a_graph(n):
         want = c.run()
         torch.cuda.synchronize()
         assert (o.isnan().all() and lse.isnan().all()) if wrong else (torch.equal(o, want[0]) and torch.equal(lse, want[1]))
+
+
+def _check_but(c, bad, **kw):
+    """As Case.check, but for sequences `bad`, which are NaN."""
+    o, lse = c.run(**kw)
+    ro, rl, ob, lb = c.exact()
+    wrong = torch.tensor([b in bad for b in range(len(c.lens))], device=DEV).repeat_interleave(_i32(c.new))
+    assert o[wrong].isnan().all() and lse[wrong].isnan().all()
+    # (rows that see nothing have a logarithm of -inf on both sides)
+    assert ((o.double() - ro).abs() <= ob)[~wrong].all() and (((lse.double() - rl).abs() <= lb) | (lse.double() == rl))[~wrong].all()
+    again = c.run(**kw)
+    assert torch.equal(o[~wrong], again[0][~wrong]) and torch.equal(lse[~wrong], again[1][~wrong])
+
+
+def _ragged(n, kv, new=None, **kw):
+    """Prefixes of 1000 to 5999 tokens, an empty one and one of one token among them, with two, one or no sequences each, and a sequence before and
+    behind them without one."""
+    plens = [1000 + 1237 * i % 5000 for i in range(n)]
+    plens[n // 2], plens[-1] = 0, 1
+    sizes = [(2, 1, 0, 2)[i % 4] for i in range(n)]
+    lens = [(53 * b) % 200 for b in range(sum(sizes) + 2)]
+    if new:
+        lens, new = [n + 3 for n in lens], [new[b % len(new)] for b in range(len(lens))]
+    return Case(plens, sizes, lens, new, kv=kv, before=1, **kw)
+
+
+# Several prefixes of at most 32 rows (16 above 128 channels), bounds above 1536 tokens of 64 channels, 768 of 128, 384 of 256: counted shares. With
+# five prefixes the shares are many, a stretch of one prefix each; 24 prefixes of eight heads (at 16 bits from 96 channels on, at 8 from 192 on), 40 of them at 8 bits and 300 of
+# one leave fewer than two a prefix, which hold the end of one prefix and the start of the next.
+@pytest.mark.parametrize("page", [8, 64])
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("dim", [64, 96, 128, 192, 256])
+def test_long_prefixes_are_shared_out(dim, bits, page):
+    _ragged(5, 2, dim=dim, bits=bits, page=page).check()
+    _ragged(24, 8, dim=dim, bits=bits, page=page).check()
+
+
+@pytest.mark.parametrize("n", [2, 3, 40, 300])
+@pytest.mark.parametrize("dim,bits", [(64, 16), (128, 8)])
+def test_any_number_of_long_prefixes(n, dim, bits):
+    _ragged(n, 1, dim=dim, bits=bits).check()
+
+
+@pytest.mark.parametrize("n,kv", [(5, 2), (40, 8)])
+def test_drafts_behind_long_prefixes(n, kv):
+    """Up to 24 rows behind a prefix, in two blocks, beside own tokens of one and of two."""
+    _ragged(n, kv, (3, 1, 2, 3), dim=128, bits=8).check()
+    _ragged(n, kv, (3, 1, 0, 2), dim=64, page=1).check()
+
+
+@pytest.mark.parametrize("n,kv,dim", [(5, 2, 128), (24, 8, 128), (24, 8, 256)])
+def test_long_prefixes_with_wrong_values(n, kv, dim):
+    """Wrong lengths and pages: the sequences behind them are NaN, the others right however the shares fall."""
+    c = _ragged(n, kv, dim=dim)
+    behind = [{b for b, g in enumerate(c.of) if g == i} for i in range(n)]
+    for at, wrong in ((0, -1), (3, 6000), (1, 2 ** 31 - 1)):
+        lens = c.prefix_lens.clone()
+        lens[at] = wrong
+        _check_but(c, behind[at], prefix_lens=lens)
+    for column in (0, -1):
+        pages = c.ppages.clone()
+        at = max(range(n), key=lambda g: c.plens[g] if behind[g] else -1)
+        pages[at, (c.plens[at] - 1) // c.page if column else 0] = 10 ** 9
+        _check_but(c, behind[at], prefix_pages=pages)
+    lens = c.seq_lens.clone()
+    lens[2] = -5
+    _check_but(c, {2}, seq_lens=lens)
+
+
+@pytest.mark.parametrize("n", [512, 513])
+def test_prefixes_up_to_what_is_shared_out_by_lengths(n):
+    """One long prefix among short ones, with a bound that has 512 of them counted and 513 not."""
+    plens = [(37 * i) % 90 for i in range(n)]
+    plens[7] = 4500
+    sizes = [i % 3 for i in range(n)]
+    sizes[7] = 2
+    Case(plens, sizes, [(11 * i) % 40 for i in range(sum(sizes) + 2)], dim=64, kv=1, before=1).check()
+
+
+def test_long_prefixes_under_a_graph():
+    """Captured once, replayed while the prefixes' lengths change: the shares are counted anew each time."""
+    c = _ragged(5, 2, dim=128, bits=8)
+    plens, side = c.prefix_lens.clone(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    c.run(prefix_lens=plens, stream=side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        o, lse = c.run(prefix_lens=plens)
+    for cut in (0, 700, 5999, 1, 3000):
+        plens.copy_((c.prefix_lens - cut).clamp_min(0))
+        torch.cuda.synchronize()
+        graph.replay()
+        want = c.run(prefix_lens=plens)
+        torch.cuda.synchronize()
+        assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
