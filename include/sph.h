@@ -444,7 +444,9 @@ sph_status sph_attention_shared(const sph_kv_cache* cache, int64_t prefixes, con
                                 int64_t pages_stride, const int32_t* d_seq_lens, int64_t max_len, float scale, void* d_o,
                                 int64_t o_token_stride, int64_t o_head_stride, float* d_lse, void* d_ws, size_t ws_bytes, void* stream);
 
-/* Device workspace of sph_attention_shared with these arguments on the current device: the parts of every row. */
+/* Device workspace of sph_attention_shared with these arguments on the current device: the parts of every row, up to 32 rows (16 above 128 channels) a
+ * sequence of as many as max_q of every sequence has, otherwise of `tokens`. SPH_ERR_SHAPE, from the call too, where batch * max_q * q_heads
+ * passes 2^26 - 1 (with more than 20 parts a row 32 / head_dim of that), or the workgroups of prefixes and own tokens 2^24 - 1. */
 sph_status sph_attention_shared_workspace_bytes(const sph_kv_cache* cache, int64_t prefixes, int64_t max_group, int64_t max_prefix,
                                                 int64_t batch, int64_t tokens, int32_t q_heads, int64_t max_q, int64_t max_len,
                                                 size_t* bytes);

@@ -26,8 +26,8 @@ struct AttnArgs {
   int64_t pages_stride;
   const int32_t* lens;
   float* lse;
-  // Parts of rows whose keys several workgroups share: [slot][kv head][row of the sequence] of dim fp32 sums, of (m, l) pairs, and
-  // for k_attn each sequence's (first slot, slots).
+  // Parts of rows whose keys several workgroups share: [slot][kv head][row of the sequence] (kParts of many rows: [split][kv head][token][row of its group])
+  // of dim fp32 sums, of (m, l) pairs, and for k_attn each sequence's (first slot, slots).
   float* part;
   float2* ml;
   int2* where;
@@ -120,6 +120,11 @@ __device__ __forceinline__ void write_out(const AttnArgs& a, int64_t token, int 
 
 __device__ __forceinline__ int64_t part_at(const AttnArgs& a, int slot, int kvh, int row) {
   return ((int64_t)slot * a.c.kv_heads + kvh) * ((int64_t)a.max_q * a.group) + row;
+}
+
+// The same in the order of all tokens, row `row` of those from `token` on: no more parts than there are rows, however they are shared among sequences.
+__device__ __forceinline__ int64_t token_part_at(const AttnArgs& a, int split, int kvh, int64_t token, int row) {
+  return (((int64_t)split * a.c.kv_heads + kvh) * a.tokens + token) * a.group + row;
 }
 
 __device__ __forceinline__ void write_part(const AttnArgs& a, int64_t at, int ch, f32x4 acc, float m, float l) {

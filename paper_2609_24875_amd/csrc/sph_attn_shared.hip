@@ -65,9 +65,12 @@ __global__ __launch_bounds__(kThreads) void k_attn_shared_join(SharedArgs both) 
   const int64_t token = (int64_t)s.start + row / a.group;
   bool down = false;
   const int g = prefix_of(p, both.descends, b, down);
+  // (a token outside the arrays is a wrong one's: any part)
+  const int64_t near = min(max(token, (int64_t)0), a.tokens - 1);
   int2 w = make_int2(b, both.own_many ? a.splits : 1);
   if (!both.own_many && (a.shares || a.each > 0)) w = a.where[b];
-  const int64_t first = part_at(a, w.x, kvh, row), step = part_at(a, w.x + (both.own_many ? a.batch : 1), kvh, row) - first;
+  const int64_t first = both.own_many ? token_part_at(a, 0, kvh, near, row % a.group) : part_at(a, w.x, kvh, row);
+  const int64_t step = both.own_many ? (int64_t)a.c.kv_heads * (a.tokens * a.group) : part_at(a, 1, kvh, row) - part_at(a, 0, kvh, row);
   int64_t pre_first = 0, pre_step = 0;
   int parts = w.y, pre_parts = 0;
   bool bad = s.bad | down;
@@ -77,9 +80,8 @@ __global__ __launch_bounds__(kThreads) void k_attn_shared_join(SharedArgs both) 
     // (a token that is not among the prefix's has starts that do not ascend)
     bad |= q.bad || token < q.start || token >= q.end;
     if (both.pre_many) {
-      const int64_t at = min(max(token, (int64_t)0), a.tokens - 1);
       pre_step = (int64_t)a.c.kv_heads * (a.tokens * a.group);
-      pre_first = both.pre_part + (int64_t)kvh * (a.tokens * a.group) + at * a.group + row % a.group, pre_parts = p.splits;
+      pre_first = both.pre_part + token_part_at(a, 0, kvh, near, row % a.group), pre_parts = p.splits;
     } else {
       w = p.shares || p.each > 0 ? p.where[g] : make_int2(g, 1);
       const int r = (int)min(max(token - q.start, (int64_t)0), (int64_t)p.max_q - 1) * a.group + row % a.group;
@@ -207,9 +209,11 @@ SharedPlan shared_plan(const sph_kv_cache* c, int64_t prefixes, int64_t max_grou
     p.pre.grid = units * p.pre.splits;
   }
   p.kind = p.own.wide ? kManyMany : p.pre.wide ? kManyFew : kFewFew;
-  const auto slots = [](const Plan& q, int each, int64_t n) { return q.wide ? q.splits * n : each > 0 ? each * n : q.shares ? q.shares + n : n; };
-  p.own_parts = (size_t)slots(p.own, p.own_each, batch) * c->kv_heads * rows;
-  p.pre_parts = p.pre.wide ? (size_t)p.pre.splits * tokens * q_heads : (size_t)slots(p.pre, p.pre_each, prefixes) * c->kv_heads * p.pre_q * group;
+  const auto parts = [&](const Plan& q, int each, int64_t n, int64_t most) {
+    if (q.wide) return (size_t)q.splits * tokens * q_heads;
+    return (size_t)(each > 0 ? each * n : q.shares ? q.shares + n : n) * c->kv_heads * (most * group);
+  };
+  p.own_parts = parts(p.own, p.own_each, batch, max_q), p.pre_parts = parts(p.pre, p.pre_each, prefixes, p.pre_q);
   p.bytes = (p.own_parts + p.pre_parts) * (c->head_dim + 2) * sizeof(float) + (size_t)(batch + prefixes) * sizeof(int2);
   p.flag = prefixes > 63 ? sizeof(int2) : 0;
   p.bytes += p.flag;

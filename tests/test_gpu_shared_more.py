@@ -1,5 +1,5 @@
 """Attention behind shared prefixes on the GPU, what else its arguments allow: starts of prefixes that descend, long prefixes with few rows each, whose tiles are
-counted and shared out by their lengths. Cases, results in
+counted and shared out by their lengths, prompts beside single tokens. Cases, results in
 64 bits and bounds are test_gpu_shared's."""
 from __future__ import annotations
 
@@ -173,3 +173,18 @@ def test_long_prefixes_under_a_graph():
         want = c.run(prefix_lens=plens)
         torch.cuda.synchronize()
         assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("dim", [64, 96, 128, 192, 256])
+def test_prompts_beside_single_tokens(dim, bits):
+    """Parts are in the order of the tokens: prompts, tokens and sequences without new ones in any order, of one split and of several."""
+    new = [1, 300, 0, 1, 77, 1, 1, 0]
+    Case([257], [8], [n + 40 * (b % 3) for b, n in enumerate(new)], new, dim=dim, bits=bits).check()
+    Case([90, 0, 700], [3, 1, 2], [n + 900 * (b % 2) for b, n in enumerate(new)], new, dim=dim, bits=bits, before=1).check()
+
+
+@pytest.mark.parametrize("group", [1, 3, 40])
+def test_groups_of_heads_of_prompts(group):
+    new = [200, 1, 3, 0, 60]
+    Case([400], [5], [2000 if n == 200 else n + 5 for n in new], new, kv=2, group=group, dim=128, bits=8).check()

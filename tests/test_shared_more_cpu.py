@@ -30,3 +30,15 @@ def test_room_for_what_becomes_of_many_starts(prefixes):
     row, batch = (128 + 2) * 4, 4
     rows = batch * 8 + prefixes * 2 * 16             # rows of all own parts; of the prefixes', two kv heads, four sequences of four heads
     assert _need(prefixes, 4, 64, batch, batch, 8, 1, 64) == rows * row + (batch + prefixes) * 8 + (8 if prefixes > 63 else 0)
+
+
+@needs_lib
+@pytest.mark.parametrize("batch,chunk", [(64, 4096), (128, 4096), (1, 300)])
+def test_prompts_beside_single_tokens_have_a_part_for_every_row(batch, chunk):
+    """One prompt and a token each of the other sequences: parts for the rows that there are, not for as many as the longest's of every sequence."""
+    row, tokens = (128 + 2) * 4, chunk + batch - 1
+    for max_prefix, max_len in ((1024, 8192), (1, 8192)):
+        need = _need(1, batch, max_prefix, batch, tokens, 32, chunk, max_len, kv=8)
+        parts, rest = divmod(need - (batch + 1) * 8, 32 * tokens * row)
+        # one for the own tokens and one for the prefix; a single sequence's few rows are cut for the chip's sake
+        assert rest == 0 and (parts == 2 or batch == 1 and 2 < parts < 64)
