@@ -69,6 +69,20 @@ def kernel_resources(stderr: str) -> dict:
     return res
 
 
+# The products', the rotation's, the cache's, the attention's and the eviction's kernels keep everything in registers: a record
+# buffer or an accumulator put in scratch memory (a spill, or an array the compiler could not promote)
+# halves their speed without any other sign, so the build refuses it. Allowed by name, and without scratch memory: the shared prefixes' kernels of 192 channels at
+# 8 bits, one wave a SIMD, count three copies to accumulation registers, which they have to spare, as spills.
+IN_REGISTERS = ("k_gemm", "k_rope", "k_kv_", "k_attn", "k_weights", "k_evict")
+SPILLS_ALLOWED = {"k_attn_sharedILi192ELi8E": 3}
+
+
+def spilled(resources: dict) -> dict:
+    """Those of the kernels that the build refuses."""
+    return {k: v for k, v in resources.items() if any(n in k for n in IN_REGISTERS) and
+            (v.get("scratch", 0) or v.get("vgpr_spill", 0) > max((most for n, most in SPILLS_ALLOWED.items() if n in k), default=0))}
+
+
 def _run(cmd) -> str:
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
@@ -85,15 +99,10 @@ def _compile(sources, out: str, verbose: bool) -> str:
         said = "".join(pool.map(_run, [[hipcc(), *each, RESOURCE_REMARKS, "-I", os.path.join(ROOT, "include"), "-c", "-o", o, s]
                                        for s, o in zip(sources, objects)]))
         _run([hipcc(), "--offload-arch=gfx950", "-fPIC", "-shared", "-o", tmp, *objects])
-    # The products', the rotation's, the cache's, the attention's and the eviction's kernels keep everything in registers: a record
-    # buffer or an accumulator put in scratch memory (a spill, or an array the compiler could not promote)
-    # halves their speed without any other sign, so the build refuses it. (A few copies to accumulation registers, which a kernel of one wave a SIMD has
-    # to spare, are counted as spills without scratch memory.)
-    bad = {k: v for k, v in kernel_resources(said).items()
-           if any(n in k for n in ("k_gemm", "k_rope", "k_kv_", "k_attn", "k_weights", "k_evict")) and (v.get("scratch", 0) or v.get("vgpr_spill", 0) > 4)}
+    bad = spilled(kernel_resources(said))
     if bad:
         os.remove(tmp)
-        raise RuntimeError(f"kernels using scratch memory: {bad}")
+        raise RuntimeError(f"kernels using scratch memory or spilling registers: {bad}")
     warnings = [ln for ln in said.splitlines() if "remark:" not in ln and ln.strip()]
     if verbose and warnings:
         print("\n".join(warnings))
