@@ -486,7 +486,7 @@ sph_status sph_attention_weights_workspace_bytes(const sph_kv_cache* cache, int6
  *
  * d_new_lens: device int32[batch], min(length, keep); may be d_seq_lens. d_new_sums: device fp32 rows of new_width (min(keep, max_len)..2^30), apart from each
  * other: the kept tokens' sums, then zeros; may be d_sums with the same strides, otherwise must not overlap it. d_kept: device int32[batch][heads][keep],
- * which tokens were kept, in order, then -1. A sequence whose length is outside 0..max_len stays as it is, with NaN for its
+ * which tokens were kept, in order, then -1 (keep above max_len evicts nothing, as max_len does with first and recent 0, whose rows are shorter). A sequence whose length is outside 0..max_len stays as it is, with NaN for its
  * new sums and -1 for kept. A token of a page outside the pool is NaN in its new place; nothing is written to such a page.
  * Results do not depend on the launch. SPH_ERR_SHAPE also where batch * heads passes 2^22 - 1, or a launch 2^32 threads. Asynchronous. */
 sph_status sph_kv_evict(const sph_kv_cache* cache, int64_t batch, const int32_t* d_pages, int64_t pages_stride, const int32_t* d_seq_lens,

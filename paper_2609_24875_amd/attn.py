@@ -701,7 +701,7 @@ def kv_evict(cache: KVCache, pages, seq_lens, sums, keep: int, recent: int = 0, 
     ``to_pages`` tokens move within their pages, which other sequences must not share from the first evicted token on; with int32 [batch][columns] ``to_pages``
     (pages of no sequence here) they are copied there, and pages may be shared. Returns (lens int32 [batch]: the new lengths, ``lens_out`` or a
     new tensor; sums: the kept tokens' and zeros behind them, ``sums_out``, which may be sums, or new fp32 [batch][heads][max_len]; kept int32
-    [batch][heads][keep]: which tokens were kept, then -1)."""
+    [batch][heads][min(keep, max_len), at least 1]: which tokens were kept, then -1)."""
     import torch
     if stream is not None:                      # what is made for the call belongs to its stream
         with torch.cuda.stream(stream):
@@ -737,6 +737,8 @@ def kv_evict(cache: KVCache, pages, seq_lens, sums, keep: int, recent: int = 0, 
     else:
         pl = _ints(lens_out, "lens_out", dev, batch)
     _on_gpu(seq_lens)
+    if keep > max_len:                          # nothing goes: a row of what was kept is no longer than a sequence can be
+        keep, recent, first = max(max_len, 1), 0, 0
     kept = torch.empty((batch, heads, keep), dtype=torch.int32, device=dev)
     st = _library().sph_kv_evict(cache._ref, batch, pp, row, lens, max_len, ps, heads, ss, sh, keep, recent, first, pt, to_row, pl, pn,
                                  sums_out.shape[2], ns, nh, kept.data_ptr(), _stream_handle())
