@@ -268,22 +268,29 @@ def rope(x, positions, table, interleaved: bool = False, inverse: bool = False, 
 
 
 def rope_gradient(grad, positions, table, interleaved: bool, inverse: bool = False, axes=None):
-    """The gradient of ``rope``'s rows from that of its result, whose tensors have passed ``rope``'s checks: they are not repeated, since
-    Python on autograd's thread costs several times what it does elsewhere."""
+    """The gradient of ``rope``'s rows from that of its result. positions, table and axes have passed ``rope``'s checks, but come back through
+    whatever autograd's hooks for saved tensors make of them: what the kernel reads by is checked again."""
+    import torch
     grad = aligned_rows(grad)
     n, heads, dim = grad.shape
     gt, gh, _ = grad.stride()
+    gpu, lead, (rows, pairs, two) = grad.get_device(), positions.stride(), table.shape
+    # (in few steps, since Python on autograd's thread costs several times what it does elsewhere: where they do not do, rope's checks say why)
+    if not (table.dtype is torch.float32 and positions.dtype is torch.int32 and table.get_device() == gpu == positions.get_device() and
+            table.is_contiguous() and lead[-1] == 1 and positions.shape[-1] == n and len(lead) == (1 if axes is None else 2) and
+            two == 2 and (axes is None or (axes.dtype is torch.uint8 and axes.get_device() == gpu and axes.numel() == pairs and axes.is_contiguous()))):
+        dev = grad.device
+        _rope_desc(table, dev, interleaved, inverse)
+        _ints(positions, "positions", dev, n) if axes is None else _axes(axes, positions, table, dev, n)
     out = _new(grad)
-    desc = CRope(table.data_ptr(), table.shape[0], 2 * table.shape[1],
-                 (ROPE_INTERLEAVED if interleaved else 0) | (0 if inverse else ROPE_INVERSE))
+    desc = CRope(table.data_ptr(), rows, 2 * pairs, (ROPE_INTERLEAVED if interleaved else 0) | (0 if inverse else ROPE_INVERSE))
     args = (SPH_F16 if grad.element_size() == 2 else SPH_F32, n, heads, dim, grad.data_ptr(), gt if n > 1 else 0, gh if heads > 1 else 0,
             positions.data_ptr(), out.data_ptr(), heads * dim, dim, _stream_handle())
     if axes is None:
         _check(_library().sph_rope(ctypes.byref(desc), *args), "sph_rope")
     else:
         count = positions.shape[0]
-        _check(_library().sph_rope_axes(ctypes.byref(desc), axes.data_ptr(), count, positions.stride(0) if count > 1 else 0, *args),
-               "sph_rope_axes")
+        _check(_library().sph_rope_axes(ctypes.byref(desc), axes.data_ptr(), count, lead[0] if count > 1 else 0, *args), "sph_rope_axes")
     return out
 
 
