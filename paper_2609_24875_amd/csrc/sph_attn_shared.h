@@ -37,7 +37,7 @@ struct SharedArgs {
   OwnArgs own;
   PrefixArgs pre;
   int* descends;           // of more prefixes than a wave looks at at once: 1 if their starts descend anywhere, else 0
-  uint32_t pre_blocks, blocks;   // workgroups of the prefixes; of them and the own tokens
+  uint32_t check, pre_blocks, blocks;   // workgroups before all others that find `descends`, 0 or 1; of the prefixes; of them and the own tokens
   int64_t pre_part;        // rows of parts before the prefixes'
   bool pre_many, own_many;
 };
@@ -57,10 +57,11 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 128 ? 2 : 1)) void k_attn_sh
   __shared__ __attribute__((aligned(16))) char lds_a[L::kA], lds_b[L::kB];
   __shared__ float2 ml_s[KIND == kManyMany ? 1 : kWaves][16 * NB];
   __shared__ int before[KIND == kManyMany ? 1 : kEvenBatch + 1], sums[KIND == kManyMany ? 1 : kEvenBatch / 32];
-  if (blockIdx.x < both.pre_blocks) {
+  const uint32_t place = blockIdx.x - both.check;            // (of the one that finds `descends`: above all others)
+  if (place < both.pre_blocks) {
     typedef PrefixArgs A;
     const A& a = both.pre;
-    const uint32_t block = blockIdx.x;
+    const uint32_t block = place;
     if constexpr (KIND == kFewFew) {
       char* lds = lds_a;
 #include "sph_attn_few.inc"
@@ -68,10 +69,10 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 128 ? 2 : 1)) void k_attn_sh
       typedef Wide<DIM, BITS> W;
 #include "sph_attn_many.inc"
     }
-  } else if (blockIdx.x < both.blocks) {
+  } else if (place < both.blocks) {
     typedef OwnArgs A;
     const A& a = both.own;
-    const uint32_t block = blockIdx.x - both.pre_blocks;
+    const uint32_t block = place - both.pre_blocks;
     if constexpr (KIND == kManyMany) {
       typedef Wide<DIM, BITS> W;
 #include "sph_attn_many.inc"
@@ -80,7 +81,7 @@ __global__ __launch_bounds__(kThreads, (DIM * NB <= 128 ? 2 : 1)) void k_attn_sh
 #include "sph_attn_few.inc"
     }
   } else {
-    // one workgroup more, where there is a `descends` to write
+    // (first of all: as the last it was the launch's end, 2 us of 603 with 1000 prefixes)
     const PrefixArgs& a = both.pre;
     bool down = false;
     for (int g = threadIdx.x; g < a.batch; g += kThreads) down |= a.first[g] > a.first[g + 1];

@@ -28,19 +28,22 @@ namespace {
 __device__ __forceinline__ int prefix_of(const PrefixArgs& a, const int* descends, int b, bool& down) {
   if (!a.first) return 0;
   const int lane = threadIdx.x & 63, all = a.batch + 1;
-  const int mine = all > 64 ? *descends : a.first[min(lane, all - 1)];
+  const int here = all > 64 ? *descends : a.first[min(lane, all - 1)], next = all > 64 ? 0 : a.first[min(lane + 1, all - 1)];
+  if (all <= 64) {
+    // (ascending, the lanes that are not above b are the first few)
+    const int last = 63 - __builtin_clzll(__ballot(lane < all && here <= b) | 1);
+    down = __any(here > next);
+    return last < a.batch && __builtin_amdgcn_readlane(here, last) <= b ? last : -1;
+  }
   int lo = 0, n = all;                                       // among the n entries from lo on, the last that is not above b
   while (n > 1) {
     const int step = (n + 63) / 64, at = lane * step;
-    const uint64_t not_above = __ballot(at < n && a.first[lo + min(at, n - 1)] <= b);
-    // (ascending, the lanes are the first few)
-    const int last = 63 - __builtin_clzll(not_above | 1);
+    const int last = 63 - __builtin_clzll(__ballot(at < n && a.first[lo + min(at, n - 1)] <= b) | 1);
     lo += last * step;
     n = min(step, n - last * step);
   }
   lo = __builtin_amdgcn_readfirstlane(lo);
-  const int below = __shfl_up(mine, 1);                      // (lane 0: its own)
-  down = __any(all > 64 ? mine != 0 : below > mine);
+  down = __any(here > next);
   return lo < a.batch && a.first[lo] <= b && b < a.first[lo + 1] ? lo : -1;
 }
 
@@ -311,14 +314,15 @@ sph_status sph_attention_shared(const sph_kv_cache* cache, int64_t prefixes, con
   b.first = d_first, b.seqs = (int)batch;
   b.part = a.part + p.own_parts * dim, b.ml = a.ml + p.own_parts, b.where = a.where + batch;
   both.descends = (int*)(a.where + batch + prefixes);
-  both.pre_blocks = (uint32_t)p.pre.grid, both.blocks = (uint32_t)(p.pre.grid + p.own.grid), both.pre_part = (int64_t)p.own_parts;
+  both.pre_blocks = (uint32_t)p.pre.grid, both.blocks = (uint32_t)(p.pre.grid + p.own.grid), both.check = d_first && p.flag ? 1 : 0;
+  both.pre_part = (int64_t)p.own_parts;
   both.pre_many = p.pre.wide, both.own_many = p.own.wide;
   const bool uni = cache->page_size >= 16;
   const int nb = p.kind == kFewFew ? p.pre.nb : p.own.nb;
   const void* fn = bits == 16  ? sph_attn_shared_kernel16(dim, p.kind, nb, uni)
                    : bits == 8 ? sph_attn_shared_kernel8(dim, p.kind, nb, uni)
                                : sph_attn_shared_kernel4(dim, p.kind, nb, uni);
-  if (!launch_ok(fn, p.pre.grid + p.own.grid + (d_first && p.flag ? 1 : 0), (hipStream_t)stream, both)) return SPH_ERR_HIP;
+  if (!launch_ok(fn, both.check + p.pre.grid + p.own.grid, (hipStream_t)stream, both)) return SPH_ERR_HIP;
   if (!launch_ok(p.few ? (const void*)k_attn_shared_join<true> : (const void*)k_attn_shared_join<false>, (p.joins + kWaves - 1) / kWaves,
                  (hipStream_t)stream, both))
     return SPH_ERR_HIP;
