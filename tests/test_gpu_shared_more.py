@@ -188,3 +188,17 @@ def test_prompts_beside_single_tokens(dim, bits):
 def test_groups_of_heads_of_prompts(group):
     new = [200, 1, 3, 0, 60]
     Case([400], [5], [2000 if n == 200 else n + 5 for n in new], new, kv=2, group=group, dim=128, bits=8).check()
+
+
+@pytest.mark.parametrize("new", [[1] * 6, [3, 1, 5, 0, 2, 1], [60, 1, 40, 0, 7, 1]])
+def test_tokens_behind_the_last_sequence(new):
+    """A padded batch, as graphs of a fixed size have: rows of no sequence stay as they are, whatever the padding holds, and the others' are the same."""
+    c = Case([90, 300], [4, 1], [n + 20 for n in new], new, dim=128, bits=8)
+    start = dict(q_start=c.start, max_q=max(new))
+    want = c.run(**start)
+    n = c.q.shape[0]
+    q = torch.full((n + 9, *c.q.shape[1:]), float("nan"), dtype=torch.float16, device=DEV)
+    q[:n] = c.q
+    out = torch.full_like(q, 7.0)
+    o, lse = c.run(q=q, out=out, **start)
+    assert o is out and torch.equal(o[:n], want[0]) and torch.equal(lse[:n], want[1]) and (o[n:] == 7).all()
