@@ -6,10 +6,10 @@
 // with m the largest, and o / l at the end. One launch does both kinds, so that the prefix's products run beside the own tokens' reads; the
 // join is the second. Parts are fp32, weights fp16 as in sph_attention: 2.2e-4 to 2.8e-4 relative to 64 bits, where a plain form has 2.1e-4.
 //
-// 32 query heads over 8 of 128 channels, fp16, kernel and join: 128 sequences of 1024 own tokens behind 32768 shared 155 + 8.5 us, bound by the prefix's
-// products and the own tokens' reads side by side (alone 100 and 92); 32 of up to 512 behind 8192 19.6 + 7.3 (alone 17.7 and 12.6), the first tiles' and the
+// 32 query heads over 8 of 128 channels, fp16, kernel and join: 128 sequences of 1024 own tokens behind 32768 shared 161 + 8 us, bound by the prefix's
+// products and the own tokens' reads side by side (alone 100 and 92); 32 of up to 512 behind 8192 19 + 7 (alone 17.7 and 12.6), the first tiles' and the
 // join's latency: a workgroup's first tile of 64 keys takes 10 us, the second 2, later ones 1.3 each. Measured and not kept, of these two and of 8 times 8 at
-// 8 bits (now 155, 20 and 41): own tokens' workgroups first 201, 28 and 50; prefixes by blocks of 32 rows through k_attn's way -, 40 and 52.
+// 8 bits (now 161, 19 and 41): own tokens' workgroups first 201, 28 and 50; prefixes by blocks of 32 rows through k_attn's way -, 40 and 52.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
